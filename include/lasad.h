@@ -452,6 +452,78 @@ int lasad_backward_layer_norm(const void *q_pre, const void *z, const void *v, c
                               const float *norm_weight, float norm_eps,
                               void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * The operators of a softmax layer between the linear-attention layers: norms and rotation of its query and key heads
+ * (below), and attention with a window and sinks.
+ *
+ * Rotation of the d / 2 pairs of a head's channels by a token's raster position p = r * W + c (0-indexed):
+ *   LASAD_ROPE_1D  pair i turns by p base^(-2i/d)
+ *   LASAD_ROPE_2D  pairs 0 .. d/4-1 turn by r base^(-4i/d), pairs d/4 + i by c base^(-4i/d)
+ * Channels of pair i: 2i and 2i + 1 (LASAD_PAIR_ADJACENT), or the two halves of what one axis turns
+ * (LASAD_PAIR_HALVES: i and i + d/2 with one axis; i and i + d/4 inside each half of the head with two).
+ * A pair (a, b) becomes (a cos - b sin, a sin + b cos).
+ */
+typedef enum { LASAD_ROPE_NONE = 0, LASAD_ROPE_1D = 1, LASAD_ROPE_2D = 2 } lasad_rope_t;
+typedef enum { LASAD_PAIR_ADJACENT = 0, LASAD_PAIR_HALVES = 1 } lasad_pairing_t;
+
+/*
+ * Norms of query and key heads with the rotation in the same pass, over positions start_pos .. start_pos + n_tokens - 1:
+ *   y = rotate(x rstd w),   rstd = 1 / sqrt(mean over the head's channels of x^2 + eps)
+ * for every head of q and of k.
+ *   q, k             [B, n_tokens, n_q_heads, d] and [B, n_tokens, n_k_heads, d], type io_dtype, each with strides of its
+ *                    own (views of one projection's output; stride 0 where they are broadcast).
+ *   q_out, k_out     the same shapes, type out_dtype (fp32, or bf16 with bf16 inputs); may be q and k themselves with the
+ *                    same type and strides, must not overlap the inputs otherwise.
+ *   q_weight, k_weight  fp32 [heads, d], with shared_weight != 0 [d] for all heads; NULL: ones.
+ *   norm_eps         negative: no norm (the weights must then be NULL), the rotation alone.
+ *   rope_base        > 1; not read without a rotation.
+ *   d                32, 64 or 128.  Pointers 16-byte aligned, strides multiples of 8 elements (fp32: 4).
+ * Arithmetic in fp32, angles in fp64.  n_tokens may be 0.
+ */
+int lasad_forward_qk(const void *q, const void *k, void *q_out, void *k_out,
+                     const lasad_layout_t *q_layout, const lasad_layout_t *k_layout,
+                     const lasad_layout_t *q_out_layout, const lasad_layout_t *k_out_layout,
+                     int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                     int grid_h, int grid_w, int start_pos, int n_tokens,
+                     const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
+                     int rope, int pairing, float rope_base, void *hip_stream);
+
+/*
+ * Gradients of lasad_forward_qk: from dL/dq_out and dL/dk_out (d_q, d_k) those of q and k, and of the weights,
+ *   dx = rstd (g w - xh mean(g w xh)),   dw = sum of g xh,   g = the output's gradient turned back, xh = x rstd.
+ *   d_q, d_k               type io_dtype, strides of their own.
+ *   dq, dk                 type grad_dtype (fp32, or bf16 with bf16 inputs); overwritten; must not overlap the inputs.
+ *   dq_weight, dk_weight   fp32, laid out like the weights ([heads, d] or, shared, [d]; a NULL weight has the gradient at
+ *                          ones); overwritten.  NULL: not formed.  Both must be NULL with norm_eps < 0.
+ *   workspace              lasad_backward_qk_workspace_bytes(...) bytes, 16-byte aligned; needed (else LASAD_ERR_WORKSPACE) if a
+ *                          weight gradient is wanted and n_tokens > 0.
+ * The sums have a fixed order: results are deterministic.
+ */
+size_t lasad_backward_qk_workspace_bytes(int B, int n_q_heads, int n_k_heads, int n_tokens, int d, int shared_weight);
+int lasad_backward_qk(const void *q, const void *k, const void *d_q, const void *d_k, void *dq, void *dk,
+                      float *dq_weight, float *dk_weight,
+                      const lasad_layout_t *q_layout, const lasad_layout_t *k_layout,
+                      const lasad_layout_t *d_q_layout, const lasad_layout_t *d_k_layout,
+                      const lasad_layout_t *dq_layout, const lasad_layout_t *dk_layout,
+                      int io_dtype, int grad_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                      int grid_h, int grid_w, int start_pos, int n_tokens,
+                      const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
+                      int rope, int pairing, float rope_base,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * lasad_forward_qk for one token of every batch row.
+ *   q, k, q_out, k_out  [B, heads, d] contiguous; in place as above.
+ *   pos                 raster position of the token, 0 <= pos < H*W; not read with pos_rows.
+ *   pos_rows            int32 [B], device: a position for every row; a row whose position is off the grid is
+ *                       inactive (its outputs are not written).  NULL: pos for all.
+ */
+int lasad_decode_step_qk(const void *q, const void *k, void *q_out, void *k_out,
+                         int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                         int grid_h, int grid_w, int pos, const int32_t *pos_rows,
+                         const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
+                         int rope, int pairing, float rope_base, void *hip_stream);
+
 /* Reason for the last non-OK status returned on this thread (static storage). */
 const char *lasad_last_error(void);
 

@@ -17,6 +17,8 @@ LIB_PATH = os.path.join(_HERE, "liblasad.so")
 
 F32, BF16 = 0, 1
 RESET_LAST_COL, RESET_FIRST_COL, RESET_NONE = 0, 1, 2
+ROPE_NONE, ROPE_1D, ROPE_2D = 0, 1, 2
+PAIR_ADJACENT, PAIR_HALVES = 0, 1
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_HIP = 0, 1, 2, 3, 4
 
 EXPORTS = (
@@ -30,6 +32,7 @@ EXPORTS = (
     "lasad_backward_gated_workspace_bytes", "lasad_backward_gated",
     "lasad_backward_gated_carried_workspace_bytes", "lasad_backward_gated_carried",
     "lasad_backward_layer_workspace_bytes", "lasad_backward_layer", "lasad_backward_layer_norm",
+    "lasad_forward_qk", "lasad_backward_qk_workspace_bytes", "lasad_backward_qk", "lasad_decode_step_qk",
     "lasad_last_error", "lasad_version",
 )
 
@@ -117,6 +120,14 @@ def load() -> ctypes.CDLL:
     lib.lasad_backward_layer_norm.argtypes = [vp, vp, vp, vp, vp, vp, lp, lp, lp, ci, ci, ci, ci, ci, ci, ci, ci, ci, ci,
                                               ctypes.c_float, vp, ctypes.c_float, vp, ctypes.c_size_t, vp]
     lib.lasad_backward_layer_norm.restype = ci
+    lib.lasad_forward_qk.argtypes = [vp] * 4 + [lp] * 4 + [ci] * 10 + [vp, vp, ci, cf, ci, ci, cf, vp]
+    lib.lasad_forward_qk.restype = ci
+    lib.lasad_backward_qk_workspace_bytes.argtypes = [ci] * 6
+    lib.lasad_backward_qk_workspace_bytes.restype = ctypes.c_size_t
+    lib.lasad_backward_qk.argtypes = [vp] * 8 + [lp] * 6 + [ci] * 10 + [vp, vp, ci, cf, ci, ci, cf, vp, ctypes.c_size_t, vp]
+    lib.lasad_backward_qk.restype = ci
+    lib.lasad_decode_step_qk.argtypes = [vp] * 4 + [ci] * 9 + [vp, vp, vp, ci, cf, ci, ci, cf, vp]
+    lib.lasad_decode_step_qk.restype = ci
     lib.lasad_last_error.argtypes = []
     lib.lasad_last_error.restype = ctypes.c_char_p
     lib.lasad_version.argtypes = []
@@ -822,6 +833,137 @@ def lasad_backward_layer_norm(q_pre: torch.Tensor, z: torch.Tensor, v: torch.Ten
         B, Hh, d, grid_h, grid_w, start_pos, n, boundary_mode, q_scale, _ptr(norm_weight), norm_eps,
         _ptr(workspace), 0 if workspace is None else workspace.numel(), _stream(stream)))
     return d_o, dweight
+
+
+# ---- the operators of a softmax layer: norms and rotation of query and key heads ----
+
+def _rows(t: torch.Tensor, what: str) -> Layout:
+    """Strides of a logical [B, n, heads, d] tensor; those of dimensions of size one, which torch may set to anything, are 0."""
+    if t.dim() != 4 or (t.shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{what} must be [B, n_tokens, heads, d] with unit stride along d")
+    if t.numel() == 0:
+        return Layout(0, t.shape[2] * t.shape[3], t.shape[3])
+    return Layout(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
+
+
+def _head_weights(q_weight, k_weight, Hq: int, Hk: int, d: int) -> bool:
+    """Checks the norm weights of query and key heads; whether they are one [d] for all heads."""
+    shared = None
+    for w, heads in ((q_weight, Hq), (k_weight, Hk)):
+        if w is None:
+            continue
+        if w.dtype != torch.float32 or not w.is_contiguous() or tuple(w.shape) not in ((d,), (heads, d)):
+            raise ValueError("norm weights must be contiguous fp32 [heads, d] or [d]")
+        if shared is not None and shared != (w.dim() == 1):
+            raise ValueError("one norm weight is shared by the heads and the other is not")
+        shared = w.dim() == 1
+    return bool(shared)
+
+
+def _qk_pair(q, k, what: str):
+    if q.dim() != k.dim() or q.shape[:-2] != k.shape[:-2] or q.shape[-1] != k.shape[-1] or q.dtype != k.dtype:
+        raise ValueError(f"{what} must share a dtype and every dimension but the heads")
+
+
+def _pair_out(given, q, k, dtype, what: str):
+    """The two tensors of `given`, checked, or new ones like q and k."""
+    if given is None:
+        return tuple(torch.empty(t.shape, dtype=dtype or t.dtype, device=t.device) for t in (q, k))
+    a, b = given
+    if a.shape != q.shape or b.shape != k.shape or a.dtype != b.dtype:
+        raise ValueError(f"{what} must have the shapes of q and k and one dtype")
+    return a, b
+
+
+def lasad_forward_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: int,
+                     q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, norm_eps: float = 1e-6,
+                     rope: int = ROPE_2D, pairing: int = PAIR_ADJACENT, rope_base: float = 10000.0, start_pos: int = 0,
+                     out: tuple | None = None, out_dtype: torch.dtype | None = None, stream=None):
+    """RMS norm of every query and key head, weight, rotation by raster position (see include/lasad.h).  q: [B, n, Hq, d],
+    k: [B, n, Hk, d] views; weights fp32 [heads, d] or [d]; norm_eps < 0 switches the norm off.  Returns the two tensors;
+    `out` may give them, (q, k) for in place."""
+    _qk_pair(q, k, "q and k")
+    lq, lk = _rows(q, "q"), _rows(k, "k")
+    B, n, Hq, d = q.shape
+    Hk = k.shape[2]
+    shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
+    qo, ko = _pair_out(out, q, k, out_dtype, "out")
+    lqo, lko = _rows(qo, "out"), _rows(ko, "out")
+    _reachable(q, k, qo, ko, q_weight, k_weight)
+    _check(load().lasad_forward_qk(
+        _ptr(q), _ptr(k), _ptr(qo), _ptr(ko), ctypes.byref(lq), ctypes.byref(lk), ctypes.byref(lqo), ctypes.byref(lko),
+        _dtype_code(q), _dtype_code(qo), B, Hq, Hk, d, grid_h, grid_w, start_pos, n,
+        _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base, _stream(stream)))
+    return qo, ko
+
+
+def lasad_backward_qk_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, n_tokens: int, d: int, shared_weight: bool) -> int:
+    return int(load().lasad_backward_qk_workspace_bytes(B, n_q_heads, n_k_heads, n_tokens, d, shared_weight))
+
+
+def lasad_backward_qk(q: torch.Tensor, k: torch.Tensor, d_q: torch.Tensor, d_k: torch.Tensor, grid_h: int, grid_w: int,
+                      q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, norm_eps: float = 1e-6,
+                      rope: int = ROPE_2D, pairing: int = PAIR_ADJACENT, rope_base: float = 10000.0, start_pos: int = 0,
+                      grads: tuple | None = None, grad_dtype: torch.dtype | None = None, want_dweight: bool = True,
+                      workspace: torch.Tensor | None = None, stream=None):
+    """Gradients of lasad_forward_qk; d_q, d_k: those of its outputs.  Returns (dq, dk, dq_weight, dk_weight); the weight
+    gradients are fp32 like the weights (without a weight: [heads, d], at ones), None without a norm or with
+    want_dweight=False."""
+    _qk_pair(q, k, "q and k")
+    if d_q.shape != q.shape or d_k.shape != k.shape or d_q.dtype != q.dtype or d_k.dtype != q.dtype:
+        raise ValueError("d_q and d_k must have the shapes and the dtype of q and k")
+    layouts = [_rows(t, what) for t, what in ((q, "q"), (k, "k"), (d_q, "d_q"), (d_k, "d_k"))]
+    B, n, Hq, d = q.shape
+    Hk = k.shape[2]
+    shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
+    dq, dk = _pair_out(grads, q, k, grad_dtype, "grads")
+    layouts += [_rows(dq, "grads"), _rows(dk, "grads")]
+    dwq = dwk = None
+    if want_dweight and norm_eps >= 0:
+        dwq, dwk = (torch.empty((d,) if shared else (heads, d), dtype=torch.float32, device=q.device) for heads in (Hq, Hk))
+        if workspace is None:
+            need = lasad_backward_qk_workspace_bytes(B, Hq, Hk, n, d, shared)
+            if need:
+                workspace = _scratch(need, q.device, stream)
+    _reachable(q, k, d_q, d_k, dq, dk, q_weight, k_weight, workspace)
+    _check(load().lasad_backward_qk(
+        _ptr(q), _ptr(k), _ptr(d_q), _ptr(d_k), _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), *(ctypes.byref(x) for x in layouts),
+        _dtype_code(q), _dtype_code(dq), B, Hq, Hk, d, grid_h, grid_w, start_pos, n,
+        _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base,
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return dq, dk, dwq, dwk
+
+
+def _step_position(pos, B: int):
+    """pos as an integer, or as a position for every batch row."""
+    if not isinstance(pos, torch.Tensor):
+        return pos, None
+    if pos.dtype != torch.int32 or pos.numel() != B or not pos.is_contiguous():
+        raise ValueError("positions of batch rows must be contiguous int32 [B]")
+    return 0, pos
+
+
+def lasad_decode_step_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: int, pos,
+                         q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, norm_eps: float = 1e-6,
+                         rope: int = ROPE_2D, pairing: int = PAIR_ADJACENT, rope_base: float = 10000.0,
+                         out: tuple | None = None, out_dtype: torch.dtype | None = None, stream=None):
+    """lasad_forward_qk for one token: q [B, Hq, d], k [B, Hk, d] contiguous; pos: an integer, or an int32 tensor [B] on the
+    device with a position for every row (off the grid: inactive, nothing written)."""
+    _qk_pair(q, k, "q and k")
+    if q.dim() != 3 or not q.is_contiguous() or not k.is_contiguous():
+        raise ValueError("q and k must be contiguous [B, heads, d]")
+    B, Hq, d = q.shape
+    Hk = k.shape[1]
+    pos, pos_rows = _step_position(pos, B)
+    shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
+    qo, ko = _pair_out(out, q, k, out_dtype, "out")
+    if not qo.is_contiguous() or not ko.is_contiguous():
+        raise ValueError("out must be contiguous")
+    _reachable(q, k, qo, ko, q_weight, k_weight, pos_rows)
+    _check(load().lasad_decode_step_qk(
+        _ptr(q), _ptr(k), _ptr(qo), _ptr(ko), _dtype_code(q), _dtype_code(qo), B, Hq, Hk, d, grid_h, grid_w, pos, _ptr(pos_rows),
+        _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base, _stream(stream)))
+    return qo, ko
 
 
 # ---- host <-> device helpers for seeded numpy inputs (no arithmetic) ---------

@@ -34,6 +34,8 @@ SOURCES = [
     "lasad_backward_gated_mfma.hip",
     "lasad_backward_gated_chunk.hip",
     "lasad_backward_layer.hip",
+    "lasad_api_attention.hip",
+    "lasad_qk.hip",
 ]
 
 # Packed-fp32 instruction selection is switched off for every HIP translation unit.

@@ -7,11 +7,11 @@
 
 #include <mutex>
 
-#include "lasad_internal.h"
+#include "lasad_attention.h"
 
-namespace {
+namespace lasad {
 
-thread_local char g_err[256] = "";
+static thread_local char g_err[256] = "";
 
 int fail(int code, const char *fmt, ...)
 {
@@ -26,6 +26,13 @@ int hip_fail(const char *what, hipError_t e)
 {
     return fail(LASAD_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+
+}  // namespace lasad
+
+using lasad::fail;
+using lasad::hip_fail;
+
+namespace {
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
@@ -85,7 +92,7 @@ int static_scratch(void **out)
 
 extern "C" {
 
-const char *lasad_last_error(void) { return g_err; }
+const char *lasad_last_error(void) { return lasad::g_err; }
 
 const char *lasad_version(void) { return "lasad 0.1 gfx950"; }
 
