@@ -524,6 +524,76 @@ int lasad_decode_step_qk(const void *q, const void *k, void *q_out, void *k_out,
                          const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
                          int rope, int pairing, float rope_base, void *hip_stream);
 
+/*
+ * Softmax attention with a sliding window and a few first tokens that stay visible (sinks), over raster positions.  Query i
+ * has position p = start_pos + i, key j position j.  It is seen if
+ *     j <= p,  j < length of the batch row,  and  p - j < window or j < sinks;
+ *     o_i = sum over the seen j of P_ij v_j,   P_ij = exp(scale q_i . k_j - lse_i),   lse_i = log sum_j exp(scale q_i . k_j).
+ * A query that sees nothing has o = 0 and lse = -infinity.  Keys that a query does not see have no part in its row, whatever
+ * their memory holds.
+ *   q         [B, n_tokens, n_q_heads, d], type io_dtype;  k, v  [B, n_keys, n_k_heads, d], type io_dtype; strides of their
+ *             own (0 where broadcast).  n_q_heads is a multiple of n_k_heads; key head h serves query heads
+ *             h G .. h G + G - 1, G = n_q_heads / n_k_heads.
+ *   o         like q, type out_dtype (fp32, or bf16 with bf16 inputs); must not overlap the inputs.
+ *   lse       [B, n_q_heads, n_tokens] fp32 or NULL.
+ *   window    >= 1 (2^31 - 1: all keys up to the query's);  sinks >= 0.
+ *   kv_lens   int32 [B], device: valid keys of each batch row (clamped to 0 .. n_keys); NULL: n_keys.
+ *   scale     > 0 and finite.
+ *   d         32, 64 or 128.  Pointers 16-byte aligned, strides multiples of 8 elements (fp32: 4).
+ * start_pos + n_tokens and n_keys are at most 2^30; either count may be 0.  Sums are fp32; with bf16 inputs P (and in the
+ * backward dS) is rounded to bf16 as a matrix-core operand.
+ */
+int lasad_forward_window(const void *q, const void *k, const void *v, void *o, float *lse,
+                         const lasad_layout_t *q_layout, const lasad_layout_t *k_layout,
+                         const lasad_layout_t *v_layout, const lasad_layout_t *o_layout,
+                         int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                         int start_pos, int n_tokens, int n_keys, int window, int sinks,
+                         const int32_t *kv_lens, float scale, void *hip_stream);
+
+/*
+ * Gradients of lasad_forward_window: with delta_i = d_o_i . o_i and dS = P (d_o v^T - delta) scale,
+ *     dq = dS k,   dk = dS^T q,   dv = P^T d_o,      dk and dv summed over the query heads that share them.
+ *   o, lse           what the forward returned (o in type io_dtype: its rounding enters delta).
+ *   d_o              like o, strides of its own.
+ *   dq, dk, dv       like q, k, v, type grad_dtype (fp32, or bf16 with bf16 inputs), strides of their own; overwritten
+ *                    (keys that nobody sees: 0); must not overlap the inputs or each other.
+ *   workspace        lasad_backward_window_workspace_bytes(...) bytes, 16-byte aligned; required (else LASAD_ERR_WORKSPACE).
+ * The sums have a fixed order: results are deterministic.
+ */
+size_t lasad_backward_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int n_keys,
+                                             int window, int sinks);
+int lasad_backward_window(const void *q, const void *k, const void *v, const void *o, const float *lse, const void *d_o,
+                          void *dq, void *dk, void *dv,
+                          const lasad_layout_t *q_layout, const lasad_layout_t *k_layout, const lasad_layout_t *v_layout,
+                          const lasad_layout_t *o_layout, const lasad_layout_t *d_o_layout,
+                          const lasad_layout_t *dq_layout, const lasad_layout_t *dk_layout, const lasad_layout_t *dv_layout,
+                          int io_dtype, int grad_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                          int start_pos, int n_tokens, int n_keys, int window, int sinks,
+                          const int32_t *kv_lens, float scale,
+                          void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * lasad_forward_window for one token of every batch row, against a cache that need not hold more than is seen:
+ * key j lies in cache row j < sinks ? j : sinks + (j - sinks) mod (cache_tokens - sinks), so that the row of
+ * a key that has left the window is taken by a new one.  This step's k and v are written to their row by the call.
+ *   q, o              [B, n_q_heads, d] contiguous, io_dtype and out_dtype;  k, v  [B, n_k_heads, d] contiguous, io_dtype.
+ *   k_cache, v_cache  [B, n_k_heads, cache_tokens, d] contiguous, io_dtype, cache_tokens > sinks; the rows of all earlier
+ *                     keys that are seen must hold them.
+ *   pos               position of the token; not read with pos_rows.  0 <= pos, and pos < cache_tokens unless
+ *                     cache_tokens >= sinks + window.
+ *   pos_rows          int32 [B], device: a position for every row; a row whose position breaks that rule is inactive
+ *                     (its output and its cache are not written).  NULL: pos for all.
+ *   workspace         lasad_decode_step_window_workspace_bytes(...) bytes, 16-byte aligned: few heads with many keys are
+ *                     then dealt out over several workgroups.  NULL: they are not (same results up to rounding); a smaller
+ *                     one is LASAD_ERR_WORKSPACE.
+ */
+size_t lasad_decode_step_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int cache_tokens, int window,
+                                                int sinks);
+int lasad_decode_step_window(const void *q, const void *k, const void *v, void *o, void *k_cache, void *v_cache,
+                             int cache_tokens, int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                             int pos, const int32_t *pos_rows, int window, int sinks, float scale,
+                             void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Reason for the last non-OK status returned on this thread (static storage). */
 const char *lasad_last_error(void);
 

@@ -33,6 +33,8 @@ EXPORTS = (
     "lasad_backward_gated_carried_workspace_bytes", "lasad_backward_gated_carried",
     "lasad_backward_layer_workspace_bytes", "lasad_backward_layer", "lasad_backward_layer_norm",
     "lasad_forward_qk", "lasad_backward_qk_workspace_bytes", "lasad_backward_qk", "lasad_decode_step_qk",
+    "lasad_forward_window", "lasad_backward_window_workspace_bytes", "lasad_backward_window",
+    "lasad_decode_step_window_workspace_bytes", "lasad_decode_step_window",
     "lasad_last_error", "lasad_version",
 )
 
@@ -128,6 +130,16 @@ def load() -> ctypes.CDLL:
     lib.lasad_backward_qk.restype = ci
     lib.lasad_decode_step_qk.argtypes = [vp] * 4 + [ci] * 9 + [vp, vp, vp, ci, cf, ci, ci, cf, vp]
     lib.lasad_decode_step_qk.restype = ci
+    lib.lasad_forward_window.argtypes = [vp] * 5 + [lp] * 4 + [ci] * 11 + [vp, cf, vp]
+    lib.lasad_forward_window.restype = ci
+    lib.lasad_backward_window_workspace_bytes.argtypes = [ci] * 8
+    lib.lasad_backward_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.lasad_backward_window.argtypes = [vp] * 9 + [lp] * 8 + [ci] * 11 + [vp, cf, vp, ctypes.c_size_t, vp]
+    lib.lasad_backward_window.restype = ci
+    lib.lasad_decode_step_window_workspace_bytes.argtypes = [ci] * 7
+    lib.lasad_decode_step_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.lasad_decode_step_window.argtypes = [vp] * 6 + [ci] * 8 + [vp, ci, ci, cf, vp, ctypes.c_size_t, vp]
+    lib.lasad_decode_step_window.restype = ci
     lib.lasad_last_error.argtypes = []
     lib.lasad_last_error.restype = ctypes.c_char_p
     lib.lasad_version.argtypes = []
@@ -964,6 +976,117 @@ def lasad_decode_step_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: 
         _ptr(q), _ptr(k), _ptr(qo), _ptr(ko), _dtype_code(q), _dtype_code(qo), B, Hq, Hk, d, grid_h, grid_w, pos, _ptr(pos_rows),
         _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base, _stream(stream)))
     return qo, ko
+
+
+# ---- attention with a window and sinks ----
+
+def _window_inputs(q, k, v, kv_lens):
+    """Checks the tensors of a forward or backward; their layouts."""
+    lq, lk, lv = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
+    if k.shape != v.shape or k.shape[0] != q.shape[0] or k.shape[3] != q.shape[3] or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError("q must be [B, n, Hq, d], k and v [B, m, Hk, d], of one dtype")
+    if kv_lens is not None and (kv_lens.dtype != torch.int32 or kv_lens.numel() != q.shape[0] or not kv_lens.is_contiguous()):
+        raise ValueError("kv_lens must be contiguous int32 [B]")
+    return lq, lk, lv
+
+
+def lasad_forward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, sinks: int = 0, start_pos: int = 0,
+                         kv_lens: torch.Tensor | None = None, scale: float | None = None,
+                         out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None, want_lse: bool = False, stream=None):
+    """Softmax attention in which position p sees the positions p - window + 1 .. p and the first `sinks` (see include/lasad.h).
+    q: [B, n, Hq, d], the tokens from start_pos on; k, v: [B, m, Hk, d], those from 0 on; kv_lens: valid keys of each batch row
+    (int32 [B] on the device); scale: d ** -0.5 unless given.  Returns o, with want_lse (o, lse [B, Hq, n])."""
+    lq, lk, lv = _window_inputs(q, k, v, kv_lens)
+    B, n, Hq, d = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out has the wrong shape")
+    lo = _rows(out, "out")
+    lse = torch.empty((B, Hq, n), dtype=torch.float32, device=q.device) if want_lse else None
+    _reachable(q, k, v, out, kv_lens)
+    _check(load().lasad_forward_window(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), ctypes.byref(lq), ctypes.byref(lk), ctypes.byref(lv), ctypes.byref(lo),
+        _dtype_code(q), _dtype_code(out), B, Hq, k.shape[2], d, start_pos, n, k.shape[1], window, sinks, _ptr(kv_lens),
+        d ** -0.5 if scale is None else scale, _stream(stream)))
+    return (out, lse) if want_lse else out
+
+
+def lasad_backward_window_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, n_tokens: int, n_keys: int, window: int,
+                                          sinks: int) -> int:
+    return int(load().lasad_backward_window_workspace_bytes(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks))
+
+
+def lasad_backward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor, d_o: torch.Tensor,
+                          window: int, sinks: int = 0, start_pos: int = 0, kv_lens: torch.Tensor | None = None,
+                          scale: float | None = None, grads: tuple | None = None, grad_dtype: torch.dtype | None = None,
+                          workspace: torch.Tensor | None = None, stream=None):
+    """Gradients of lasad_forward_window from what it returned (o in q's dtype, lse) and d_o.  Returns (dq, dk, dv); those of
+    shared key heads are summed over their query heads."""
+    lq, lk, lv = _window_inputs(q, k, v, kv_lens)
+    B, n, Hq, d = q.shape
+    m, Hk = k.shape[1:3]
+    for t in (o, d_o):
+        if t.shape != q.shape or t.dtype != q.dtype:
+            raise ValueError("o and d_o must have q's shape and dtype")
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (B, Hq, n) or not lse.is_contiguous():
+        raise ValueError("lse must be contiguous fp32 [B, Hq, n]")
+    if grads is None:
+        grads = tuple(torch.empty(t.shape, dtype=grad_dtype or q.dtype, device=q.device) for t in (q, k, v))
+    for t, x in zip(grads, (q, k, v)):
+        if t.shape != x.shape or t.dtype != grads[0].dtype:
+            raise ValueError("grads must have the shapes of q, k, v and one dtype")
+    dq, dk, dv = grads
+    layouts = [lq, lk, lv, _rows(o, "o"), _rows(d_o, "d_o"), _rows(dq, "grads"), _rows(dk, "grads"), _rows(dv, "grads")]
+    if workspace is None:
+        need = lasad_backward_window_workspace_bytes(B, Hq, Hk, d, n, m, window, sinks)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    _reachable(q, k, v, o, lse, d_o, dq, dk, dv, kv_lens, workspace)
+    _check(load().lasad_backward_window(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), *(ctypes.byref(x) for x in layouts),
+        _dtype_code(q), _dtype_code(dq), B, Hq, Hk, d, start_pos, n, m, window, sinks, _ptr(kv_lens),
+        d ** -0.5 if scale is None else scale,
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return dq, dk, dv
+
+
+def lasad_decode_step_window_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, cache_tokens: int, window: int,
+                                             sinks: int) -> int:
+    return int(load().lasad_decode_step_window_workspace_bytes(B, n_q_heads, n_k_heads, d, cache_tokens, window, sinks))
+
+
+def lasad_decode_step_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                             pos, window: int, sinks: int = 0, scale: float | None = None,
+                             out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                             workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
+    """lasad_forward_window for one token: q [B, Hq, d], k, v [B, Hk, d]; caches [B, Hk, rows, d], in which this call writes
+    k and v to the token's row (key j: row j < sinks ? j : sinks + (j - sinks) % (rows - sinks)); pos: an integer, or an int32
+    tensor [B] on the device (a row whose position does not fit the cache is inactive)."""
+    B, Hq, d = q.shape
+    _same(k, (v,), "k and v must be contiguous [B, Hk, d] of one shape and dtype")
+    if not q.is_contiguous() or k.dim() != 3 or k.shape[0] != B or k.shape[2] != d or k.dtype != q.dtype:
+        raise ValueError("q must be contiguous [B, Hq, d], k and v [B, Hk, d], of one dtype")
+    Hk = k.shape[1]
+    _same(k_cache, (v_cache,), "the caches must be contiguous, of one shape and dtype")
+    if k_cache.dim() != 4 or k_cache.shape[:2] != (B, Hk) or k_cache.shape[3] != d or k_cache.dtype != q.dtype:
+        raise ValueError("the caches must be [B, Hk, rows, d] in q's dtype")
+    rows = k_cache.shape[2]
+    pos, pos_rows = _step_position(pos, B)
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    elif out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous [B, Hq, d]")
+    if workspace is None and use_workspace:
+        need = lasad_decode_step_window_workspace_bytes(B, Hq, Hk, d, rows, window, sinks)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    _reachable(q, k, v, k_cache, v_cache, out, pos_rows, workspace)
+    _check(load().lasad_decode_step_window(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(k_cache), _ptr(v_cache), rows, _dtype_code(q), _dtype_code(out), B, Hq, Hk, d,
+        pos, _ptr(pos_rows), window, sinks, d ** -0.5 if scale is None else scale,
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
 
 
 # ---- host <-> device helpers for seeded numpy inputs (no arithmetic) ---------

@@ -36,6 +36,9 @@ SOURCES = [
     "lasad_backward_layer.hip",
     "lasad_api_attention.hip",
     "lasad_qk.hip",
+    "lasad_window_forward.hip",
+    "lasad_window_backward.hip",
+    "lasad_window_step.hip",
 ]
 
 # Packed-fp32 instruction selection is switched off for every HIP translation unit.

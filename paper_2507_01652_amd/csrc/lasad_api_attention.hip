@@ -105,6 +105,40 @@ int qk_forward(const void *q, const void *k, void *q_out, void *k_out,
     return LASAD_OK;
 }
 
+int check_window(int n_q_heads, int n_k_heads, int window, int sinks, float scale)
+{
+    if (n_q_heads % n_k_heads) return fail(LASAD_ERR_INVALID_ARG, "%d query heads cannot share %d key heads evenly", n_q_heads, n_k_heads);
+    if (window < 1 || sinks < 0) return fail(LASAD_ERR_INVALID_ARG, "window = %d, sinks = %d", window, sinks);
+    if (!(scale > 0.f && scale < INFINITY)) return fail(LASAD_ERR_INVALID_ARG, "scale must be positive and finite");
+    return LASAD_OK;
+}
+
+// Sizes of a forward or backward: what a launch counts fits 32 bits.
+int check_window_sizes(int B, int n_q_heads, int n_k_heads, int d, int start_pos, int n_tokens, int n_keys, int window, int sinks,
+                       float scale, int io_dtype, int out_dtype)
+{
+    if (int rc = check_sizes(B, n_q_heads, n_k_heads, d, n_tokens, io_dtype, out_dtype)) return rc;
+    if (int rc = check_window(n_q_heads, n_k_heads, window, sinks, scale)) return rc;
+    if (n_keys < 0 || start_pos < 0) return fail(LASAD_ERR_INVALID_ARG, "n_keys = %d, start_pos = %d", n_keys, start_pos);
+    if ((int64_t)start_pos + n_tokens > 1 << 30 || n_keys > 1 << 30) return fail(LASAD_ERR_UNSUPPORTED, "positions beyond 2^30");
+    // (workgroups of 128 queries or keys; a key head's sink tiles have up to 64 each)
+    if (((int64_t)n_tokens / 128 + 9) * B * n_q_heads > 0x7fffffff || ((int64_t)n_keys / 128 + 9) * B * n_k_heads * 64 > 0x7fffffff)
+        return fail(LASAD_ERR_UNSUPPORTED, "B * heads * tokens overflows the launch grid");
+    return LASAD_OK;
+}
+
+lasad::WindowArgs window_args(const void *q, const void *k, const void *v, int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads,
+                              int d, int start_pos, int n_tokens, int n_keys, int window, int sinks, const int32_t *kv_lens, float scale)
+{
+    lasad::WindowArgs a = {};
+    a.q = q; a.k = k; a.v = v;
+    a.io_dtype = io_dtype; a.out_dtype = out_dtype;
+    a.B = B; a.Hq = n_q_heads; a.Hk = n_k_heads; a.d = d;
+    a.start_pos = start_pos; a.n = n_tokens; a.m = n_keys;
+    a.window = window; a.sinks = sinks; a.lens = kv_lens; a.scale = scale;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -188,6 +222,137 @@ int lasad_backward_qk(const void *q, const void *k, const void *d_q, const void 
     a.dw[0] = dq_weight; a.dw[1] = dk_weight; a.partial = (float *)workspace;
     const hipError_t e = lasad::launch_qk_backward(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_backward_qk launch", e);
+    return LASAD_OK;
+}
+
+int lasad_forward_window(const void *q, const void *k, const void *v, void *o, float *lse,
+                         const lasad_layout_t *q_layout, const lasad_layout_t *k_layout,
+                         const lasad_layout_t *v_layout, const lasad_layout_t *o_layout,
+                         int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                         int start_pos, int n_tokens, int n_keys, int window, int sinks,
+                         const int32_t *kv_lens, float scale, void *hip_stream)
+{
+    if (int rc = check_window_sizes(B, n_q_heads, n_k_heads, d, start_pos, n_tokens, n_keys, window, sinks, scale, io_dtype, out_dtype)) return rc;
+    if (int rc = check_layout("q", q_layout, io_dtype, false, B, n_tokens, n_q_heads, d)) return rc;
+    if (int rc = check_layout("k", k_layout, io_dtype, false, B, n_keys, n_k_heads, d)) return rc;
+    if (int rc = check_layout("v", v_layout, io_dtype, false, B, n_keys, n_k_heads, d)) return rc;
+    if (int rc = check_layout("o", o_layout, out_dtype, true, B, n_tokens, n_q_heads, d)) return rc;
+    if (!aligned(kv_lens, 4) || !aligned(lse, 4)) return fail(LASAD_ERR_INVALID_ARG, "kv_lens and lse must be 4-byte aligned");
+    if (n_tokens == 0) return LASAD_OK;
+    if (int rc = check_pointer("q", q, 16)) return rc;
+    if (int rc = check_pointer("o", o, 16)) return rc;
+    if (n_keys > 0) {
+        if (int rc = check_pointer("k", k, 16)) return rc;
+        if (int rc = check_pointer("v", v, 16)) return rc;
+    }
+    if (o == q || o == k || o == v || (void *)lse == o) return fail(LASAD_ERR_INVALID_ARG, "o aliases another buffer");
+    lasad::WindowArgs a = window_args(q, k, v, io_dtype, out_dtype, B, n_q_heads, n_k_heads, d, start_pos, n_tokens, n_keys, window, sinks,
+                                      kv_lens, scale);
+    a.o = o; a.lse = lse;
+    a.lq = *q_layout; a.lk = *k_layout; a.lv = *v_layout; a.lo = *o_layout;
+    const hipError_t e = lasad::launch_window_forward(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail("lasad_forward_window launch", e);
+    return LASAD_OK;
+}
+
+size_t lasad_backward_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int n_keys,
+                                             int window, int sinks)
+{
+    if (B < 1 || n_q_heads < 1 || n_k_heads < 1 || d < 1 || n_tokens < 1 || n_keys < 0 || window < 1 || sinks < 0) return 0;
+    return lasad::window_backward_bytes(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks);
+}
+
+int lasad_backward_window(const void *q, const void *k, const void *v, const void *o, const float *lse, const void *d_o,
+                          void *dq, void *dk, void *dv,
+                          const lasad_layout_t *q_layout, const lasad_layout_t *k_layout, const lasad_layout_t *v_layout,
+                          const lasad_layout_t *o_layout, const lasad_layout_t *d_o_layout,
+                          const lasad_layout_t *dq_layout, const lasad_layout_t *dk_layout, const lasad_layout_t *dv_layout,
+                          int io_dtype, int grad_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                          int start_pos, int n_tokens, int n_keys, int window, int sinks,
+                          const int32_t *kv_lens, float scale,
+                          void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (int rc = check_window_sizes(B, n_q_heads, n_k_heads, d, start_pos, n_tokens, n_keys, window, sinks, scale, io_dtype, grad_dtype)) return rc;
+    const struct { const char *name; const lasad_layout_t *l; bool out, key; } layouts[] = {
+        {"q", q_layout, false, false}, {"k", k_layout, false, true}, {"v", v_layout, false, true}, {"o", o_layout, false, false},
+        {"d_o", d_o_layout, false, false}, {"dq", dq_layout, true, false}, {"dk", dk_layout, true, true}, {"dv", dv_layout, true, true}};
+    for (const auto &x : layouts)
+        if (int rc = check_layout(x.name, x.l, x.out ? grad_dtype : io_dtype, x.out, B, x.key ? n_keys : n_tokens, x.key ? n_k_heads : n_q_heads, d))
+            return rc;
+    if (!aligned(kv_lens, 4) || !aligned(lse, 4)) return fail(LASAD_ERR_INVALID_ARG, "kv_lens and lse must be 4-byte aligned");
+    if (n_tokens > 0) {
+        if (int rc = check_pointer("q", q, 16)) return rc;
+        if (int rc = check_pointer("o", o, 16)) return rc;
+        if (int rc = check_pointer("d_o", d_o, 16)) return rc;
+        if (int rc = check_pointer("dq", dq, 16)) return rc;
+        if (int rc = check_pointer("lse", lse, 4)) return rc;
+    }
+    if (n_keys > 0) {
+        if (int rc = check_pointer("k", k, 16)) return rc;
+        if (int rc = check_pointer("v", v, 16)) return rc;
+        if (int rc = check_pointer("dk", dk, 16)) return rc;
+        if (int rc = check_pointer("dv", dv, 16)) return rc;
+    }
+    const void *in[] = {q, k, v, o, d_o, lse}, *out[] = {dq, dk, dv};
+    for (int i = 0; i < 3; ++i) {
+        for (const void *p : in)
+            if (out[i] && out[i] == p) return fail(LASAD_ERR_INVALID_ARG, "a gradient aliases an input");
+        if (out[i] && out[i] == out[(i + 1) % 3]) return fail(LASAD_ERR_INVALID_ARG, "gradients alias each other");
+    }
+    const size_t need = lasad_backward_window_workspace_bytes(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks);
+    if (need > 0 && (!workspace || workspace_bytes < need))
+        return fail(LASAD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace ? workspace_bytes : (size_t)0, need);
+    if (!aligned(workspace, 16)) return fail(LASAD_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    lasad::WindowArgs a = window_args(q, k, v, io_dtype, grad_dtype, B, n_q_heads, n_k_heads, d, start_pos, n_tokens, n_keys, window, sinks,
+                                      kv_lens, scale);
+    a.o = const_cast<void *>(o); a.lse = const_cast<float *>(lse); a.d_o = d_o;
+    a.dq = dq; a.dk = dk; a.dv = dv;
+    a.lq = *q_layout; a.lk = *k_layout; a.lv = *v_layout; a.lo = *o_layout; a.ldo = *d_o_layout;
+    a.ldq = *dq_layout; a.ldk = *dk_layout; a.ldv = *dv_layout;
+    const hipError_t e = lasad::launch_window_backward(a, workspace, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail("lasad_backward_window launch", e);
+    return LASAD_OK;
+}
+
+size_t lasad_decode_step_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int cache_tokens, int window,
+                                                int sinks)
+{
+    if (B < 1 || n_q_heads < 1 || n_k_heads < 1 || d < 1 || cache_tokens < 1 || window < 1 || sinks < 0) return 0;
+    const int64_t seen = (int64_t)window + sinks < cache_tokens ? (int64_t)window + sinks : cache_tokens;
+    return lasad::window_step_bytes(B, n_q_heads, d, lasad::window_step_splits(B, n_k_heads, seen));
+}
+
+int lasad_decode_step_window(const void *q, const void *k, const void *v, void *o, void *k_cache, void *v_cache,
+                             int cache_tokens, int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                             int pos, const int32_t *pos_rows, int window, int sinks, float scale,
+                             void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    if (int rc = check_sizes(B, n_q_heads, n_k_heads, d, 1, io_dtype, out_dtype)) return rc;
+    if (int rc = check_window(n_q_heads, n_k_heads, window, sinks, scale)) return rc;
+    if ((int64_t)B * n_q_heads > 0x7fffffff) return fail(LASAD_ERR_UNSUPPORTED, "B * n_q_heads overflows the launch grid");
+    if (cache_tokens <= sinks) return fail(LASAD_ERR_INVALID_ARG, "a cache of %d rows has no room beside %d sinks", cache_tokens, sinks);
+    if (!pos_rows && (pos < 0 || (pos >= cache_tokens && cache_tokens - sinks < window)))
+        return fail(LASAD_ERR_INVALID_ARG, "pos %d does not fit a cache of %d rows (window %d, sinks %d)", pos, cache_tokens, window, sinks);
+    if (!aligned(pos_rows, 4)) return fail(LASAD_ERR_INVALID_ARG, "pos_rows must be 4-byte aligned");
+    const struct { const char *name; const void *p; } pointers[] = {{"q", q}, {"k", k}, {"v", v}, {"o", o}, {"k_cache", k_cache}, {"v_cache", v_cache}};
+    for (const auto &x : pointers)
+        if (int rc = check_pointer(x.name, x.p, 16)) return rc;
+    if (o == q || o == k || o == v || k_cache == v_cache || o == k_cache || o == v_cache || k == k_cache || v == v_cache)
+        return fail(LASAD_ERR_INVALID_ARG, "buffers alias");
+    const size_t need = lasad_decode_step_window_workspace_bytes(B, n_q_heads, n_k_heads, d, cache_tokens, window, sinks);
+    if (workspace && workspace_bytes < need) return fail(LASAD_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", workspace_bytes, need);
+    if (!aligned(workspace, 16)) return fail(LASAD_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    lasad::WindowStepArgs a = {};
+    a.q = q; a.k = k; a.v = v; a.o = o; a.k_cache = k_cache; a.v_cache = v_cache;
+    a.io_dtype = io_dtype; a.out_dtype = out_dtype;
+    a.B = B; a.Hq = n_q_heads; a.Hk = n_k_heads; a.d = d; a.cap = cache_tokens;
+    a.pos = pos; a.pos_rows = pos_rows; a.window = window; a.sinks = sinks; a.scale = scale;
+    int64_t seen = (int64_t)window + sinks < cache_tokens ? (int64_t)window + sinks : cache_tokens;
+    if (!pos_rows && (int64_t)pos + 1 < seen) seen = (int64_t)pos + 1;
+    a.parts = (float *)workspace;
+    a.splits = workspace && need ? lasad::window_step_splits(B, n_k_heads, seen) : 1;
+    const hipError_t e = lasad::launch_window_step(a, (hipStream_t)hip_stream);
+    if (e != hipSuccess) return hip_fail("lasad_decode_step_window launch", e);
     return LASAD_OK;
 }
 

@@ -31,4 +31,39 @@ hipError_t launch_qk_forward(const QkArgs &a, hipStream_t s);
 hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s);
 size_t qk_partial_bytes(int64_t tokens, int heads, int d, int shared);
 
+// Attention with a window and sinks.  Key j is seen from position p if j <= p, j < length of the batch row, and
+// p - j < window or j < sinks.
+struct WindowArgs {
+    const void *q, *k, *v, *d_o;
+    void *o, *dq, *dk, *dv;
+    float *lse;                        // [B, Hq, n]: written by the forward (or NULL), read by the backward
+    lasad_layout_t lq, lk, lv, lo, ldo, ldq, ldk, ldv;
+    int io_dtype, out_dtype, B, Hq, Hk, d, n, m;       // n queries from position start_pos on, m keys from 0 on
+    int start_pos, window, sinks;
+    const int32_t *lens;               // valid keys of the batch rows, or NULL: m
+    float scale;
+    float *delta;                      // backward workspace: [B, Hq, n] rows' sums of d_o o
+    float *parts;                      // backward workspace: partial dk and dv of the sinks' key tiles
+    int sink_tiles, sink_parts;        // plan of the backward's key pass (window_plan)
+};
+hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s);
+size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int window, int sinks);
+
+// One token against a cache [B, Hk, cap, d]: key j lies in row j < sinks ? j : sinks + (j - sinks) mod (cap - sinks).
+struct WindowStepArgs {
+    const void *q, *k, *v;
+    void *o, *k_cache, *v_cache;
+    int io_dtype, out_dtype, B, Hq, Hk, d, cap;
+    int pos;
+    const int32_t *pos_rows;
+    int window, sinks;
+    float scale;
+    float *parts;                      // workspace of splits
+    int splits;
+};
+int window_step_splits(int B, int Hk, int64_t seen);
+size_t window_step_bytes(int B, int Hq, int d, int splits);
+hipError_t launch_window_step(const WindowStepArgs &a, hipStream_t s);
+
 }  // namespace lasad

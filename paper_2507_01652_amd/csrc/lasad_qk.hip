@@ -165,7 +165,7 @@ qk_forward_kernel(QkArgs a, int tile)
 {
     constexpr int LPR = D / 8, P = D / 2, MAX_TILE = 512 / D, SLOTS = kThreads / LPR;
     constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4;
-    __shared__ float2 cs[MAX_TILE * P];
+    __shared__ __align__(16) float2 cs[MAX_TILE * P];
     __shared__ Tokens tok[MAX_TILE];
     const int64_t total = (int64_t)a.B * a.n, first = (int64_t)blockIdx.x * tile;
     const int count = (int)(total - first < tile ? total - first : tile);
@@ -243,7 +243,7 @@ qk_backward_kernel(QkArgs a, int tile)
 {
     constexpr int LPR = D / 8, P = D / 2, RPW = 64 / LPR;
     constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4;
-    __shared__ float2 cs[kBackTile * P];
+    __shared__ __align__(16) float2 cs[kBackTile * P];
     __shared__ Tokens tok[kBackTile];
     __shared__ float red[4 * 64 * 8 * (SHARED ? 2 : 1)];
     const int64_t total = (int64_t)a.B * a.n, first = (int64_t)blockIdx.x * tile;

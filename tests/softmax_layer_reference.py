@@ -100,3 +100,98 @@ def qk_backward_bound(x, w, dy, rope, halves, eps, grad_dtype, dx, last_pos=0):
     gw = g if w is None else g * w.abs()
     m = (gw * xh).mean(-1, keepdim=True)
     return 48 * U * rstd * (gw + xh * m) + stored(grad_dtype, dx), 24 * U * g * xh
+
+
+# ---- attention with a window and sinks -----------------------------------------------------------------------------
+
+def seen_mask(n, m, start, window, sinks, lens=None, B=1):
+    """[B, n, m]: does query i (position start + i) of a batch row see key j?"""
+    p, j = start + torch.arange(n)[:, None], torch.arange(m)[None]
+    seen = ((j <= p) & ((p - j < window) | (j < sinks)))[None].expand(B, n, m)
+    if lens is not None:
+        seen = seen & (j[None] < torch.as_tensor(lens).view(B, 1, 1))
+    return seen
+
+
+def shared(x, Hq):
+    """Key heads repeated for the query heads that share them: [B, m, Hk, d] -> [B, m, Hq, d]."""
+    return x.repeat_interleave(Hq // x.shape[2], 2)
+
+
+def window_forward(q, k, v, mask, scale):
+    """q [B, n, Hq, d], k, v [B, m, Hk, d] in fp64, mask [B, n, m].  Returns o and lse [B, Hq, n]."""
+    k, v = shared(k, q.shape[2]), shared(v, q.shape[2])
+    s = torch.einsum("bihd,bjhd->bhij", q, k) * scale
+    s = s.masked_fill(~mask[:, None], -math.inf)
+    lse = torch.logsumexp(s, -1) if s.shape[-1] else s.new_full(s.shape[:-1], -math.inf)
+    p = torch.exp(s - lse.masked_fill(lse == -math.inf, 0.0)[..., None])
+    return torch.einsum("bhij,bjhd->bihd", p, v), lse
+
+
+def window_backward(q, k, v, do, mask, scale):
+    """The formulas of the gradients, nothing of them by automatic differentiation (a CPU test compares the two)."""
+    Hk, Hq = k.shape[2], q.shape[2]
+    o, lse = window_forward(q, k, v, mask, scale)
+    ks, vs = shared(k, Hq), shared(v, Hq)
+    s = torch.einsum("bihd,bjhd->bhij", q, ks) * scale
+    p = torch.where(mask[:, None], torch.exp(s - lse.masked_fill(lse == -math.inf, 0.0)[..., None]), 0.0)
+    dp = torch.einsum("bihd,bjhd->bhij", do, vs)
+    ds = p * (dp - (do * o).sum(-1).transpose(1, 2)[..., None]) * scale
+    fold = lambda x: x.unflatten(2, (Hk, Hq // Hk)).sum(3)
+    return (torch.einsum("bhij,bjhd->bihd", ds, ks), fold(torch.einsum("bhij,bihd->bjhd", ds, q)),
+            fold(torch.einsum("bhij,bihd->bjhd", p, do)))
+
+
+def _rounded(dtype):
+    """Rounding of a matrix-core operand formed by the kernel."""
+    return 2.0 ** -8 if dtype == torch.bfloat16 else 0.0
+
+
+def _score_errors(q, k, mask, scale, s_abs_max=None):
+    """[B, Hq, n]: bound of the error of any seen score of a query (as a power's exponent), and how many keys it sees."""
+    a = torch.einsum("bihd,bjhd->bhij", q.abs(), shared(k, q.shape[2]).abs()) * scale
+    a = a.masked_fill(~mask[:, None], 0.0)
+    top = a.amax(-1) if a.shape[-1] else a.new_zeros(a.shape[:-1])
+    # d products added up; scaled, shifted, exponential: 8 roundings of numbers no larger than the largest sum
+    return (q.shape[-1] + 8) * U * (top + 1), mask.sum(-1)[:, None].expand(top.shape)
+
+
+def window_forward_bounds(q, k, v, mask, scale, dtype, out_dtype, o, lse):
+    """A term is off by the score's error, the sum by as much, both by one rounding an addition and a rescaling (at most two a
+    key); bf16: the term is rounded to the operand's type."""
+    e, count = _score_errors(q, k, mask, scale)
+    pv, _ = window_forward(q, k, v.abs(), mask, scale)
+    rel = 2 * e + (4 * count + 16) * U + _rounded(dtype)
+    lse_bound = e + (2 * count + 16) * U + 4 * U * lse.masked_fill(lse == -math.inf, 0.0).abs()
+    return pv * rel.transpose(1, 2)[..., None] + stored(out_dtype, o), lse_bound
+
+
+def window_backward_bounds(q, k, v, do, mask, scale, dtype, grad_dtype, grads):
+    """P is off by the score's error and that of lse; dP by its d products; delta by its d products and by o's error, storing
+    included; dS by all of these and its rounding as an operand; a sum by one rounding an addition."""
+    Hk, Hq, d = k.shape[2], q.shape[2], q.shape[3]
+    ks, vs = shared(k, Hq), shared(v, Hq)
+    o, lse = window_forward(q, k, v, mask, scale)
+    e, count = _score_errors(q, k, mask, scale)
+    o_bound, lse_bound = window_forward_bounds(q, k, v, mask, scale, dtype, dtype, o, lse)
+    s = torch.einsum("bihd,bjhd->bhij", q, ks) * scale
+    p = torch.where(mask[:, None], torch.exp(s - lse.masked_fill(lse == -math.inf, 0.0)[..., None]), 0.0)
+    dp = torch.einsum("bihd,bjhd->bhij", do, vs)
+    g = torch.einsum("bihd,bjhd->bhij", do.abs(), vs.abs())
+    delta = (do * o).sum(-1).transpose(1, 2)[..., None]
+    delta_bound = ((do.abs() * o_bound).sum(-1) + d * U * (do * o).abs().sum(-1)).transpose(1, 2)[..., None]
+    p_rel = (e + lse_bound + 8 * U)[..., None]
+    x = p * (dp - delta).abs()
+    ds_err = (x * (p_rel + 4 * U + _rounded(dtype)) + p * ((d + 2) * U * g + delta_bound + 2 * U * delta.abs())) * scale
+    ds_abs = x * scale
+    fold = lambda t: t.unflatten(2, (Hk, Hq // Hk)).sum(3)
+    keys = (count.amax() + 16) * U
+    queries = ((mask.sum(1).amax() if mask.numel() else 0) * (Hq // Hk) + 80) * U
+    dq = torch.einsum("bhij,bjhd->bihd", ds_err + keys * ds_abs, ks.abs())
+    dk = fold(torch.einsum("bhij,bihd->bjhd", ds_err + queries * ds_abs, q.abs()))
+    dv = fold(torch.einsum("bhij,bihd->bjhd", p * (p_rel + queries + _rounded(dtype)), do.abs()))
+    return [b + stored(grad_dtype, t) for b, t in zip((dq, dk, dv), grads)]
+
+
+def cache_row(j, sinks, rows):
+    return j if j < sinks else sinks + (j - sinks) % (rows - sinks)
