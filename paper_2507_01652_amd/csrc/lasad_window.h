@@ -88,6 +88,18 @@ __device__ inline f32x16 zeros16()
     return z;
 }
 
+// x of this lane and of the one 32 lanes away, joined
+__device__ inline float both_halves_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float both_halves_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // row of a lane's register i in a 32 x 32 block
 __device__ inline int block_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 
@@ -104,6 +116,36 @@ __device__ inline bool sees_none(const WindowArgs &a, int keys, int p0, int p1, 
 __device__ inline bool sees_all(const WindowArgs &a, int keys, int p0, int p1, int j0, int j1)
 {
     return j1 <= p0 && j1 < keys && (p1 - j0 < a.window || j1 < a.sinks);
+}
+
+// What a column's query sees of the rows of a block of keys (or a column's key of the rows of a block of queries): rows
+// lo .. hi, and those before `first`.  Two comparisons with a constant an entry, and which of them a block needs is the same for
+// the whole wavefront, so that a block inside the window pays none.
+struct Edge {
+    int lo, hi, first;
+};
+__device__ inline Edge query_edge(const WindowArgs &a, int keys, int p)
+{
+    const int hi = min(p, keys - 1);
+    return {max(0, p - a.window + 1), hi, min(a.sinks, hi + 1)};
+}
+__device__ inline Edge key_edge(const WindowArgs &a, int keys, int j)
+{
+    const int far = 0x5fffffff;                          // (behind all positions, and a block's offset may be taken off)
+    return {j < keys ? j : far, j < a.sinks ? far : (int)min((int64_t)far, (int64_t)j + a.window - 1), 0};
+}
+// x in the entries of block rows r0 .. r0 + 31 that are not seen; top, bottom: rows behind hi, before lo are among them
+__device__ inline void hide(f32x16 &s, const Edge &e, int r0, int half, bool top, bool bottom, float x)
+{
+    const int hi = e.hi - r0 - 4 * half, lo = e.lo - r0 - 4 * half, first = e.first - r0 - 4 * half;
+    if (top) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) <= hi ? s[i] : x;
+    }
+    if (bottom) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) >= lo || 8 * (i >> 2) + (i & 3) < first ? s[i] : x;
+    }
 }
 // valid keys of batch row b
 __device__ inline int valid_keys(const WindowArgs &a, int b)

@@ -18,16 +18,61 @@ namespace {
 
 constexpr int kThreads = 256, kTile = 128;               // queries (keys) of a workgroup
 
+// NB blocks of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: dS, and its product with k.
+template <typename T, int D, int NB>
+__device__ inline void dq_blocks(const WindowArgs &a, const typename Mat<T>::F (&q)[D / Mat<T>::KF], const typename Mat<T>::F (&g)[D / Mat<T>::KF],
+                                 const T *kt, const T *vt, int j0, int keys, int p0, const Edge &edge, float scale2, float lse2, float delta,
+                                 int lane, f32x16 (&acc)[D / 32])
+{
+    typedef Mat<T> M;
+    typedef typename M::F F;
+    constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
+    constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
+    const int half = lane >> 5, col = lane & 31;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const T *kb = kt + b * 32 * LD, *vb = vt + b * 32 * LD;
+        F kf[NF], vf[NF], kc[M::GROUPS][DB];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) { kf[f] = M::row(kb + col * LD, f, half); vf[f] = M::row(vb + col * LD, f, half); }
+        const auto columns = [&]() {
+#pragma unroll
+            for (int r = 0; r < M::GROUPS; ++r)
+#pragma unroll
+                for (int d = 0; d < DB; ++d) kc[r][d] = M::column(kb, LD, d * 32, r, lane);
+        };
+        if (EARLY) {
+            columns();
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+        for (int f = 0; f < NF; ++f) { s = M::mma(kf[f], q[f], s); dp = M::mma(vf[f], g[f], dp); }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)) * (dp[i] - delta);
+        const int jb = j0 + 32 * b;
+        const bool top_edge = jb + 31 > p0 || jb + 31 >= keys, bottom_edge = p0 + 31 - jb >= a.window;
+        if (top_edge || bottom_edge) hide(s, edge, jb, half, top_edge, bottom_edge, 0.f);
+        if (!EARLY) columns();
+#pragma unroll
+        for (int r = 0; r < M::GROUPS; ++r) {
+            const F ds = M::pack(s, r);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] = M::mma(kc[r][d], ds, acc[d]);
+        }
+    }
+}
+
 template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, D <= 32 ? 3 : D <= 64 ? 2 : 1)
 window_dq_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
     typedef typename M::F F;
     constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, KB = KT / 32, DB = D / 32, NF = D / M::KF;
-    constexpr int N = KT * D / M::VEC / kThreads, PPR = D / M::VEC;
+    constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = KT / RPP;
     __shared__ __align__(16) T tile[2][2][KT * LD];
-    __shared__ int infinite[2];                          // number of the last tile in this half whose keys are not all finite
+    __shared__ int infinite;                             // whether a key that was taken out of a tile was not finite
 
     const int qt = (a.n + kTile - 1) / kTile;
     const int64_t id = xcd_run(blockIdx.x, (int64_t)qt * a.B * a.Hq);
@@ -43,6 +88,55 @@ window_dq_kernel(WindowArgs a)
     const T *kp = (const T *)a.k + (int64_t)b * a.lk.stride_b + (int64_t)hk * a.lk.stride_h;
     const T *vp = (const T *)a.v + (int64_t)b * a.lv.stride_b + (int64_t)hk * a.lv.stride_h;
 
+    const float scale2 = a.scale * kLog2e;
+    const Edge edge = query_edge(a, keys, p);
+
+    const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
+    const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
+    uint4 kr[N], vr[N];
+    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
+    const int row0 = threadIdx.x / PPR, col0 = (threadIdx.x % PPR) * M::VEC;
+    const int64_t koff = row0 * a.lk.stride_n + col0, voff = row0 * a.lv.stride_n + col0;
+    const auto load = [&](int t) {                       // (as in the forward)
+        const int j0 = at(t);
+        const T *k0 = kp + j0 * a.lk.stride_n, *v0 = vp + j0 * a.lv.stride_n;
+        int64_t ko[N], vo[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) { ko[i] = koff + i * RPP * a.lk.stride_n; vo[i] = voff + i * RPP * a.lv.stride_n; }
+        if (j0 + KT - 1 > hi) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t row = min(row0 + i * RPP, hi - j0);
+                ko[i] = row * a.lk.stride_n + col0;
+                vo[i] = row * a.lv.stride_n + col0;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            kr[i] = *(const uint4 *)(k0 + ko[i]);
+            vr[i] = *(const uint4 *)(v0 + vo[i]);
+        }
+    };
+    const auto whole = [&](int t) { return sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1); };
+    const auto store = [&](int t) {
+        if (!whole(t)) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int j = at(t) + row0 + i * RPP;
+                if (j > hi || (j < lo && j >= a.sinks)) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+                bad |= make_finite<T>(kr[i]);
+            }
+            if (bad) infinite = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            *(uint4 *)(tile[t & 1][0] + (row0 + i * RPP) * LD + col0) = kr[i];
+            *(uint4 *)(tile[t & 1][1] + (row0 + i * RPP) * LD + col0) = vr[i];
+        }
+    };
+    if (threadIdx.x == 0) infinite = 0;
+    if (tiles > 0) load(0);
     F q[NF], g[NF];
     float delta = 0.f, lse2 = INFINITY;
     {
@@ -56,7 +150,7 @@ window_dq_kernel(WindowArgs a)
             g[f] = on ? M::row(gp, f, half) : M::zero();
             if (on) delta += M::dot(g[f], M::row(op, f, half));
         }
-        delta += __shfl_xor(delta, 32);
+        delta = both_halves_sum(delta);
         if (on) {
             lse2 = a.lse[(int64_t)bh * a.n + iq] * kLog2e;
             if (half == 0) a.delta[(int64_t)bh * a.n + iq] = delta;
@@ -65,81 +159,37 @@ window_dq_kernel(WindowArgs a)
     f32x16 acc[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zeros16();
-    const float scale2 = a.scale * kLog2e;
-
-    const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
-    const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
-    uint4 kr[N], vr[N];
-    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
-    const auto load = [&](int j0) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * kThreads, j = j0 + c / PPR;
-            kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-            if (j <= hi && (j >= lo || j < a.sinks)) {
-                kr[i] = *(const uint4 *)(kp + (int64_t)j * a.lk.stride_n + (c % PPR) * M::VEC);
-                vr[i] = *(const uint4 *)(vp + (int64_t)j * a.lv.stride_n + (c % PPR) * M::VEC);
-            }
-        }
-    };
-    const auto store = [&](int t) {
-        if (!sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1)) {
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < N; ++i) bad |= make_finite<T>(kr[i]);
-            if (bad) infinite[t & 1] = t;
-        }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * kThreads, at = (c / PPR) * LD + (c % PPR) * M::VEC;
-            *(uint4 *)(tile[t & 1][0] + at) = kr[i];
-            *(uint4 *)(tile[t & 1][1] + at) = vr[i];
-        }
-    };
-    if (threadIdx.x < 2) infinite[threadIdx.x] = -1;
-    if (tiles > 0) load(at(0));
+    // (the loop would wait for everything in flight if it might have to wait for the queries)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
     if (tiles > 0) store(0);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
         const int j0 = at(t);
-        if (t + 1 < tiles) load(at(t + 1));
-        if (!sees_none(a, keys, p0, p1, j0, j0 + KT - 1)) {
-            const T *kt = tile[t & 1][0], *vt = tile[t & 1][1];
-            const bool all = sees_all(a, keys, p0, p1, j0, j0 + KT - 1);
+        const T *kt = tile[t & 1][0], *vt = tile[t & 1][1];
+        load(min(t + 1, tiles - 1));
+        const auto none = [&](int b) { return sees_none(a, keys, p0, p1, j0 + 32 * b, j0 + 32 * b + 31); };
+        const int from = KB == 1 || !none(0) ? 0 : 1, to = KB == 2 && !none(1) ? 2 : 1;
+        if (KB == 2 && to - from == 2)
+            dq_blocks<T, D, KB>(a, q, g, kt, vt, j0, keys, p0, edge, scale2, lse2, delta, lane, acc);
+        else if (to > from && !none(from))
+            dq_blocks<T, D, 1>(a, q, g, kt + from * 32 * LD, vt + from * 32 * LD, j0 + 32 * from, keys, p0, edge, scale2, lse2, delta, lane, acc);
+        if (t + 1 < tiles) store(t + 1);
+        __syncthreads();
+    }
+    if (infinite) {                                      // (a seen key that is not finite: so is the row's gradient)
+        for (int t = 0; t < tiles; ++t) {
+            if (whole(t)) continue;                      // (as it was)
+            for (int j = at(t); j < min(at(t) + KT, keys); ++j) {
+                const bool bad = row_infinite<T, D>(kp + (int64_t)j * a.lk.stride_n, lane);
+                if (bad && sees(a, keys, p, j)) {
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                f32x16 s = zeros16(), dp = zeros16();
+                    for (int d = 0; d < DB; ++d)
 #pragma unroll
-                for (int f = 0; f < NF; ++f) s = M::mma(M::row(kt + (kb * 32 + col) * LD, f, half), q[f], s);
-#pragma unroll
-                for (int f = 0; f < NF; ++f) dp = M::mma(M::row(vt + (kb * 32 + col) * LD, f, half), g[f], dp);
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)) * (dp[i] - delta);
-                    s[i] = all || sees(a, keys, p, j0 + kb * 32 + block_row(i, half)) ? x : 0.f;
-                }
-#pragma unroll
-                for (int gr = 0; gr < M::GROUPS; ++gr) {
-                    const F ds = M::pack(s, gr);
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) acc[d] = M::mma(M::column(kt + kb * 32 * LD, LD, d * 32, gr, lane), ds, acc[d]);
-                }
-            }
-            if (infinite[t & 1] == t) {                  // (a seen key that is not finite: so is the row's gradient)
-                for (int j = j0; j < min(j0 + KT, keys); ++j) {
-                    const bool bad = row_infinite<T, D>(kp + (int64_t)j * a.lk.stride_n, lane);
-                    if (bad && sees(a, keys, p, j)) {
-#pragma unroll
-                        for (int d = 0; d < DB; ++d)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[d][i] = NAN;
-                    }
+                        for (int i = 0; i < 16; ++i) acc[d][i] = NAN;
                 }
             }
         }
-        if (t + 1 < tiles) store(t + 1);
-        __syncthreads();
     }
     if (iq >= a.n) return;
     O *dq = (O *)a.dq + (int64_t)b * a.ldq.stride_b + (int64_t)iq * a.ldq.stride_n + (int64_t)h * a.ldq.stride_h;
@@ -151,18 +201,81 @@ window_dq_kernel(WindowArgs a)
                    acc[d][4 * r + 3] * a.scale);
 }
 
+// One block of 32 queries (positions from pb on, rows of qt and gt, their lse and delta) for a wavefront's keys: P and dS, and
+// their products with d_o and q.
+template <typename T, int D>
+__device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (&k)[D / Mat<T>::KF], const typename Mat<T>::F (&v)[D / Mat<T>::KF],
+                                 const T *qt, const T *gt, const float *lse2, const float *delta, int pb, int keys, int w0, const Edge &edge,
+                                 float scale2, int lane, f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32])
+{
+    typedef Mat<T> M;
+    typedef typename M::F F;
+    constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
+    constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
+    const int half = lane >> 5, col = lane & 31;
+    F qf[NF], gf[NF], qc[M::GROUPS][DB], gc[M::GROUPS][DB];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) { qf[f] = M::row(qt + col * LD, f, half); gf[f] = M::row(gt + col * LD, f, half); }
+    float ls[16], de[16];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const float4 x = *(const float4 *)(lse2 + 8 * r + 4 * half), y = *(const float4 *)(delta + 8 * r + 4 * half);
+        ls[4 * r] = x.x; ls[4 * r + 1] = x.y; ls[4 * r + 2] = x.z; ls[4 * r + 3] = x.w;
+        de[4 * r] = y.x; de[4 * r + 1] = y.y; de[4 * r + 2] = y.z; de[4 * r + 3] = y.w;
+    }
+    const auto columns = [&]() {
+#pragma unroll
+        for (int r = 0; r < M::GROUPS; ++r)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) {
+                gc[r][d] = M::column(gt, LD, d * 32, r, lane);
+                qc[r][d] = M::column(qt, LD, d * 32, r, lane);
+            }
+    };
+    if (EARLY) {
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+    for (int f = 0; f < NF; ++f) { s = M::mma(qf[f], k[f], s); dp = M::mma(gf[f], v[f], dp); }
+    if (EARLY) {
+        columns();
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -ls[i]));
+        dp[i] = s[i] * (dp[i] - de[i]);
+    }
+    const bool first_edge = pb < w0 + 31 || w0 + 31 >= keys, last_edge = pb + 31 - w0 >= a.window;
+    if (first_edge || last_edge) {
+        hide(s, edge, pb, half, last_edge, first_edge, 0.f);
+        hide(dp, edge, pb, half, last_edge, first_edge, 0.f);
+    }
+    if (!EARLY) columns();
+#pragma unroll
+    for (int r = 0; r < M::GROUPS; ++r) {
+        const F pf = M::pack(s, r), df = M::pack(dp, r);
+#pragma unroll
+        for (int d = 0; d < DB; ++d) {
+            dv[d] = M::mma(gc[r][d], pf, dv[d]);
+            dk[d] = M::mma(qc[r][d], df, dk[d]);
+        }
+    }
+}
+
 // Workgroups: first the sinks' key tiles, part after part, then the others.
 template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, D <= 64 ? 2 : 1)
 window_dkv_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
     typedef typename M::F F;
     constexpr int QT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, QB = QT / 32, DB = D / 32, NF = D / M::KF;
-    constexpr int N = QT * D / M::VEC / kThreads, PPR = D / M::VEC;
+    constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = QT / RPP;
     __shared__ __align__(16) T tile[2][2][QT * LD];
-    __shared__ int infinite[2];                          // number of the last step in this half whose rows are not all finite
     __shared__ __align__(16) float stat[2][2][QT];       // lse (in powers of two) and delta of a tile's queries
+    __shared__ int infinite;                             // whether a row that was taken out of a tile was not finite
 
     const int kt = (a.m + kTile - 1) / kTile;
     const int units = a.sink_tiles * a.sink_parts + kt - a.sink_tiles;      // workgroups of a key head
@@ -193,6 +306,7 @@ window_dkv_kernel(WindowArgs a)
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zeros16();
     const float scale2 = a.scale * kLog2e;
+    const Edge edge = key_edge(a, keys, jk);
 
     // queries that see any key of the tile, in tiles of QT counted from the first query; this part's share of them
     const int j1 = min(j0 + kTile, keys) - 1;                        // (no valid key: j1 < j0)
@@ -208,92 +322,81 @@ window_dkv_kernel(WindowArgs a)
     const int64_t stat0 = ((int64_t)b * a.Hq + hk * G) * a.n;
     uint4 qr[N], gr[N];
     float sr = 0.f;
-    int i_next = 0, h_next = 0;                          // tile (of the share) and head that are loaded next
-    const auto load = [&]() {
-        const int i0 = (t_first + i_next) * QT;
+    const int row0 = threadIdx.x / PPR, col0 = (threadIdx.x % PPR) * M::VEC;
+    const int64_t qoff = row0 * a.lq.stride_n + col0, goff = row0 * a.ldo.stride_n + col0;
+    const float *statp = threadIdx.x < QT ? a.lse : a.delta;
+    const auto load = [&](int ti, int hi) {              // tile (of the share) of a head of the group; rows behind the last: the last
+        const int i0 = (t_first + ti) * QT;
+        const T *q0 = qp + i0 * a.lq.stride_n + hi * a.lq.stride_h, *g0 = gp + i0 * a.ldo.stride_n + hi * a.ldo.stride_h;
+        int64_t qo[N], go[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * kThreads, iq = i0 + c / PPR;
-            qr[i] = gr[i] = make_uint4(0, 0, 0, 0);
-            if (iq < a.n) {
-                qr[i] = *(const uint4 *)(qp + (int64_t)iq * a.lq.stride_n + h_next * a.lq.stride_h + (c % PPR) * M::VEC);
-                gr[i] = *(const uint4 *)(gp + (int64_t)iq * a.ldo.stride_n + h_next * a.ldo.stride_h + (c % PPR) * M::VEC);
+        for (int i = 0; i < N; ++i) { qo[i] = qoff + i * RPP * a.lq.stride_n; go[i] = goff + i * RPP * a.ldo.stride_n; }
+        if (i0 + QT > a.n) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t row = min(row0 + i * RPP, a.n - 1 - i0);
+                qo[i] = row * a.lq.stride_n + col0;
+                go[i] = row * a.ldo.stride_n + col0;
             }
         }
-        if (threadIdx.x < 2 * QT) {
-            const int iq = i0 + threadIdx.x % QT;
-            const float *x = threadIdx.x < QT ? a.lse : a.delta;
-            sr = iq < a.n ? x[stat0 + (int64_t)h_next * a.n + iq] : threadIdx.x < QT ? INFINITY : 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            qr[i] = *(const uint4 *)(q0 + qo[i]);
+            gr[i] = *(const uint4 *)(g0 + go[i]);
         }
-        if (++i_next == t_count) { i_next = 0; ++h_next; }
+        if (threadIdx.x < 2 * QT) sr = statp[stat0 + (int64_t)hi * a.n + min(i0 + (int)threadIdx.x % QT, a.n - 1)];
     };
-    const auto store = [&](int t) {                      // step t, whose loads came last
-        const int buf = t & 1, p0 = a.start_pos + (t_first + t % t_count) * QT;
-        if (!sees_all(a, keys, p0, p0 + QT - 1, j0, j0 + kTile - 1)) {
+    const auto whole = [&](int ti) {
+        const int p0 = a.start_pos + (t_first + ti) * QT;
+        return (t_first + ti + 1) * QT <= a.n && sees_all(a, keys, p0, p0 + QT - 1, j0, j0 + kTile - 1);
+    };
+    const auto store = [&](int buf, int ti) {            // what was loaded last
+        const int i0 = (t_first + ti) * QT;
+        if (!whole(ti)) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
+                if (i0 + row0 + i * RPP >= a.n) qr[i] = gr[i] = make_uint4(0, 0, 0, 0);
                 bad |= make_finite<T>(qr[i]);
                 bad |= make_finite<T>(gr[i]);
             }
-            if (bad) infinite[buf] = t;
+            if (bad) infinite = 1;
+            if (i0 + (int)threadIdx.x % QT >= a.n) sr = threadIdx.x < QT ? INFINITY : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * kThreads, at = (c / PPR) * LD + (c % PPR) * M::VEC;
-            *(uint4 *)(tile[buf][0] + at) = qr[i];
-            *(uint4 *)(tile[buf][1] + at) = gr[i];
+            *(uint4 *)(tile[buf][0] + (row0 + i * RPP) * LD + col0) = qr[i];
+            *(uint4 *)(tile[buf][1] + (row0 + i * RPP) * LD + col0) = gr[i];
         }
         if (threadIdx.x < 2 * QT) stat[buf][threadIdx.x / QT][threadIdx.x % QT] = threadIdx.x < QT ? sr * kLog2e : sr;
     };
-    if (threadIdx.x < 2) infinite[threadIdx.x] = -1;
-    if (steps > 0) load();
+    if (threadIdx.x == 0) infinite = 0;
+    if (steps > 0) load(0, 0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);                  // (as in the query pass)
     __syncthreads();
-    if (steps > 0) store(0);
+    if (steps > 0) store(0, 0);
     __syncthreads();
     int ti = 0, hi = 0;                                  // tile and head of the present step
     for (int t = 0; t < steps; ++t) {
-        const int p0 = a.start_pos + (t_first + ti) * QT, p1 = p0 + QT - 1;
-        if (t + 1 < steps) load();
-        if (!sees_none(a, keys, p0, p1, w0, w1)) {
-            const T *qt = tile[t & 1][0], *gt = tile[t & 1][1];
-            const bool all = sees_all(a, keys, p0, p1, w0, w1);
+        const int p0 = a.start_pos + (t_first + ti) * QT;
+        if (++ti == t_count) { ti = 0; ++hi; }
+        if (t + 1 < steps) load(ti, hi);
+        const T *qt = tile[t & 1][0], *gt = tile[t & 1][1];
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-                f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-                for (int f = 0; f < NF; ++f) s = M::mma(M::row(qt + (qb * 32 + col) * LD, f, half), k[f], s);
-#pragma unroll
-                for (int f = 0; f < NF; ++f) dp = M::mma(M::row(gt + (qb * 32 + col) * LD, f, half), v[f], dp);
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float4 ls = *(const float4 *)(stat[t & 1][0] + qb * 32 + 8 * r + 4 * half);
-                    const float4 de = *(const float4 *)(stat[t & 1][1] + qb * 32 + 8 * r + 4 * half);
-                    const float lsx[4] = {ls.x, ls.y, ls.z, ls.w}, dex[4] = {de.x, de.y, de.z, de.w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int i = 4 * r + e;
-                        const bool on = all || sees(a, keys, p0 + qb * 32 + block_row(i, half), jk);
-                        const float pr = on ? __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lsx[e])) : 0.f;
-                        dp[i] = on ? pr * (dp[i] - dex[e]) : 0.f;
-                        s[i] = pr;
-                    }
-                }
-#pragma unroll
-                for (int g = 0; g < M::GROUPS; ++g) {
-                    const F pf = M::pack(s, g), df = M::pack(dp, g);
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) {
-                        dv[d] = M::mma(M::column(gt + qb * 32 * LD, LD, d * 32, g, lane), pf, dv[d]);
-                        dk[d] = M::mma(M::column(qt + qb * 32 * LD, LD, d * 32, g, lane), df, dk[d]);
-                    }
-                }
-            }
-            if (infinite[t & 1] == t) {                  // (a query that is not finite: so are the gradients of all keys it sees)
-                for (int p = p0; p < min(p0 + QT, a.start_pos + a.n); ++p) {
-                    const int64_t iq = p - a.start_pos;
-                    const bool on = sees(a, keys, p, jk), bad = row_infinite<T, D>(qp + iq * a.lq.stride_n + hi * a.lq.stride_h, lane);
-                    add_infinite<T, DB>(gp + iq * a.ldo.stride_n + hi * a.ldo.stride_h, on, half, dv);
+        for (int qb = 0; qb < QB; ++qb)
+            if (!sees_none(a, keys, p0 + 32 * qb, p0 + 32 * qb + 31, w0, w1))
+                dkv_block<T, D>(a, k, v, qt + qb * 32 * LD, gt + qb * 32 * LD, stat[t & 1][0] + 32 * qb, stat[t & 1][1] + 32 * qb, p0 + 32 * qb,
+                                keys, w0, edge, scale2, lane, dk, dv);
+        if (t + 1 < steps) store((t + 1) & 1, ti);
+        __syncthreads();
+    }
+    if (infinite) {                                      // (a query that is not finite: so are the gradients of all keys it sees)
+        for (int h = 0; h < G; ++h)
+            for (int t = 0; t < t_count; ++t) {
+                if (whole(t)) continue;                  // (as they were)
+                for (int iq = (t_first + t) * QT; iq < min((t_first + t + 1) * QT, a.n); ++iq) {
+                    const bool on = sees(a, keys, a.start_pos + iq, jk), bad = row_infinite<T, D>(qp + iq * a.lq.stride_n + h * a.lq.stride_h, lane);
+                    add_infinite<T, DB>(gp + iq * a.ldo.stride_n + h * a.ldo.stride_h, on, half, dv);
                     if (bad && on) {
 #pragma unroll
                         for (int d = 0; d < DB; ++d)
@@ -302,10 +405,6 @@ window_dkv_kernel(WindowArgs a)
                     }
                 }
             }
-        }
-        if (++ti == t_count) { ti = 0; ++hi; }
-        if (t + 1 < steps) store(t + 1);
-        __syncthreads();
     }
     if (parts > 1) {                                     // (whole tiles, rows past the last key included)
         float *out = a.parts + (((int64_t)bh * a.sink_tiles * a.sink_parts + unit) * 2 * kTile + 32 * wave + col) * D;
@@ -359,13 +458,17 @@ window_sink_sum_kernel(WindowArgs a)
     store4(out, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
-// Key tiles with sinks and the parts they are cut into: a part walks about as many queries as an ordinary tile has.
-// (None where the sinks' tiles alone are workgroups enough: at most 1024 parts in all, which bounds the workspace.)
+// Key tiles with sinks and the parts they are cut into.  In steps of 64 queries: an ordinary tile takes (window + 128) / 64, one
+// with sinks n / 64.  Uncut it ends last where it takes longer than an ordinary one and than half of what the chip's 512
+// workgroup slots have to do anyway; a part takes about that long.  At most 1024 parts, which bounds the workspace.
 void plan(int64_t heads, int n, int m, int window, int sinks, int &tiles, int &parts)
 {
-    const int64_t ordinary = (int64_t)window + kTile;
     tiles = (int)(((int64_t)(sinks < m ? sinks : m) + kTile - 1) / kTile);
-    const int64_t want = (n + ordinary - 1) / ordinary, most = tiles > 0 ? 1024 / (heads * tiles) : 1;
+    const int64_t all = ((int64_t)m + kTile - 1) / kTile, sink = (n + 63) / 64, near = ((int64_t)window + kTile + 63) / 64;
+    const int64_t ordinary = near < sink ? near : sink;
+    const int64_t slot = heads * ((all - tiles) * ordinary + tiles * sink) / 512;
+    const int64_t long_enough = ordinary > slot / 2 ? ordinary : slot / 2;
+    const int64_t want = long_enough > 0 ? (sink + long_enough - 1) / long_enough : 1, most = tiles > 0 ? 1024 / (heads * tiles) : 1;
     parts = (int)(want > most ? most : want);
     parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
 }

@@ -13,43 +13,102 @@ namespace lasad {
 namespace {
 
 constexpr int kThreads = 256, kQueries = 128;
+constexpr float kSlack = 8.f;
 
-// Rows j0 .. j0 + KT - 1 of one head's keys or values, a thread's 16-byte pieces; what no query of the workgroup may see is 0
-// (so that what lies there cannot reach a sum as 0 * NaN).
-template <typename T, int D, int KT, int N>
-__device__ inline void load_tile(uint4 (&r)[N], const T *base, int64_t stride_n, int j0, int lo, int hi, int sinks)
+// NB blocks of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: scores, their exponentials, products with v.
+template <typename T, int D, int NB>
+__device__ inline void forward_blocks(const WindowArgs &a, const typename Mat<T>::F (&q)[D / Mat<T>::KF], const T *kt, const T *vt, int j0,
+                                      int keys, int p0, const Edge &edge, float scale2, int lane, float &m, float &l, f32x16 (&acc)[D / 32])
 {
-    constexpr int PPR = D / Mat<T>::VEC;                 // pieces of a row
+    typedef Mat<T> M;
+    constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
+    const int half = lane >> 5, col = lane & 31;
+    // all LDS reads of a product are issued before its first step, those of v before the exponentials where registers allow
+    constexpr bool EARLY = D <= 64;
+    f32x16 s[NB];
+    {
+        typename M::F kf[NB][NF];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = threadIdx.x + i * kThreads, j = j0 + c / PPR;
-        r[i] = make_uint4(0, 0, 0, 0);
-        if (j <= hi && (j >= lo || j < sinks)) r[i] = *(const uint4 *)(base + (int64_t)j * stride_n + (c % PPR) * Mat<T>::VEC);
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int f = 0; f < NF; ++f) kf[b][f] = M::row(kt + (b * 32 + col) * LD, f, half);
+        if (EARLY) __builtin_amdgcn_sched_barrier(0);
+        for (int b = 0; b < NB; ++b) s[b] = zeros16();
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s[b] = M::mma(kf[b][f], q[f], s[b]);
     }
-}
-
-template <typename T, int D, int KT, int N>
-__device__ inline void store_tile(const uint4 (&r)[N], T *lds)
-{
-    constexpr int PPR = D / Mat<T>::VEC, LD = D + Mat<T>::PAD;
+    typename M::F vf[NB][M::GROUPS][DB];
+    const auto read_v = [&](int b) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int c = threadIdx.x + i * kThreads;
-        *(uint4 *)(lds + (c / PPR) * LD + (c % PPR) * Mat<T>::VEC) = r[i];
+        for (int g = 0; g < M::GROUPS; ++g)
+#pragma unroll
+            for (int d = 0; d < DB; ++d) vf[b][g][d] = M::column(vt + b * 32 * LD, LD, d * 32, g, lane);
+    };
+    if (EARLY) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) read_v(b);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    const int j1 = j0 + 32 * NB - 1;
+    const bool top_edge = j1 > p0 || j1 >= keys, bottom_edge = p0 + 31 - j0 >= a.window;
+    if (top_edge || bottom_edge) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) hide(s[b], edge, j0 + 32 * b, half, top_edge, bottom_edge, -INFINITY);
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    top = both_halves_max(top);
+    // m need not be the maximum, only near it: it is raised (and what was summed up rescaled) where a score passes it by 2^8,
+    // which some query of 32 does in every tile when every new maximum counts, and hardly ever so
+    top *= scale2;
+    if (__any(top > m + kSlack)) {
+        const float m1 = top > m + kSlack ? top : m;
+        const float fade = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
+        m = m1;
+        l *= fade;
+#pragma unroll
+        for (int d = 0; d < DB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= fade;
+    }
+    const float use = m == -INFINITY ? 0.f : m;          // (nothing seen yet: every term is 2^-inf)
+    float sum = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale2, -use));
+            sum += s[b][i];
+        }
+    l += sum;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        if (!EARLY) read_v(b);
+#pragma unroll
+        for (int g = 0; g < M::GROUPS; ++g) {
+            const typename M::F pf = M::pack(s[b], g);
+#pragma unroll
+            for (int d = 0; d < DB; ++d) acc[d] = M::mma(vf[b][g][d], pf, acc[d]);
+        }
     }
 }
 
 template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, D <= 64 ? 3 : 2)
 window_forward_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
     typedef typename M::F F;
     constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, KB = KT / 32, DB = D / 32, NF = D / M::KF;
-    constexpr int N = KT * D / M::VEC / kThreads;        // a thread's pieces of a tile
+    constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = KT / RPP;
     static_assert(N >= 1, "a tile has at least one piece for every thread");
     __shared__ __align__(16) T tile[2][2][KT * LD];
-    __shared__ int infinite[2];                          // number of the last tile in this half whose values are not all finite
+    __shared__ int infinite;                             // whether a value that was taken out of a tile was not finite
 
     const int qt = (a.n + kQueries - 1) / kQueries;
     const int64_t id = xcd_run(blockIdx.x, (int64_t)qt * a.B * a.Hq);
@@ -65,6 +124,58 @@ window_forward_kernel(WindowArgs a)
     const T *kp = (const T *)a.k + (int64_t)b * a.lk.stride_b + (int64_t)hk * a.lk.stride_h;
     const T *vp = (const T *)a.v + (int64_t)b * a.lv.stride_b + (int64_t)hk * a.lv.stride_h;
 
+    const float scale2 = a.scale * kLog2e;
+    const Edge edge = query_edge(a, keys, p);
+
+    // key tiles: those of the sinks before the window's, then the window's
+    const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
+    const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
+    uint4 kr[N], vr[N];
+    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
+    // a thread's 16-byte pieces of a tile: PPR to a row, rows RPP apart.  Rows behind the last one that is seen are loaded from
+    // there; what no query of the workgroup may see is 0 in LDS (what lies there cannot reach a sum as 0 * NaN).
+    const int row0 = threadIdx.x / PPR, col0 = (threadIdx.x % PPR) * M::VEC;
+    const int64_t koff = row0 * a.lk.stride_n + col0, voff = row0 * a.lv.stride_n + col0;
+    const auto load = [&](int t) {
+        const int j0 = at(t);
+        const T *k0 = kp + j0 * a.lk.stride_n, *v0 = vp + j0 * a.lv.stride_n;
+        int64_t ko[N], vo[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) { ko[i] = koff + i * RPP * a.lk.stride_n; vo[i] = voff + i * RPP * a.lv.stride_n; }
+        if (j0 + KT - 1 > hi) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int64_t row = min(row0 + i * RPP, hi - j0);
+                ko[i] = row * a.lk.stride_n + col0;
+                vo[i] = row * a.lv.stride_n + col0;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            kr[i] = *(const uint4 *)(k0 + ko[i]);
+            vr[i] = *(const uint4 *)(v0 + vo[i]);
+        }
+    };
+    const auto store = [&](int t) {
+        const int j0 = at(t);
+        if (!sees_all(a, keys, a.start_pos + i0, a.start_pos + last, j0, j0 + KT - 1)) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int j = j0 + row0 + i * RPP;
+                if (j > hi || (j < lo && j >= a.sinks)) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
+                bad |= make_finite<T>(vr[i]);
+            }
+            if (bad) infinite = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            *(uint4 *)(tile[t & 1][0] + (row0 + i * RPP) * LD + col0) = kr[i];
+            *(uint4 *)(tile[t & 1][1] + (row0 + i * RPP) * LD + col0) = vr[i];
+        }
+    };
+    if (threadIdx.x == 0) infinite = 0;
+    if (tiles > 0) load(0);
     F q[NF];
     {
         const T *qp = (const T *)a.q + (int64_t)b * a.lq.stride_b + (int64_t)iq * a.lq.stride_n + (int64_t)h * a.lq.stride_h;
@@ -75,100 +186,44 @@ window_forward_kernel(WindowArgs a)
 #pragma unroll
     for (int d = 0; d < DB; ++d) acc[d] = zeros16();
     float m = -INFINITY, l = 0.f;
-    const float scale2 = a.scale * kLog2e;
-
-    // key tiles: those of the sinks before the window's, then the window's
-    const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
-    const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
-    uint4 kr[N], vr[N];
-    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
-    const auto load = [&](int t) {
-        load_tile<T, D, KT>(kr, kp, a.lk.stride_n, at(t), lo, hi, a.sinks);
-        load_tile<T, D, KT>(vr, vp, a.lv.stride_n, at(t), lo, hi, a.sinks);
-    };
-    const auto store = [&](int t) {
-        if (!sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1)) {
-            bool bad = false;
-#pragma unroll
-            for (int i = 0; i < N; ++i) bad |= make_finite<T>(vr[i]);
-            if (bad) infinite[t & 1] = t;
-        }
-        store_tile<T, D, KT>(kr, tile[t & 1][0]);
-        store_tile<T, D, KT>(vr, tile[t & 1][1]);
-    };
-    if (threadIdx.x < 2) infinite[threadIdx.x] = -1;
-    if (tiles > 0) load(0);
+    // (the loop would wait for everything in flight if it might have to wait for the queries)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
     if (tiles > 0) store(0);
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
         const int j0 = at(t);
         const T *kt = tile[t & 1][0], *vt = tile[t & 1][1];
-        if (t + 1 < tiles) load(t + 1);
-        if (!sees_none(a, keys, p0, p1, j0, j0 + KT - 1)) {
-            f32x16 s[KB];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                s[kb] = zeros16();
-#pragma unroll
-                for (int f = 0; f < NF; ++f) s[kb] = M::mma(M::row(kt + (kb * 32 + col) * LD, f, half), q[f], s[kb]);
-            }
-            if (!sees_all(a, keys, p0, p1, j0, j0 + KT - 1)) {
-#pragma unroll
-                for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[kb][i] = sees(a, keys, p, j0 + kb * 32 + block_row(i, half)) ? s[kb][i] : -INFINITY;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-            top = fmaxf(top, __shfl_xor(top, 32));
-            const float m1 = fmaxf(m, top * scale2);
-            const float use = m1 == -INFINITY ? 0.f : m1;            // (nothing seen yet: every term is 2^-inf)
-            const float fade = __builtin_amdgcn_exp2f(m - use);
-            m = m1;
-            float sum = 0.f;
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], scale2, -use));
-                    sum += s[kb][i];
-                }
-            l = fmaf(l, fade, sum);
-            if (__any(fade != 1.f)) {
-#pragma unroll
-                for (int d = 0; d < DB; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[d][i] *= fade;
-            }
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int g = 0; g < M::GROUPS; ++g) {
-                    const F pf = M::pack(s[kb], g);
-#pragma unroll
-                    for (int d = 0; d < DB; ++d) acc[d] = M::mma(M::column(vt + kb * 32 * LD, LD, d * 32, g, lane), pf, acc[d]);
-                }
-            if (infinite[t & 1] == t) {
-                for (int j = j0; j < min(j0 + KT, keys); ++j) add_infinite<T, DB>(vp + (int64_t)j * a.lv.stride_n, sees(a, keys, p, j), half, acc);
-            }
-        }
+        load(min(t + 1, tiles - 1));                     // (the last tile once more rather than a branch around loads in flight)
+        const auto none = [&](int b) { return sees_none(a, keys, p0, p1, j0 + 32 * b, j0 + 32 * b + 31); };
+        const int from = KB == 1 || !none(0) ? 0 : 1, to = KB == 2 && !none(1) ? 2 : 1;
+        if (KB == 2 && to - from == 2)
+            forward_blocks<T, D, KB>(a, q, kt, vt, j0, keys, p0, edge, scale2, lane, m, l, acc);
+        else if (to > from && !none(from))
+            forward_blocks<T, D, 1>(a, q, kt + from * 32 * LD, vt + from * 32 * LD, j0 + 32 * from, keys, p0, edge, scale2, lane, m, l, acc);
         if (t + 1 < tiles) store(t + 1);
         __syncthreads();
     }
-    l += __shfl_xor(l, 32);                              // (each half of the wavefront added up its own rows)
+    l = both_halves_sum(l);                              // (each half of the wavefront added up its own rows)
     if (iq >= a.n) return;
     const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= inv;
+    if (infinite) {
+        for (int t = 0; t < tiles; ++t)
+            for (int j = at(t); j < min(at(t) + KT, keys); ++j) {
+                if (sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1)) break;     // (as it was)
+                add_infinite<T, DB>(vp + (int64_t)j * a.lv.stride_n, sees(a, keys, p, j), half, acc);
+            }
+    }
     O *op = (O *)a.o + (int64_t)b * a.lo.stride_b + (int64_t)iq * a.lo.stride_n + (int64_t)h * a.lo.stride_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
         for (int g = 0; g < 4; ++g)
-            store4(op + d * 32 + 8 * g + 4 * half, acc[d][4 * g] * inv, acc[d][4 * g + 1] * inv, acc[d][4 * g + 2] * inv, acc[d][4 * g + 3] * inv);
+            store4(op + d * 32 + 8 * g + 4 * half, acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]);
     if (a.lse && half == 0) a.lse[(int64_t)bh * a.n + iq] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 

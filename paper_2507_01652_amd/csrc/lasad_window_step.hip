@@ -222,36 +222,50 @@ window_step_kernel(WindowStepArgs a)
     }
 }
 
-// The splits of a query head joined; workgroup: one wavefront a head.
+// The splits (at most 64) of a query head joined: a wavefront takes every fourth of them, a lane one channel (two of 128).
 template <int OBF16, int D>
-__global__ void __launch_bounds__(64)
+__global__ void __launch_bounds__(kThreads)
 window_join_kernel(WindowStepArgs a)
 {
+    constexpr int C = D < 64 ? 1 : D / 64, UNROLL = 4;
+    __shared__ float factor[64], part[kWaves][D];
     const int64_t row = blockIdx.x;
-    const int b = (int)(row / a.Hq), lane = threadIdx.x;
+    const int b = (int)(row / a.Hq), wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     Seen s;
     if (!seen_rows(a, a.pos_rows ? a.pos_rows[b] : a.pos, s)) return;
     const float *p = a.parts + row * a.splits * (D + 2);
-    float top = -INFINITY;
-    for (int i = lane; i < a.splits; i += 64) top = fmaxf(top, p[i * (D + 2) + D]);
+    const int ch = lane % (D < 64 ? D : 64);
+    // (every wavefront forms the splits' factors for itself: no wait before the sums' loads)
+    const float m = lane < a.splits ? p[lane * (D + 2) + D] : -INFINITY, l = lane < a.splits ? p[lane * (D + 2) + D + 1] : 0.f;
+    float top = m;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
-    const float use = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, o[(D + 63) / 64] = {};
-    for (int i = 0; i < a.splits; ++i) {
-        const float f = __builtin_amdgcn_exp2f(p[i * (D + 2) + D] - use);
-        sum = fmaf(p[i * (D + 2) + D + 1], f, sum);
+    const float f = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+    float sum = l * f;
 #pragma unroll
-        for (int c = 0; c < (D + 63) / 64; ++c)
-            if (c * 64 + lane < D) o[c] = fmaf(p[i * (D + 2) + c * 64 + lane], f, o[c]);
+    for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
+    if (wave == 0) factor[lane] = f;
+    float o[C] = {};
+    __syncthreads();
+    for (int i = wave; i < a.splits; i += kWaves * UNROLL) {
+        float x[UNROLL][C];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[u][c] = p[min(i + u * kWaves, a.splits - 1) * (D + 2) + c * 64 + ch];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] = i + u * kWaves < a.splits ? fmaf(x[u][c], factor[i + u * kWaves], o[c]) : o[c];
     }
 #pragma unroll
-    for (int c = 0; c < (D + 63) / 64; ++c) {
-        const int e = c * 64 + lane;
-        if (e >= D) continue;
-        if (OBF16) ((uint16_t *)a.o)[row * D + e] = float_to_bf16_bits(o[c] / sum);
-        else ((float *)a.o)[row * D + e] = o[c] / sum;
-    }
+    for (int c = 0; c < C; ++c) part[wave][c * 64 + ch] = o[c];
+    __syncthreads();
+    if (threadIdx.x >= D) return;
+    const int e = threadIdx.x;
+    const float r = ((part[0][e] + part[1][e]) + (part[2][e] + part[3][e])) / sum;
+    if (OBF16) ((uint16_t *)a.o)[row * D + e] = float_to_bf16_bits(r);
+    else ((float *)a.o)[row * D + e] = r;
 }
 
 template <int BF16, int OBF16, int D>
@@ -267,7 +281,7 @@ hipError_t launch(const WindowStepArgs &a, hipStream_t s)
 #undef LASAD_WS
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
-        window_join_kernel<OBF16, D><<<dim3((unsigned)(a.B * a.Hq)), dim3(64), 0, s>>>(a);
+        window_join_kernel<OBF16, D><<<dim3((unsigned)(a.B * a.Hq)), dim3(kThreads), 0, s>>>(a);
         e = hipGetLastError();
     }
     return e;
