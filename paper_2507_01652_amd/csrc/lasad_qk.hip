@@ -330,29 +330,35 @@ qk_backward_kernel(QkArgs a, int tile)
     }
 }
 
-// Weight gradients: column c of `rows` partial sums [rows, columns] added up in a fixed order, 16 columns to a workgroup.
-// Columns are queries' heads, then keys' heads (shared: one of each).
-__global__ void __launch_bounds__(256)
+// Weight gradients: the columns of `rows` partial sums [rows, columns] added up in a fixed order.  A workgroup has 32 columns, a
+// thread four of them and every 32nd row, eight rows in flight.  Columns are queries' heads, then keys' (shared: one of each).
+__global__ void __launch_bounds__(kThreads)
 qk_weight_kernel(const float *partial, int64_t rows, int columns, int q_columns, float *dwq, float *dwk)
 {
-    __shared__ float red[16][17];
-    const int c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
-    const int col = blockIdx.x * 16 + c;
-    float s0 = 0.f, s1 = 0.f;
-    int64_t r = r0;
-    for (; r + 16 < rows; r += 32) {
-        s0 += partial[r * columns + col];
-        s1 += partial[(r + 16) * columns + col];
-    }
-    if (r < rows) s0 += partial[r * columns + col];
-    red[r0][c] = s0 + s1;
-    __syncthreads();
-    if (r0 == 0) {
-        float s = 0.f;
+    __shared__ __align__(16) float red[32][36];
+    const int c = (threadIdx.x & 7) * 4, r0 = threadIdx.x >> 3;
+    const float *p = partial + blockIdx.x * 32 + c;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int64_t r = r0; r < rows; r += 32 * 8) {
+        float4 x[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s += red[i][c];
+        for (int u = 0; u < 8; ++u) {
+            const int64_t row = r + 32 * u;
+            x[u] = *(const float4 *)(p + (row < rows ? row : r0) * columns);
+            if (row >= rows) x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) { s.x += x[u].x; s.y += x[u].y; s.z += x[u].z; s.w += x[u].w; }
+    }
+    *(float4 *)&red[r0][c] = s;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum += red[i][threadIdx.x];
+        const int col = blockIdx.x * 32 + threadIdx.x;
         float *dw = col < q_columns ? dwq : dwk;
-        if (dw) dw[col < q_columns ? col : col - q_columns] = s;
+        if (dw) dw[col < q_columns ? col : col - q_columns] = sum;
     }
 }
 
@@ -384,7 +390,7 @@ hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s)
     }
     if (want) {
         const int columns = (a.shared ? 2 : a.heads[0] + a.heads[1]) * a.d;
-        qk_weight_kernel<<<dim3(columns / 16), dim3(256), 0, s>>>(a.partial, groups, columns, (a.shared ? 1 : a.heads[0]) * a.d,
+        qk_weight_kernel<<<dim3(columns / 32), dim3(kThreads), 0, s>>>(a.partial, groups, columns, (a.shared ? 1 : a.heads[0]) * a.d,
                                                                  a.dw[0], a.dw[1]);
         return hipGetLastError();
     }
