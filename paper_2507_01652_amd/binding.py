@@ -894,6 +894,10 @@ def lasad_forward_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: int,
     """RMS norm of every query and key head, weight, rotation by raster position (see include/lasad.h).  q: [B, n, Hq, d],
     k: [B, n, Hk, d] views; weights fp32 [heads, d] or [d]; norm_eps < 0 switches the norm off.  Returns the two tensors;
     `out` may give them, (q, k) for in place."""
+    if out is None and out_dtype is None and stream is None:
+        done = _fast("forward_qk", q, k, grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base, start_pos)
+        if done is not None:
+            return done
     _qk_pair(q, k, "q and k")
     lq, lk = _rows(q, "q"), _rows(k, "k")
     B, n, Hq, d = q.shape
@@ -921,6 +925,11 @@ def lasad_backward_qk(q: torch.Tensor, k: torch.Tensor, d_q: torch.Tensor, d_k: 
     """Gradients of lasad_forward_qk; d_q, d_k: those of its outputs.  Returns (dq, dk, dq_weight, dk_weight); the weight
     gradients are fp32 like the weights (without a weight: [heads, d], at ones), None without a norm or with
     want_dweight=False."""
+    if grads is None and grad_dtype is None and workspace is None and stream is None:
+        done = _fast("backward_qk", q, k, grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base, start_pos, d_q, d_k,
+                     want_dweight)
+        if done is not None:
+            return done
     _qk_pair(q, k, "q and k")
     if d_q.shape != q.shape or d_k.shape != k.shape or d_q.dtype != q.dtype or d_k.dtype != q.dtype:
         raise ValueError("d_q and d_k must have the shapes and the dtype of q and k")
@@ -961,6 +970,10 @@ def lasad_decode_step_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: 
                          out: tuple | None = None, out_dtype: torch.dtype | None = None, stream=None):
     """lasad_forward_qk for one token: q [B, Hq, d], k [B, Hk, d] contiguous; pos: an integer, or an int32 tensor [B] on the
     device with a position for every row (off the grid: inactive, nothing written)."""
+    if out is None and out_dtype is None and stream is None:
+        done = _fast("decode_step_qk", q, k, grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base, pos)
+        if done is not None:
+            return done
     _qk_pair(q, k, "q and k")
     if q.dim() != 3 or not q.is_contiguous() or not k.is_contiguous():
         raise ValueError("q and k must be contiguous [B, heads, d]")
@@ -980,6 +993,10 @@ def lasad_decode_step_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: 
 
 # ---- attention with a window and sinks ----
 
+def _scale(scale, q: torch.Tensor) -> float:
+    return (q.shape[-1] or 1) ** -0.5 if scale is None else scale
+
+
 def _window_inputs(q, k, v, kv_lens):
     """Checks the tensors of a forward or backward; their layouts."""
     lq, lk, lv = _rows(q, "q"), _rows(k, "k"), _rows(v, "v")
@@ -996,6 +1013,10 @@ def lasad_forward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, wind
     """Softmax attention in which position p sees the positions p - window + 1 .. p and the first `sinks` (see include/lasad.h).
     q: [B, n, Hq, d], the tokens from start_pos on; k, v: [B, m, Hk, d], those from 0 on; kv_lens: valid keys of each batch row
     (int32 [B] on the device); scale: d ** -0.5 unless given.  Returns o, with want_lse (o, lse [B, Hq, n])."""
+    if out is None and out_dtype is None and stream is None:
+        done = _fast("forward_window", q, k, v, window, sinks, start_pos, kv_lens, _scale(scale, q), want_lse)
+        if done is not None:
+            return done if want_lse else done[0]
     lq, lk, lv = _window_inputs(q, k, v, kv_lens)
     B, n, Hq, d = q.shape
     if out is None:
@@ -1008,7 +1029,7 @@ def lasad_forward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, wind
     _check(load().lasad_forward_window(
         _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), ctypes.byref(lq), ctypes.byref(lk), ctypes.byref(lv), ctypes.byref(lo),
         _dtype_code(q), _dtype_code(out), B, Hq, k.shape[2], d, start_pos, n, k.shape[1], window, sinks, _ptr(kv_lens),
-        d ** -0.5 if scale is None else scale, _stream(stream)))
+        _scale(scale, q), _stream(stream)))
     return (out, lse) if want_lse else out
 
 
@@ -1023,6 +1044,11 @@ def lasad_backward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: 
                           workspace: torch.Tensor | None = None, stream=None):
     """Gradients of lasad_forward_window from what it returned (o in q's dtype, lse) and d_o.  Returns (dq, dk, dv); those of
     shared key heads are summed over their query heads."""
+    if grads is None and grad_dtype is None and workspace is None and stream is None:
+        done = _fast("backward_window", q, k, v, o, lse, d_o, window, sinks, start_pos, kv_lens,
+                     _scale(scale, q))
+        if done is not None:
+            return done
     lq, lk, lv = _window_inputs(q, k, v, kv_lens)
     B, n, Hq, d = q.shape
     m, Hk = k.shape[1:3]
@@ -1046,7 +1072,7 @@ def lasad_backward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: 
     _check(load().lasad_backward_window(
         _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(dq), _ptr(dk), _ptr(dv), *(ctypes.byref(x) for x in layouts),
         _dtype_code(q), _dtype_code(dq), B, Hq, Hk, d, start_pos, n, m, window, sinks, _ptr(kv_lens),
-        d ** -0.5 if scale is None else scale,
+        _scale(scale, q),
         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
     return dq, dk, dv
 
@@ -1063,6 +1089,10 @@ def lasad_decode_step_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     """lasad_forward_window for one token: q [B, Hq, d], k, v [B, Hk, d]; caches [B, Hk, rows, d], in which this call writes
     k and v to the token's row (key j: row j < sinks ? j : sinks + (j - sinks) % (rows - sinks)); pos: an integer, or an int32
     tensor [B] on the device (a row whose position does not fit the cache is inactive)."""
+    if out is None and out_dtype is None and workspace is None and use_workspace and stream is None:
+        done = _fast("decode_step_window", q, k, v, k_cache, v_cache, pos, window, sinks, _scale(scale, q))
+        if done is not None:
+            return done[0]
     B, Hq, d = q.shape
     _same(k, (v,), "k and v must be contiguous [B, Hk, d] of one shape and dtype")
     if not q.is_contiguous() or k.dim() != 3 or k.shape[0] != B or k.shape[2] != d or k.dtype != q.dtype:
@@ -1084,7 +1114,7 @@ def lasad_decode_step_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     _reachable(q, k, v, k_cache, v_cache, out, pos_rows, workspace)
     _check(load().lasad_decode_step_window(
         _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(k_cache), _ptr(v_cache), rows, _dtype_code(q), _dtype_code(out), B, Hq, Hk, d,
-        pos, _ptr(pos_rows), window, sinks, d ** -0.5 if scale is None else scale,
+        pos, _ptr(pos_rows), window, sinks, _scale(scale, q),
         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
     return out
 

@@ -409,6 +409,234 @@ PyObject *backward_layer(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- the operators of a softmax layer ----
+
+// A [B, n, heads, d] view with unit stride along d; strides of dimensions of size one are not looked at.
+lasad_layout_t rows(const at::Tensor &t)
+{
+    if (t.dim() != 4 || (t.size(3) > 1 && t.stride(3) != 1)) throw NotHandled();
+    lasad_layout_t l;
+    l.stride_b = t.size(0) > 1 ? t.stride(0) : 0;
+    l.stride_n = t.size(1) > 1 ? t.stride(1) : 0;
+    l.stride_h = t.size(2) > 1 ? t.stride(2) : 0;
+    return l;
+}
+
+int narrow(int64_t x)
+{
+    if (x != (int)x) throw NotHandled();
+    return (int)x;
+}
+
+// Norm weights [heads, d] or [d] of query and key heads.
+const float *head_weight(PyObject *o, int heads, int d, int &shared)     // shared: -1 not known yet
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    const bool one = t.dim() == 1;
+    if (t.scalar_type() != at::kFloat || (one ? t.size(0) != d : t.dim() != 2 || t.size(0) != heads || t.size(1) != d)) throw NotHandled();
+    if (shared >= 0 && shared != (int)one) throw NotHandled();
+    shared = one;
+    return (const float *)t.data_ptr();
+}
+
+struct Pair {                                      // q and k: everything alike but the heads
+    const at::Tensor &q, &k;
+    int B, n, Hq, Hk, d, io;
+    Pair(PyObject *oq, PyObject *ok, int dims) : q(any_strides(oq)), k(any_strides(ok))
+    {
+        if (q.dim() != dims || k.dim() != dims || q.scalar_type() != k.scalar_type()) throw NotHandled();
+        for (int i = 0; i < dims; ++i)
+            if (i != dims - 2 && q.size(i) != k.size(i)) throw NotHandled();
+        B = narrow(q.size(0)); n = dims == 4 ? narrow(q.size(1)) : 1;
+        Hq = narrow(q.size(dims - 2)); Hk = narrow(k.size(dims - 2)); d = narrow(q.size(dims - 1));
+        io = code(q);
+    }
+};
+
+struct QkOptions {                                 // grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base
+    int gh, gw, shared = -1, rope, pairing;
+    const float *wq, *wk;
+    float eps, base;
+    QkOptions(const Pair &p, PyObject *const *a)
+    {
+        gh = integer(a[0]); gw = integer(a[1]);
+        wq = head_weight(a[2], p.Hq, p.d, shared); wk = head_weight(a[3], p.Hk, p.d, shared);
+        if (shared < 0) shared = 0;
+        eps = real(a[4]); rope = integer(a[5]); pairing = integer(a[6]); base = real(a[7]);
+    }
+};
+
+at::Tensor dense(const at::Tensor &like) { return at::empty(like.sizes(), like.options()); }
+
+// q, k, [8 options], start_pos
+PyObject *forward_qk(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 11, [&](at::Tensor (&g)[4], int &count) {
+        const Pair p(a[0], a[1], 4);
+        const lasad_layout_t lq = rows(p.q), lk = rows(p.k);
+        const QkOptions o(p, a + 2);
+        const int start = integer(a[10]);
+        count = 2;
+        g[0] = dense(p.q); g[1] = dense(p.k);
+        const lasad_layout_t oq = rows(g[0]), ok = rows(g[1]);
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_forward_qk(p.q.data_ptr(), p.k.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), &lq, &lk, &oq, &ok, p.io, p.io, p.B, p.Hq,
+                                            p.Hk, p.d, o.gh, o.gw, start, p.n, o.wq, o.wk, o.shared, o.eps, o.rope, o.pairing, o.base, st));
+    });
+}
+
+// q, k, [8 options], start_pos, d_q, d_k, want_dweight
+PyObject *backward_qk(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 14, [&](at::Tensor (&g)[4], int &count) {
+        const Pair p(a[0], a[1], 4), dy(a[11], a[12], 4);
+        if (dy.q.sizes() != p.q.sizes() || dy.k.sizes() != p.k.sizes() || dy.io != p.io) throw NotHandled();
+        const lasad_layout_t lq = rows(p.q), lk = rows(p.k), dlq = rows(dy.q), dlk = rows(dy.k);
+        const QkOptions o(p, a + 2);
+        const int start = integer(a[10]);
+        if (a[13] != Py_True && a[13] != Py_False) throw NotHandled();
+        count = 4;
+        g[0] = dense(p.q); g[1] = dense(p.k);
+        const lasad_layout_t oq = rows(g[0]), ok = rows(g[1]);
+        at::Tensor ws;
+        size_t need = 0;
+        if (a[13] == Py_True && o.eps >= 0.f) {
+            const auto f = p.q.options().dtype(at::kFloat);
+            g[2] = o.shared ? at::empty({p.d}, f) : at::empty({p.Hq, p.d}, f);
+            g[3] = o.shared ? at::empty({p.d}, f) : at::empty({p.Hk, p.d}, f);
+            need = lasad_backward_qk_workspace_bytes(p.B, p.Hq, p.Hk, p.n, p.d, o.shared);
+            ws = at::empty({(int64_t)need}, p.q.options().dtype(at::kByte));
+        }
+        float *wq = g[2].defined() ? (float *)g[2].data_ptr() : nullptr, *wk = g[3].defined() ? (float *)g[3].data_ptr() : nullptr;
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_backward_qk(p.q.data_ptr(), p.k.data_ptr(), dy.q.data_ptr(), dy.k.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), wq, wk,
+                                             &lq, &lk, &dlq, &dlk, &oq, &ok, p.io, p.io, p.B, p.Hq, p.Hk, p.d, o.gh, o.gw, start, p.n, o.wq, o.wk,
+                                             o.shared, o.eps, o.rope, o.pairing, o.base, need ? ws.data_ptr() : nullptr, need, st));
+    });
+}
+
+// A step's position: an integer, or an int32 tensor with one for each batch row.
+const int32_t *row_positions(PyObject *o, int B, int &pos)
+{
+    pos = 0;
+    if (PyLong_CheckExact(o)) {
+        pos = integer(o);
+        return nullptr;
+    }
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != at::kInt || t.numel() != B) throw NotHandled();
+    return (const int32_t *)t.data_ptr();
+}
+
+// q, k, [8 options], pos
+PyObject *decode_step_qk(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 11, [&](at::Tensor (&g)[4], int &count) {
+        const Pair p(a[0], a[1], 3);
+        if (!p.q.is_contiguous() || !p.k.is_contiguous()) throw NotHandled();
+        const QkOptions o(p, a + 2);
+        int pos;
+        const int32_t *pos_rows = row_positions(a[10], p.B, pos);
+        count = 2;
+        g[0] = dense(p.q); g[1] = dense(p.k);
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_decode_step_qk(p.q.data_ptr(), p.k.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), p.io, p.io, p.B, p.Hq, p.Hk, p.d, o.gh,
+                                                o.gw, pos, pos_rows, o.wq, o.wk, o.shared, o.eps, o.rope, o.pairing, o.base, st));
+    });
+}
+
+struct Attention {                                 // q [B, n, Hq, d]; k, v [B, m, Hk, d]; kv_lens [B] or None
+    const at::Tensor &q, &k, &v;
+    int B, n, m, Hq, Hk, d, io;
+    lasad_layout_t lq, lk, lv;
+    const int32_t *lens = nullptr;
+    Attention(PyObject *oq, PyObject *ok, PyObject *ov, PyObject *ol) : q(any_strides(oq)), k(any_strides(ok)), v(any_strides(ov))
+    {
+        lq = rows(q); lk = rows(k); lv = rows(v);
+        if (k.sizes() != v.sizes() || k.size(0) != q.size(0) || k.size(3) != q.size(3) || k.scalar_type() != q.scalar_type() ||
+            v.scalar_type() != q.scalar_type()) throw NotHandled();
+        B = narrow(q.size(0)); n = narrow(q.size(1)); m = narrow(k.size(1));
+        Hq = narrow(q.size(2)); Hk = narrow(k.size(2)); d = narrow(q.size(3));
+        io = code(q);
+        if (ol != Py_None) {
+            const at::Tensor &t = tensor(ol);
+            if (t.scalar_type() != at::kInt || t.numel() != B) throw NotHandled();
+            lens = (const int32_t *)t.data_ptr();
+        }
+    }
+};
+
+// q, k, v, window, sinks, start_pos, kv_lens, scale, want_lse
+PyObject *forward_window(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 9, [&](at::Tensor (&g)[4], int &count) {
+        const Attention s(a[0], a[1], a[2], a[6]);
+        const int window = integer(a[3]), sinks = integer(a[4]), start = integer(a[5]);
+        const float scale = real(a[7]);
+        if (a[8] != Py_True && a[8] != Py_False) throw NotHandled();
+        count = a[8] == Py_True ? 2 : 1;
+        g[0] = dense(s.q);
+        if (count == 2) g[1] = at::empty({s.B, s.Hq, s.n}, s.q.options().dtype(at::kFloat));
+        const lasad_layout_t lo = rows(g[0]);
+        float *lse = count == 2 ? (float *)g[1].data_ptr() : nullptr;
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_forward_window(s.q.data_ptr(), s.k.data_ptr(), s.v.data_ptr(), g[0].data_ptr(), lse, &s.lq, &s.lk, &s.lv, &lo, s.io,
+                                                s.io, s.B, s.Hq, s.Hk, s.d, start, s.n, s.m, window, sinks, s.lens, scale, st));
+    });
+}
+
+// q, k, v, o, lse, d_o, window, sinks, start_pos, kv_lens, scale
+PyObject *backward_window(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 11, [&](at::Tensor (&g)[4], int &count) {
+        const Attention s(a[0], a[1], a[2], a[9]);
+        const at::Tensor &o = any_strides(a[3]), &lse = tensor(a[4]), &d_o = any_strides(a[5]);
+        if (o.sizes() != s.q.sizes() || d_o.sizes() != s.q.sizes() || o.scalar_type() != s.q.scalar_type() ||
+            d_o.scalar_type() != s.q.scalar_type()) throw NotHandled();
+        if (lse.scalar_type() != at::kFloat || lse.dim() != 3 || lse.size(0) != s.B || lse.size(1) != s.Hq || lse.size(2) != s.n) throw NotHandled();
+        const lasad_layout_t lo = rows(o), ldo = rows(d_o);
+        const int window = integer(a[6]), sinks = integer(a[7]), start = integer(a[8]);
+        const float scale = real(a[10]);
+        count = 3;
+        g[0] = dense(s.q); g[1] = dense(s.k); g[2] = dense(s.v);
+        const lasad_layout_t ldq = rows(g[0]), ldk = rows(g[1]), ldv = rows(g[2]);
+        const size_t need = lasad_backward_window_workspace_bytes(s.B, s.Hq, s.Hk, s.d, s.n, s.m, window, sinks);
+        at::Tensor ws = at::empty({(int64_t)need}, s.q.options().dtype(at::kByte));
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_backward_window(s.q.data_ptr(), s.k.data_ptr(), s.v.data_ptr(), o.data_ptr(), (const float *)lse.data_ptr(),
+                                                 d_o.data_ptr(), g[0].data_ptr(), g[1].data_ptr(), g[2].data_ptr(), &s.lq, &s.lk, &s.lv, &lo, &ldo, &ldq,
+                                                 &ldk, &ldv, s.io, s.io, s.B, s.Hq, s.Hk, s.d, start, s.n, s.m, window, sinks, s.lens, scale,
+                                                 need ? ws.data_ptr() : nullptr, need, st));
+    });
+}
+
+// q, k, v, k_cache, v_cache, pos, window, sinks, scale
+PyObject *decode_step_window(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 9, [&](at::Tensor (&g)[4], int &count) {
+        const Pair p(a[0], a[1], 3);
+        const at::Tensor &v = tensor(a[2]), &kc = tensor(a[3]), &vc = tensor(a[4]);
+        if (!p.q.is_contiguous() || !p.k.is_contiguous() || v.sizes() != p.k.sizes() || kc.sizes() != vc.sizes() || kc.dim() != 4 || kc.size(0) != p.B ||
+            kc.size(1) != p.Hk || kc.size(3) != p.d) throw NotHandled();
+        for (const at::Tensor *t : {&v, &kc, &vc})
+            if (t->scalar_type() != p.q.scalar_type()) throw NotHandled();
+        const int cap = narrow(kc.size(2)), window = integer(a[6]), sinks = integer(a[7]);
+        int pos;
+        const int32_t *pos_rows = row_positions(a[5], p.B, pos);
+        const float scale = real(a[8]);
+        count = 1;
+        g[0] = dense(p.q);
+        const size_t need = lasad_decode_step_window_workspace_bytes(p.B, p.Hq, p.Hk, p.d, cap, window, sinks);
+        at::Tensor ws;
+        if (need) ws = at::empty({(int64_t)need}, p.q.options().dtype(at::kByte));
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_decode_step_window(p.q.data_ptr(), p.k.data_ptr(), v.data_ptr(), g[0].data_ptr(), kc.data_ptr(), vc.data_ptr(), cap, p.io,
+                                                    p.io, p.B, p.Hq, p.Hk, p.d, pos, pos_rows, window, sinks, scale, need ? ws.data_ptr() : nullptr, need,
+                                                    st));
+    });
+}
+
 PyMethodDef methods[] = {
     {"decode_step", (PyCFunction)(void (*)(void))decode_step, METH_FASTCALL, nullptr},
     {"decode_step_gated", (PyCFunction)(void (*)(void))decode_step_gated, METH_FASTCALL, nullptr},
@@ -420,6 +648,12 @@ PyMethodDef methods[] = {
     {"backward_chunked", (PyCFunction)(void (*)(void))backward_chunked, METH_FASTCALL, nullptr},
     {"backward_gated", (PyCFunction)(void (*)(void))backward_gated, METH_FASTCALL, nullptr},
     {"backward_layer", (PyCFunction)(void (*)(void))backward_layer, METH_FASTCALL, nullptr},
+    {"forward_qk", (PyCFunction)(void (*)(void))forward_qk, METH_FASTCALL, nullptr},
+    {"backward_qk", (PyCFunction)(void (*)(void))backward_qk, METH_FASTCALL, nullptr},
+    {"decode_step_qk", (PyCFunction)(void (*)(void))decode_step_qk, METH_FASTCALL, nullptr},
+    {"forward_window", (PyCFunction)(void (*)(void))forward_window, METH_FASTCALL, nullptr},
+    {"backward_window", (PyCFunction)(void (*)(void))backward_window, METH_FASTCALL, nullptr},
+    {"decode_step_window", (PyCFunction)(void (*)(void))decode_step_window, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_steps", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
