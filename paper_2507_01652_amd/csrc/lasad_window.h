@@ -209,13 +209,20 @@ __device__ inline bool row_infinite(const T *row, int lane)
     return __any(bad);
 }
 
-// Workgroups follow one another over the 8 L2s: give each an unbroken run of the work, so that what shares keys meets there.
-__device__ inline int64_t xcd_run(int64_t index, int64_t total)
+// The launch order of `units` pieces of work of each of `heads` heads.  Workgroups follow one another over the 8 L2s: with 8 heads
+// and more each L2 gets heads of its own, so that what shares keys meets there, and its workgroups take piece after piece of all its
+// heads, so that pieces that take long, which come first, do not start last.  Fewer heads are dealt out over all L2s.
+struct Place {
+    int head, unit;                    // (head -1: nothing to do)
+};
+__device__ inline Place launch_place(unsigned index, int heads, int units)
 {
-    const int64_t run = (total + 7) / 8;
-    return (index & 7) * run + (index >> 3);
+    if (heads < 8) return {(int)(index % (unsigned)heads), (int)(index / (unsigned)heads)};
+    const unsigned each = ((unsigned)heads + 7) / 8, slot = index >> 3;
+    const int head = (int)((index & 7) * each + slot % each);
+    return {head < heads ? head : -1, (int)(slot / each)};
 }
-inline unsigned xcd_grid(int64_t total) { return (unsigned)((total + 7) / 8 * 8); }
+inline unsigned launch_grid(int64_t heads, int64_t units) { return (unsigned)(heads < 8 ? heads * units : (heads + 7) / 8 * 8 * units); }
 
 // Four consecutive results of a lane, as they leave the registers.
 template <typename O>

@@ -9,6 +9,8 @@
 // Key pass: 32 keys to a wavefront, 128 of one head to a workgroup, which walks the tiles of the queries that see any of them,
 // head after head of the group.  Ordinary keys are seen from `window` positions on, the sinks from all later ones: their
 // tiles are cut into parts of about an ordinary tile's work, whose sums a small kernel adds up in their order.
+// In the key pass -lse / scale and -delta are what the sums of the first two products start from, so that an entry costs a product and
+// an exponential for P and one more product for dS.
 // P and dS are rounded to the storage type as operands (bf16: half a step of 2^-8); all sums are fp32.
 #include "lasad_window.h"
 
@@ -29,7 +31,7 @@ __device__ inline void dq_blocks(const WindowArgs &a, const typename Mat<T>::F (
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
     constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
     const int half = lane >> 5, col = lane & 31;
-#pragma unroll
+#pragma unroll 1
     for (int b = 0; b < NB; ++b) {
         const T *kb = kt + b * 32 * LD, *vb = vt + b * 32 * LD;
         F kf[NF], vf[NF], kc[M::GROUPS][DB];
@@ -41,13 +43,14 @@ __device__ inline void dq_blocks(const WindowArgs &a, const typename Mat<T>::F (
 #pragma unroll
                 for (int d = 0; d < DB; ++d) kc[r][d] = M::column(kb, LD, d * 32, r, lane);
         };
+        if (EARLY) __builtin_amdgcn_sched_barrier(0);
+        f32x16 s = zeros16(), dp = zeros16();
+#pragma unroll
+        for (int f = 0; f < NF; ++f) { s = M::mma(kf[f], q[f], s); dp = M::mma(vf[f], g[f], dp); }
         if (EARLY) {
             columns();
             __builtin_amdgcn_sched_barrier(0);
         }
-        f32x16 s = zeros16(), dp = zeros16();
-#pragma unroll
-        for (int f = 0; f < NF; ++f) { s = M::mma(kf[f], q[f], s); dp = M::mma(vf[f], g[f], dp); }
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)) * (dp[i] - delta);
         const int jb = j0 + 32 * b;
@@ -64,7 +67,7 @@ __device__ inline void dq_blocks(const WindowArgs &a, const typename Mat<T>::F (
 }
 
 template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads, D <= 32 ? 3 : D <= 64 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, D > 64 ? 1 : sizeof(T) == 2 || D == 32 ? 3 : 2)
 window_dq_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
@@ -75,11 +78,11 @@ window_dq_kernel(WindowArgs a)
     __shared__ int infinite;                             // whether a key that was taken out of a tile was not finite
 
     const int qt = (a.n + kTile - 1) / kTile;
-    const int64_t id = xcd_run(blockIdx.x, (int64_t)qt * a.B * a.Hq);
-    if (id >= (int64_t)qt * a.B * a.Hq) return;
-    const int i0 = (int)(id % qt) * kTile;
-    const int bh = (int)(id / qt), b = bh / a.Hq, h = bh % a.Hq, hk = h / (a.Hq / a.Hk);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const Place place = launch_place(blockIdx.x, a.B * a.Hq, qt);
+    if (place.head < 0) return;
+    const int i0 = (qt - 1 - place.unit) * kTile;        // (the first queries see the fewest keys: last)
+    const int bh = place.head, b = bh / a.Hq, h = bh % a.Hq, hk = h / (a.Hq / a.Hk);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int iq = i0 + 32 * wave + col, p = a.start_pos + iq;
     const int p0 = a.start_pos + i0 + 32 * wave, p1 = p0 + 31;
     const int last = min(i0 + kTile, a.n) - 1;
@@ -201,11 +204,11 @@ window_dq_kernel(WindowArgs a)
                    acc[d][4 * r + 3] * a.scale);
 }
 
-// One block of 32 queries (positions from pb on, rows of qt and gt, their lse and delta) for a wavefront's keys: P and dS, and
+// One block of 32 queries (positions from pb on, rows of qt and gt, their -lse / scale and -delta) for a wavefront's keys: P and dS, and
 // their products with d_o and q.
 template <typename T, int D>
 __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (&k)[D / Mat<T>::KF], const typename Mat<T>::F (&v)[D / Mat<T>::KF],
-                                 const T *qt, const T *gt, const float *lse2, const float *delta, int pb, int keys, int w0, const Edge &edge,
+                                 const T *qt, const T *gt, const float *shift, const float *delta, int pb, int keys, int w0, const Edge &edge,
                                  float scale2, int lane, f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32])
 {
     typedef Mat<T> M;
@@ -216,12 +219,12 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
     F qf[NF], gf[NF], qc[M::GROUPS][DB], gc[M::GROUPS][DB];
 #pragma unroll
     for (int f = 0; f < NF; ++f) { qf[f] = M::row(qt + col * LD, f, half); gf[f] = M::row(gt + col * LD, f, half); }
-    float ls[16], de[16];
+    f32x16 s, dp;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const float4 x = *(const float4 *)(lse2 + 8 * r + 4 * half), y = *(const float4 *)(delta + 8 * r + 4 * half);
-        ls[4 * r] = x.x; ls[4 * r + 1] = x.y; ls[4 * r + 2] = x.z; ls[4 * r + 3] = x.w;
-        de[4 * r] = y.x; de[4 * r + 1] = y.y; de[4 * r + 2] = y.z; de[4 * r + 3] = y.w;
+        const float4 x = *(const float4 *)(shift + 8 * r + 4 * half), y = *(const float4 *)(delta + 8 * r + 4 * half);
+        s[4 * r] = x.x; s[4 * r + 1] = x.y; s[4 * r + 2] = x.z; s[4 * r + 3] = x.w;
+        dp[4 * r] = y.x; dp[4 * r + 1] = y.y; dp[4 * r + 2] = y.z; dp[4 * r + 3] = y.w;
     }
     const auto columns = [&]() {
 #pragma unroll
@@ -232,10 +235,7 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
                 qc[r][d] = M::column(qt, LD, d * 32, r, lane);
             }
     };
-    if (EARLY) {
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    f32x16 s = zeros16(), dp = zeros16();
+    if (EARLY) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int f = 0; f < NF; ++f) { s = M::mma(qf[f], k[f], s); dp = M::mma(gf[f], v[f], dp); }
     if (EARLY) {
@@ -244,8 +244,8 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -ls[i]));
-        dp[i] = s[i] * (dp[i] - de[i]);
+        s[i] = __builtin_amdgcn_exp2f(s[i] * scale2);
+        dp[i] *= s[i];
     }
     const bool first_edge = pb < w0 + 31 || w0 + 31 >= keys, last_edge = pb + 31 - w0 >= a.window;
     if (first_edge || last_edge) {
@@ -274,19 +274,19 @@ window_dkv_kernel(WindowArgs a)
     constexpr int QT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, QB = QT / 32, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = QT / RPP;
     __shared__ __align__(16) T tile[2][2][QT * LD];
-    __shared__ __align__(16) float stat[2][2][QT];       // lse (in powers of two) and delta of a tile's queries
+    __shared__ __align__(16) float stat[2][2][QT];       // -lse / scale and -delta of a tile's queries
     __shared__ int infinite;                             // whether a row that was taken out of a tile was not finite
 
     const int kt = (a.m + kTile - 1) / kTile;
     const int units = a.sink_tiles * a.sink_parts + kt - a.sink_tiles;      // workgroups of a key head
-    const int64_t id = xcd_run(blockIdx.x, (int64_t)units * a.B * a.Hk);
-    if (id >= (int64_t)units * a.B * a.Hk) return;
-    const int unit = (int)(id % units), bh = (int)(id / units), b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
+    const Place place = launch_place(blockIdx.x, a.B * a.Hk, units);
+    if (place.head < 0) return;
+    const int unit = place.unit, bh = place.head, b = bh / a.Hk, hk = bh % a.Hk, G = a.Hq / a.Hk;
     const bool sink = unit < a.sink_tiles * a.sink_parts;
     const int kti = sink ? unit / a.sink_parts : unit - a.sink_tiles * a.sink_parts + a.sink_tiles;
     const int part = sink ? unit % a.sink_parts : 0, parts = sink ? a.sink_parts : 1;
     const int j0 = kti * kTile;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int jk = j0 + 32 * wave + col;                             // this lane's key
     const int w0 = j0 + 32 * wave, w1 = w0 + 31;                     // the wavefront's
     // (keys behind the last query are nobody's; a tile's rows behind it have lse = inf, so that P is 0 for every finite key)
@@ -305,7 +305,7 @@ window_dkv_kernel(WindowArgs a)
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zeros16();
-    const float scale2 = a.scale * kLog2e;
+    const float scale2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
     const Edge edge = key_edge(a, keys, jk);
 
     // queries that see any key of the tile, in tiles of QT counted from the first query; this part's share of them
@@ -368,7 +368,7 @@ window_dkv_kernel(WindowArgs a)
             *(uint4 *)(tile[buf][0] + (row0 + i * RPP) * LD + col0) = qr[i];
             *(uint4 *)(tile[buf][1] + (row0 + i * RPP) * LD + col0) = gr[i];
         }
-        if (threadIdx.x < 2 * QT) stat[buf][threadIdx.x / QT][threadIdx.x % QT] = threadIdx.x < QT ? sr * kLog2e : sr;
+        if (threadIdx.x < 2 * QT) stat[buf][threadIdx.x / QT][threadIdx.x % QT] = threadIdx.x < QT ? -sr * inv_scale : -sr;
     };
     if (threadIdx.x == 0) infinite = 0;
     if (steps > 0) load(0, 0);
@@ -379,8 +379,8 @@ window_dkv_kernel(WindowArgs a)
     int ti = 0, hi = 0;                                  // tile and head of the present step
     for (int t = 0; t < steps; ++t) {
         const int p0 = a.start_pos + (t_first + ti) * QT;
-        if (++ti == t_count) { ti = 0; ++hi; }
-        if (t + 1 < steps) load(ti, hi);
+        if (t + 1 < steps && ++ti == t_count) { ti = 0; ++hi; }
+        load(ti, hi);                                    // (the last tile once more rather than a branch around loads in flight)
         const T *qt = tile[t & 1][0], *gt = tile[t & 1][1];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
@@ -489,26 +489,26 @@ hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
     a.delta = (float *)workspace;
     a.parts = (float *)((char *)workspace + delta_bytes(a.B, a.Hq, a.n));
     plan((int64_t)a.B * a.Hk, a.n, a.m, a.window, a.sinks, a.sink_tiles, a.sink_parts);
-    const int64_t q_total = (int64_t)((a.n + kTile - 1) / kTile) * a.B * a.Hq;
-    if (q_total > 0) {
-#define LASAD_WQ(T, O, D) window_dq_kernel<T, O, D><<<dim3(xcd_grid(q_total)), dim3(kThreads), 0, s>>>(a)
+    if (a.n > 0) {
+        const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kTile - 1) / kTile));
+#define LASAD_WQ(T, O, D) window_dq_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
         LASAD_WINDOW_DISPATCH(LASAD_WQ);
 #undef LASAD_WQ
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     const int units = a.sink_tiles * a.sink_parts + (a.m + kTile - 1) / kTile - a.sink_tiles;
-    const int64_t k_total = (int64_t)units * a.B * a.Hk;
-    if (k_total == 0) return hipSuccess;
-#define LASAD_WK(T, O, D) window_dkv_kernel<T, O, D><<<dim3(xcd_grid(k_total)), dim3(kThreads), 0, s>>>(a)
+    if (units == 0) return hipSuccess;
+    const dim3 grid(launch_grid((int64_t)a.B * a.Hk, units));
+#define LASAD_WK(T, O, D) window_dkv_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
     LASAD_WINDOW_DISPATCH(LASAD_WK);
 #undef LASAD_WK
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.sink_tiles > 0 && a.sink_parts > 1) {
         const int64_t total = (int64_t)a.B * a.Hk * a.sink_tiles * 2 * kTile * (a.d / 4);
-        const dim3 grid((unsigned)((total + kThreads - 1) / kThreads));
-        if (a.out_dtype == LASAD_BF16) window_sink_sum_kernel<uint16_t><<<grid, dim3(kThreads), 0, s>>>(a);
-        else window_sink_sum_kernel<float><<<grid, dim3(kThreads), 0, s>>>(a);
+        const dim3 sums((unsigned)((total + kThreads - 1) / kThreads));
+        if (a.out_dtype == LASAD_BF16) window_sink_sum_kernel<uint16_t><<<sums, dim3(kThreads), 0, s>>>(a);
+        else window_sink_sum_kernel<float><<<sums, dim3(kThreads), 0, s>>>(a);
         e = hipGetLastError();
     }
     return e;

@@ -111,11 +111,11 @@ window_forward_kernel(WindowArgs a)
     __shared__ int infinite;                             // whether a value that was taken out of a tile was not finite
 
     const int qt = (a.n + kQueries - 1) / kQueries;
-    const int64_t id = xcd_run(blockIdx.x, (int64_t)qt * a.B * a.Hq);
-    if (id >= (int64_t)qt * a.B * a.Hq) return;
-    const int i0 = (int)(id % qt) * kQueries;
-    const int bh = (int)(id / qt), b = bh / a.Hq, h = bh % a.Hq, hk = h / (a.Hq / a.Hk);
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const Place place = launch_place(blockIdx.x, a.B * a.Hq, qt);
+    if (place.head < 0) return;
+    const int i0 = (qt - 1 - place.unit) * kQueries;     // (the first queries see the fewest keys: last)
+    const int bh = place.head, b = bh / a.Hq, h = bh % a.Hq, hk = h / (a.Hq / a.Hk);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int iq = i0 + 32 * wave + col, p = a.start_pos + iq;       // this lane's query
     const int p0 = a.start_pos + i0 + 32 * wave, p1 = p0 + 31;       // the wavefront's
     const int last = min(i0 + kQueries, a.n) - 1;                    // the workgroup's last query
@@ -231,9 +231,9 @@ window_forward_kernel(WindowArgs a)
 
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s)
 {
-    const int64_t total = (int64_t)((a.n + kQueries - 1) / kQueries) * a.B * a.Hq;
-    if (total == 0) return hipSuccess;
-#define LASAD_WF(T, O, D) window_forward_kernel<T, O, D><<<dim3(xcd_grid(total)), dim3(kThreads), 0, s>>>(a)
+    if (a.n == 0) return hipSuccess;
+    const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kQueries - 1) / kQueries));
+#define LASAD_WF(T, O, D) window_forward_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
     LASAD_WINDOW_DISPATCH(LASAD_WF);
 #undef LASAD_WF
     return hipGetLastError();
