@@ -118,6 +118,17 @@ __device__ inline bool sees_all(const WindowArgs &a, int keys, int p0, int p1, i
     return j1 <= p0 && j1 < keys && (p1 - j0 < a.window || j1 < a.sinks);
 }
 
+// The same for a range of positions, as comparisons with four numbers that a walk over keys keeps.
+struct Range {
+    int last, before, top, bottom, sinks;
+    __device__ inline Range(const WindowArgs &a, int keys, int p0, int p1)
+        : last(min(p1, keys - 1)), before(p0 - a.window), top(min(p0, keys - 1)), bottom(p1 - a.window), sinks(a.sinks) {}
+    __device__ inline bool some(int j0, int j1) const { return j0 <= last && (j1 > before || j0 < sinks); }
+    __device__ inline bool top_edge(int j1) const { return j1 > top; }
+    __device__ inline bool bottom_edge(int j0) const { return j0 <= bottom; }                 // (sinks or not)
+    __device__ inline bool all(int j0, int j1) const { return j1 <= top && (j0 > bottom || j1 < sinks); }
+};
+
 // What a column's query sees of the rows of a block of keys (or a column's key of the rows of a block of queries): rows
 // lo .. hi, and those before `first`.  Two comparisons with a constant an entry, and which of them a block needs is the same for
 // the whole wavefront, so that a block inside the window pays none.

@@ -15,57 +15,28 @@ namespace {
 constexpr int kThreads = 256, kQueries = 128;
 constexpr float kSlack = 8.f;
 
-// NB blocks of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: scores, their exponentials, products with v.
-template <typename T, int D, int NB>
-__device__ inline void forward_blocks(const WindowArgs &a, const typename Mat<T>::F (&q)[D / Mat<T>::KF], const T *kt, const T *vt, int j0,
-                                      int keys, int p0, const Edge &edge, float scale2, int lane, float &m, float &l, f32x16 (&acc)[D / 32])
+// One block of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: scores, their exponentials, products with v.
+// Blocks are taken one after the other, not two at a time: with 16 scores a lane (and not 32) four wavefronts fit a SIMD, which hide
+// each other's waits better than a longer run of independent operations does (4 x 4096 tokens of 24 heads: 156 us with two blocks and
+// three wavefronts, 148 so; two tiles in a wavefront's registers, products beside exponentials: 245).
+template <typename T, int D>
+__device__ inline void forward_block(const typename Mat<T>::F (&q)[D / Mat<T>::KF], const T *kt, const T *vt, int j0,
+                                     const Range &range, const Edge &edge, float scale2, int lane, float &m, float &l, f32x16 (&acc)[D / 32])
 {
     typedef Mat<T> M;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
     const int half = lane >> 5, col = lane & 31;
-    // all LDS reads of a product are issued before its first step, those of v before the exponentials where registers allow
-    constexpr bool EARLY = D <= 64;
-    f32x16 s[NB];
-    {
-        typename M::F kf[NB][NF];
+    f32x16 s = zeros16();
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+    for (int f = 0; f < NF; ++f) s = M::mma(M::row(kt + col * LD, f, half), q[f], s);
+    const bool top_edge = range.top_edge(j0 + 31), bottom_edge = range.bottom_edge(j0);
+    if (top_edge || bottom_edge) hide(s, edge, j0, half, top_edge, bottom_edge, -INFINITY);
+    float top = s[0];
 #pragma unroll
-            for (int f = 0; f < NF; ++f) kf[b][f] = M::row(kt + (b * 32 + col) * LD, f, half);
-        if (EARLY) __builtin_amdgcn_sched_barrier(0);
-        for (int b = 0; b < NB; ++b) s[b] = zeros16();
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] = M::mma(kf[b][f], q[f], s[b]);
-    }
-    typename M::F vf[NB][M::GROUPS][DB];
-    const auto read_v = [&](int b) {
-#pragma unroll
-        for (int g = 0; g < M::GROUPS; ++g)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) vf[b][g][d] = M::column(vt + b * 32 * LD, LD, d * 32, g, lane);
-    };
-    if (EARLY) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) read_v(b);
-        __builtin_amdgcn_sched_barrier(0);
-    }
-    const int j1 = j0 + 32 * NB - 1;
-    const bool top_edge = j1 > p0 || j1 >= keys, bottom_edge = p0 + 31 - j0 >= a.window;
-    if (top_edge || bottom_edge) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) hide(s[b], edge, j0 + 32 * b, half, top_edge, bottom_edge, -INFINITY);
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-    top = both_halves_max(top);
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     // m need not be the maximum, only near it: it is raised (and what was summed up rescaled) where a score passes it by 2^8,
     // which some query of 32 does in every tile when every new maximum counts, and hardly ever so
-    top *= scale2;
+    top = both_halves_max(top) * scale2;
     if (__any(top > m + kSlack)) {
         const float m1 = top > m + kSlack ? top : m;
         const float fade = m == m1 ? 1.f : __builtin_amdgcn_exp2f(m - m1);
@@ -79,32 +50,26 @@ __device__ inline void forward_blocks(const WindowArgs &a, const typename Mat<T>
     const float use = m == -INFINITY ? 0.f : m;          // (nothing seen yet: every term is 2^-inf)
     float sum = 0.f;
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], scale2, -use));
-            sum += s[b][i];
-        }
+    for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -use));
+        sum += s[i];
+    }
     l += sum;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        if (!EARLY) read_v(b);
+    for (int g = 0; g < M::GROUPS; ++g) {
+        const typename M::F pf = M::pack(s, g);
 #pragma unroll
-        for (int g = 0; g < M::GROUPS; ++g) {
-            const typename M::F pf = M::pack(s[b], g);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] = M::mma(vf[b][g][d], pf, acc[d]);
-        }
+        for (int d = 0; d < DB; ++d) acc[d] = M::mma(M::column(vt, LD, d * 32, g, lane), pf, acc[d]);
     }
 }
 
 template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads, D <= 64 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, D > 64 ? 2 : sizeof(T) == 2 ? 4 : 3)
 window_forward_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
     typedef typename M::F F;
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, KB = KT / 32, DB = D / 32, NF = D / M::KF;
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = KT / RPP;
     static_assert(N >= 1, "a tile has at least one piece for every thread");
     __shared__ __align__(16) T tile[2][2][KT * LD];
@@ -128,37 +93,36 @@ window_forward_kernel(WindowArgs a)
     const Edge edge = query_edge(a, keys, p);
 
     // key tiles: those of the sinks before the window's, then the window's
+    const Range mine(a, keys, p0, p1), all(a, keys, a.start_pos + i0, a.start_pos + last);       // the wavefront's, the workgroup's
     const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
     const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
-    uint4 kr[N], vr[N];
-    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
+    const int jump_from = sink_tiles * KT, jump_to = first * KT;
+    const auto next = [&](int j0) { return j0 + KT == jump_from ? jump_to : j0 + KT; };
+    const int begin = sink_tiles > 0 ? 0 : jump_to;
     // a thread's 16-byte pieces of a tile: PPR to a row, rows RPP apart.  Rows behind the last one that is seen are loaded from
     // there; what no query of the workgroup may see is 0 in LDS (what lies there cannot reach a sum as 0 * NaN).
+    uint4 kr[N], vr[N];
     const int row0 = threadIdx.x / PPR, col0 = (threadIdx.x % PPR) * M::VEC;
     const int64_t koff = row0 * a.lk.stride_n + col0, voff = row0 * a.lv.stride_n + col0;
-    const auto load = [&](int t) {
-        const int j0 = at(t);
+    const auto load = [&](int j0) {
         const T *k0 = kp + j0 * a.lk.stride_n, *v0 = vp + j0 * a.lv.stride_n;
-        int64_t ko[N], vo[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) { ko[i] = koff + i * RPP * a.lk.stride_n; vo[i] = voff + i * RPP * a.lv.stride_n; }
         if (j0 + KT - 1 > hi) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int64_t row = min(row0 + i * RPP, hi - j0);
-                ko[i] = row * a.lk.stride_n + col0;
-                vo[i] = row * a.lv.stride_n + col0;
+                kr[i] = *(const uint4 *)(k0 + (row * a.lk.stride_n + col0));
+                vr[i] = *(const uint4 *)(v0 + (row * a.lv.stride_n + col0));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                kr[i] = *(const uint4 *)(k0 + i * RPP * a.lk.stride_n + koff);
+                vr[i] = *(const uint4 *)(v0 + i * RPP * a.lv.stride_n + voff);
             }
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            kr[i] = *(const uint4 *)(k0 + ko[i]);
-            vr[i] = *(const uint4 *)(v0 + vo[i]);
-        }
     };
-    const auto store = [&](int t) {
-        const int j0 = at(t);
-        if (!sees_all(a, keys, a.start_pos + i0, a.start_pos + last, j0, j0 + KT - 1)) {
+    const auto store = [&](int j0, int half) {
+        if (!all.all(j0, j0 + KT - 1)) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -168,14 +132,15 @@ window_forward_kernel(WindowArgs a)
             }
             if (bad) infinite = 1;
         }
+        T *at = tile[half][0] + row0 * LD + col0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            *(uint4 *)(tile[t & 1][0] + (row0 + i * RPP) * LD + col0) = kr[i];
-            *(uint4 *)(tile[t & 1][1] + (row0 + i * RPP) * LD + col0) = vr[i];
+            *(uint4 *)(at + i * RPP * LD) = kr[i];
+            *(uint4 *)(at + KT * LD + i * RPP * LD) = vr[i];
         }
     };
     if (threadIdx.x == 0) infinite = 0;
-    if (tiles > 0) load(0);
+    if (tiles > 0) load(begin);
     F q[NF];
     {
         const T *qp = (const T *)a.q + (int64_t)b * a.lq.stride_b + (int64_t)iq * a.lq.stride_n + (int64_t)h * a.lq.stride_h;
@@ -189,20 +154,20 @@ window_forward_kernel(WindowArgs a)
     // (the loop would wait for everything in flight if it might have to wait for the queries)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
-    if (tiles > 0) store(0);
+    if (tiles > 0) store(begin, 0);
     __syncthreads();
+    int j0 = begin;
     for (int t = 0; t < tiles; ++t) {
-        const int j0 = at(t);
         const T *kt = tile[t & 1][0], *vt = tile[t & 1][1];
-        load(min(t + 1, tiles - 1));                     // (the last tile once more rather than a branch around loads in flight)
-        const auto none = [&](int b) { return sees_none(a, keys, p0, p1, j0 + 32 * b, j0 + 32 * b + 31); };
-        const int from = KB == 1 || !none(0) ? 0 : 1, to = KB == 2 && !none(1) ? 2 : 1;
-        if (KB == 2 && to - from == 2)
-            forward_blocks<T, D, KB>(a, q, kt, vt, j0, keys, p0, edge, scale2, lane, m, l, acc);
-        else if (to > from && !none(from))
-            forward_blocks<T, D, 1>(a, q, kt + from * 32 * LD, vt + from * 32 * LD, j0 + 32 * from, keys, p0, edge, scale2, lane, m, l, acc);
-        if (t + 1 < tiles) store(t + 1);
+        const int j1 = t + 1 < tiles ? next(j0) : j0;    // (the last tile once more rather than a branch around loads in flight)
+        load(j1);
+#pragma unroll 1
+        for (int b = 0; b < KT; b += 32)
+            if (mine.some(j0 + b, j0 + b + 31))
+                forward_block<T, D>(q, kt + b * LD, vt + b * LD, j0 + b, mine, edge, scale2, lane, m, l, acc);
+        if (t + 1 < tiles) store(j1, (t + 1) & 1);
         __syncthreads();
+        j0 = j1;
     }
     l = both_halves_sum(l);                              // (each half of the wavefront added up its own rows)
     if (iq >= a.n) return;
@@ -212,11 +177,11 @@ window_forward_kernel(WindowArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] *= inv;
     if (infinite) {
-        for (int t = 0; t < tiles; ++t)
-            for (int j = at(t); j < min(at(t) + KT, keys); ++j) {
-                if (sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1)) break;     // (as it was)
-                add_infinite<T, DB>(vp + (int64_t)j * a.lv.stride_n, sees(a, keys, p, j), half, acc);
-            }
+        int j0 = begin;
+        for (int t = 0; t < tiles; ++t, j0 = next(j0)) {
+            if (all.all(j0, j0 + KT - 1)) continue;      // (as it was)
+            for (int j = j0; j < min(j0 + KT, keys); ++j) add_infinite<T, DB>(vp + (int64_t)j * a.lv.stride_n, sees(a, keys, p, j), half, acc);
+        }
     }
     O *op = (O *)a.o + (int64_t)b * a.lo.stride_b + (int64_t)iq * a.lo.stride_n + (int64_t)h * a.lo.stride_h;
 #pragma unroll
