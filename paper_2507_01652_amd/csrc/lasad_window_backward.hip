@@ -20,49 +20,30 @@ namespace {
 
 constexpr int kThreads = 256, kTile = 128;               // queries (keys) of a workgroup
 
-// NB blocks of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: dS, and its product with k.
-template <typename T, int D, int NB>
-__device__ inline void dq_blocks(const WindowArgs &a, const typename Mat<T>::F (&q)[D / Mat<T>::KF], const typename Mat<T>::F (&g)[D / Mat<T>::KF],
-                                 const T *kt, const T *vt, int j0, int keys, int p0, const Edge &edge, float scale2, float lse2, float delta,
-                                 int lane, f32x16 (&acc)[D / 32])
+// One block of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: dS, and its product with k.
+template <typename T, int D>
+__device__ inline void dq_block(const typename Mat<T>::F (&q)[D / Mat<T>::KF], const typename Mat<T>::F (&g)[D / Mat<T>::KF],
+                                const T *kt, const T *vt, int j0, const Range &range, const Edge &edge, float scale2, float lse2, float delta,
+                                int lane, f32x16 (&acc)[D / 32])
 {
     typedef Mat<T> M;
-    typedef typename M::F F;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
-    constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
     const int half = lane >> 5, col = lane & 31;
-#pragma unroll 1
-    for (int b = 0; b < NB; ++b) {
-        const T *kb = kt + b * 32 * LD, *vb = vt + b * 32 * LD;
-        F kf[NF], vf[NF], kc[M::GROUPS][DB];
+    f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-        for (int f = 0; f < NF; ++f) { kf[f] = M::row(kb + col * LD, f, half); vf[f] = M::row(vb + col * LD, f, half); }
-        const auto columns = [&]() {
+    for (int f = 0; f < NF; ++f) {
+        s = M::mma(M::row(kt + col * LD, f, half), q[f], s);
+        dp = M::mma(M::row(vt + col * LD, f, half), g[f], dp);
+    }
 #pragma unroll
-            for (int r = 0; r < M::GROUPS; ++r)
+    for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)) * (dp[i] - delta);
+    const bool top_edge = range.top_edge(j0 + 31), bottom_edge = range.bottom_edge(j0);
+    if (top_edge || bottom_edge) hide(s, edge, j0, half, top_edge, bottom_edge, 0.f);
 #pragma unroll
-                for (int d = 0; d < DB; ++d) kc[r][d] = M::column(kb, LD, d * 32, r, lane);
-        };
-        if (EARLY) __builtin_amdgcn_sched_barrier(0);
-        f32x16 s = zeros16(), dp = zeros16();
+    for (int r = 0; r < M::GROUPS; ++r) {
+        const typename M::F ds = M::pack(s, r);
 #pragma unroll
-        for (int f = 0; f < NF; ++f) { s = M::mma(kf[f], q[f], s); dp = M::mma(vf[f], g[f], dp); }
-        if (EARLY) {
-            columns();
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale2, -lse2)) * (dp[i] - delta);
-        const int jb = j0 + 32 * b;
-        const bool top_edge = jb + 31 > p0 || jb + 31 >= keys, bottom_edge = p0 + 31 - jb >= a.window;
-        if (top_edge || bottom_edge) hide(s, edge, jb, half, top_edge, bottom_edge, 0.f);
-        if (!EARLY) columns();
-#pragma unroll
-        for (int r = 0; r < M::GROUPS; ++r) {
-            const F ds = M::pack(s, r);
-#pragma unroll
-            for (int d = 0; d < DB; ++d) acc[d] = M::mma(kc[r][d], ds, acc[d]);
-        }
+        for (int d = 0; d < DB; ++d) acc[d] = M::mma(M::column(kt, LD, d * 32, r, lane), ds, acc[d]);
     }
 }
 
@@ -72,7 +53,7 @@ window_dq_kernel(WindowArgs a)
 {
     typedef Mat<T> M;
     typedef typename M::F F;
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, KB = KT / 32, DB = D / 32, NF = D / M::KF;
+    constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = KT / RPP;
     __shared__ __align__(16) T tile[2][2][KT * LD];
     __shared__ int infinite;                             // whether a key that was taken out of a tile was not finite
@@ -94,52 +75,53 @@ window_dq_kernel(WindowArgs a)
     const float scale2 = a.scale * kLog2e;
     const Edge edge = query_edge(a, keys, p);
 
+    // (the walk over the keys is the forward's)
+    const Range mine(a, keys, p0, p1), all(a, keys, a.start_pos + i0, a.start_pos + last);
     const int first = lo / KT, sink_tiles = min((min(a.sinks, hi + 1) + KT - 1) / KT, first);
     const int tiles = hi < 0 ? 0 : sink_tiles + max(0, hi / KT - first + 1);
+    const int jump_from = sink_tiles * KT, jump_to = first * KT;
+    const auto next = [&](int j0) { return j0 + KT == jump_from ? jump_to : j0 + KT; };
+    const int begin = sink_tiles > 0 ? 0 : jump_to;
     uint4 kr[N], vr[N];
-    const auto at = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
     const int row0 = threadIdx.x / PPR, col0 = (threadIdx.x % PPR) * M::VEC;
     const int64_t koff = row0 * a.lk.stride_n + col0, voff = row0 * a.lv.stride_n + col0;
-    const auto load = [&](int t) {                       // (as in the forward)
-        const int j0 = at(t);
+    const auto load = [&](int j0) {
         const T *k0 = kp + j0 * a.lk.stride_n, *v0 = vp + j0 * a.lv.stride_n;
-        int64_t ko[N], vo[N];
-#pragma unroll
-        for (int i = 0; i < N; ++i) { ko[i] = koff + i * RPP * a.lk.stride_n; vo[i] = voff + i * RPP * a.lv.stride_n; }
         if (j0 + KT - 1 > hi) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int64_t row = min(row0 + i * RPP, hi - j0);
-                ko[i] = row * a.lk.stride_n + col0;
-                vo[i] = row * a.lv.stride_n + col0;
+                kr[i] = *(const uint4 *)(k0 + (row * a.lk.stride_n + col0));
+                vr[i] = *(const uint4 *)(v0 + (row * a.lv.stride_n + col0));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                kr[i] = *(const uint4 *)(k0 + i * RPP * a.lk.stride_n + koff);
+                vr[i] = *(const uint4 *)(v0 + i * RPP * a.lv.stride_n + voff);
             }
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-            kr[i] = *(const uint4 *)(k0 + ko[i]);
-            vr[i] = *(const uint4 *)(v0 + vo[i]);
-        }
     };
-    const auto whole = [&](int t) { return sees_all(a, keys, a.start_pos + i0, a.start_pos + last, at(t), at(t) + KT - 1); };
-    const auto store = [&](int t) {
-        if (!whole(t)) {
+    const auto store = [&](int j0, int half) {
+        if (!all.all(j0, j0 + KT - 1)) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const int j = at(t) + row0 + i * RPP;
+                const int j = j0 + row0 + i * RPP;
                 if (j > hi || (j < lo && j >= a.sinks)) kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
                 bad |= make_finite<T>(kr[i]);
             }
             if (bad) infinite = 1;
         }
+        T *at = tile[half][0] + row0 * LD + col0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            *(uint4 *)(tile[t & 1][0] + (row0 + i * RPP) * LD + col0) = kr[i];
-            *(uint4 *)(tile[t & 1][1] + (row0 + i * RPP) * LD + col0) = vr[i];
+            *(uint4 *)(at + i * RPP * LD) = kr[i];
+            *(uint4 *)(at + KT * LD + i * RPP * LD) = vr[i];
         }
     };
     if (threadIdx.x == 0) infinite = 0;
-    if (tiles > 0) load(0);
+    if (tiles > 0) load(begin);
     F q[NF], g[NF];
     float delta = 0.f, lse2 = INFINITY;
     {
@@ -165,25 +147,26 @@ window_dq_kernel(WindowArgs a)
     // (the loop would wait for everything in flight if it might have to wait for the queries)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
-    if (tiles > 0) store(0);
+    if (tiles > 0) store(begin, 0);
     __syncthreads();
+    int j0 = begin;
     for (int t = 0; t < tiles; ++t) {
-        const int j0 = at(t);
         const T *kt = tile[t & 1][0], *vt = tile[t & 1][1];
-        load(min(t + 1, tiles - 1));
-        const auto none = [&](int b) { return sees_none(a, keys, p0, p1, j0 + 32 * b, j0 + 32 * b + 31); };
-        const int from = KB == 1 || !none(0) ? 0 : 1, to = KB == 2 && !none(1) ? 2 : 1;
-        if (KB == 2 && to - from == 2)
-            dq_blocks<T, D, KB>(a, q, g, kt, vt, j0, keys, p0, edge, scale2, lse2, delta, lane, acc);
-        else if (to > from && !none(from))
-            dq_blocks<T, D, 1>(a, q, g, kt + from * 32 * LD, vt + from * 32 * LD, j0 + 32 * from, keys, p0, edge, scale2, lse2, delta, lane, acc);
-        if (t + 1 < tiles) store(t + 1);
+        const int j1 = t + 1 < tiles ? next(j0) : j0;
+        load(j1);
+#pragma unroll 1
+        for (int b = 0; b < KT; b += 32)
+            if (mine.some(j0 + b, j0 + b + 31))
+                dq_block<T, D>(q, g, kt + b * LD, vt + b * LD, j0 + b, mine, edge, scale2, lse2, delta, lane, acc);
+        if (t + 1 < tiles) store(j1, (t + 1) & 1);
         __syncthreads();
+        j0 = j1;
     }
     if (infinite) {                                      // (a seen key that is not finite: so is the row's gradient)
-        for (int t = 0; t < tiles; ++t) {
-            if (whole(t)) continue;                      // (as it was)
-            for (int j = at(t); j < min(at(t) + KT, keys); ++j) {
+        int j0 = begin;
+        for (int t = 0; t < tiles; ++t, j0 = next(j0)) {
+            if (all.all(j0, j0 + KT - 1)) continue;      // (as it was)
+            for (int j = j0; j < min(j0 + KT, keys); ++j) {
                 const bool bad = row_infinite<T, D>(kp + (int64_t)j * a.lk.stride_n, lane);
                 if (bad && sees(a, keys, p, j)) {
 #pragma unroll
@@ -214,6 +197,7 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
     typedef Mat<T> M;
     typedef typename M::F F;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
+    // (bf16: all LDS reads of a product are issued before its first step)
     constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
     const int half = lane >> 5, col = lane & 31;
     F qf[NF], gf[NF], qc[M::GROUPS][DB], gc[M::GROUPS][DB];
