@@ -15,20 +15,17 @@ namespace {
 constexpr int kThreads = 256, kQueries = 128;
 constexpr float kSlack = 8.f;
 
-// One block of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: scores, their exponentials, products with v.
+// One block of 32 keys (from j0 on, scores s, values in the rows of vt) for a wavefront's queries: exponentials, products with v.
 // Blocks are taken one after the other, not two at a time: with 16 scores a lane (and not 32) four wavefronts fit a SIMD, which hide
 // each other's waits better than a longer run of independent operations does (4 x 4096 tokens of 24 heads: 156 us with two blocks and
 // three wavefronts, 148 so; two tiles in a wavefront's registers, products beside exponentials: 245).
 template <typename T, int D>
-__device__ inline void forward_block(const typename Mat<T>::F (&q)[D / Mat<T>::KF], const T *kt, const T *vt, int j0,
-                                     const Range &range, const Edge &edge, float scale2, int lane, float &m, float &l, f32x16 (&acc)[D / 32])
+__device__ inline void forward_block(f32x16 s, const T *vt, int j0, const Range &range, const Edge &edge, float scale2, int lane, float &m, float &l,
+                                     f32x16 (&acc)[D / 32])
 {
     typedef Mat<T> M;
-    constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
-    const int half = lane >> 5, col = lane & 31;
-    f32x16 s = zeros16();
-#pragma unroll
-    for (int f = 0; f < NF; ++f) s = M::mma(M::row(kt + col * LD, f, half), q[f], s);
+    constexpr int LD = D + M::PAD, DB = D / 32;
+    const int half = lane >> 5;
     const bool top_edge = range.top_edge(j0 + 31), bottom_edge = range.bottom_edge(j0);
     if (top_edge || bottom_edge) hide(s, edge, j0, half, top_edge, bottom_edge, -INFINITY);
     float top = s[0];
@@ -163,8 +160,12 @@ window_forward_kernel(WindowArgs a)
         load(j1);
 #pragma unroll 1
         for (int b = 0; b < KT; b += 32)
-            if (mine.some(j0 + b, j0 + b + 31))
-                forward_block<T, D>(q, kt + b * LD, vt + b * LD, j0 + b, mine, edge, scale2, lane, m, l, acc);
+            if (mine.some(j0 + b, j0 + b + 31)) {
+                f32x16 s = zeros16();
+#pragma unroll
+                for (int f = 0; f < NF; ++f) s = M::mma(M::row(kt + (b + col) * LD, f, half), q[f], s);
+                forward_block<T, D>(s, vt + b * LD, j0 + b, mine, edge, scale2, lane, m, l, acc);
+            }
         if (t + 1 < tiles) store(j1, (t + 1) & 1);
         __syncthreads();
         j0 = j1;
@@ -192,12 +193,157 @@ window_forward_kernel(WindowArgs a)
     if (a.lse && half == 0) a.lse[(int64_t)bh * a.n + iq] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+// For few queries: a workgroup has 32 of one head, and its four wavefronts take the blocks of keys in turn, each with its own
+// maximum, sum and output, which are joined at the end.  Nothing is shared on the way: keys go from memory to the products' operands,
+// values through the wavefront's own rows of LDS, without a barrier.
+template <typename T, typename O, int D>
+__global__ void __launch_bounds__(kThreads, D <= 64 ? 3 : 1)
+window_forward_few_kernel(WindowArgs a)
+{
+    typedef Mat<T> M;
+    typedef typename M::F F;
+    constexpr int LD = D + M::PAD, DB = D / 32, NF = D / M::KF, PPR = D / M::VEC, RPW = 64 / PPR, N = 32 / RPW, W = kThreads / 64;
+    constexpr int V_BYTES = W * 32 * LD * (int)sizeof(T), JOIN_BYTES = W * 32 * (D + 4) * 4;
+    __shared__ __align__(16) char lds[V_BYTES > JOIN_BYTES ? V_BYTES : JOIN_BYTES];
+    __shared__ float tops[W][32], sums[W][32];
+    __shared__ int infinite;
+
+    const int qt = (a.n + 31) / 32;
+    const Place place = launch_place(blockIdx.x, a.B * a.Hq, qt);
+    if (place.head < 0) return;
+    const int i0 = (qt - 1 - place.unit) * 32, bh = place.head, b = bh / a.Hq, h = bh % a.Hq, hk = h / (a.Hq / a.Hk);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int iq = i0 + col, p = a.start_pos + iq, p0 = a.start_pos + i0, p1 = a.start_pos + min(i0 + 32, a.n) - 1;
+    const int keys = valid_keys(a, b);
+    const int hi = min(p1, keys - 1), lo = max(0, p0 - a.window + 1);
+    const T *kp = (const T *)a.k + (int64_t)b * a.lk.stride_b + (int64_t)hk * a.lk.stride_h;
+    const T *vp = (const T *)a.v + (int64_t)b * a.lv.stride_b + (int64_t)hk * a.lv.stride_h;
+    const float scale2 = a.scale * kLog2e;
+    const Edge edge = query_edge(a, keys, p);
+    const Range range(a, keys, p0, p1);
+
+    // blocks of keys: those of the sinks before the window's, then the window's
+    const int first = lo / 32, sink_blocks = min((min(a.sinks, hi + 1) + 31) / 32, first);
+    const int blocks = hi < 0 ? 0 : sink_blocks + max(0, hi / 32 - first + 1);
+    const auto at = [&](int t) { return (t < sink_blocks ? t : first + t - sink_blocks) * 32; };
+    T *vt = (T *)lds + wave * 32 * LD;
+    F kr[NF];
+    uint4 vr[N];
+    const int row0 = lane / PPR, col0 = (lane % PPR) * M::VEC;
+    const auto load = [&](int t) {                       // (rows behind the last one that is seen: that one)
+        const int j0 = at(t);
+        const T *kq = kp + (int64_t)min(j0 + col, hi) * a.lk.stride_n;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) kr[f] = M::row(kq, f, half);
+#pragma unroll
+        for (int i = 0; i < N; ++i) vr[i] = *(const uint4 *)(vp + (int64_t)min(j0 + row0 + i * RPW, hi) * a.lv.stride_n + col0);
+    };
+    // (wavefronts with the same number share a SIMD: the first block, and with it an odd one, goes to another of them each time)
+    const int turn = (wave + blockIdx.x) % W;
+    if (turn < blocks) load(turn);
+    F q[NF];
+    {
+        const T *qp = (const T *)a.q + (int64_t)b * a.lq.stride_b + (int64_t)min(iq, a.n - 1) * a.lq.stride_n + (int64_t)h * a.lq.stride_h;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) q[f] = M::row(qp, f, half);
+    }
+    if (threadIdx.x == 0) infinite = 0;
+    __syncthreads();
+    f32x16 acc[DB];
+#pragma unroll
+    for (int d = 0; d < DB; ++d) acc[d] = zeros16();
+    float m = -INFINITY, l = 0.f;
+    for (int t = turn; t < blocks; t += W) {
+        const int j0 = at(t);
+        if (!range.all(j0, j0 + 31)) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int j = j0 + row0 + i * RPW;
+                if (j > hi || (j < lo && j >= a.sinks)) vr[i] = make_uint4(0, 0, 0, 0);
+                bad |= make_finite<T>(vr[i]);
+            }
+            if (bad) infinite = 1;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(uint4 *)(vt + (row0 + i * RPW) * LD + col0) = vr[i];
+        f32x16 s = zeros16();
+#pragma unroll
+        for (int f = 0; f < NF; ++f) s = M::mma(kr[f], q[f], s);
+        if (t + W < blocks) load(t + W);
+        // (the rows are this wavefront's own: its LDS operations are in order)
+        __builtin_amdgcn_wave_barrier();
+        forward_block<T, D>(s, vt, j0, range, edge, scale2, lane, m, l, acc);
+        __builtin_amdgcn_wave_barrier();
+    }
+    l = both_halves_sum(l);
+    if (half == 0) { tops[wave][col] = m; sums[wave][col] = l; }
+    __syncthreads();
+    float top = tops[0][col];
+#pragma unroll
+    for (int w = 1; w < W; ++w) top = fmaxf(top, tops[w][col]);
+    const float use = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) total = fmaf(sums[w][col], __builtin_amdgcn_exp2f(tops[w][col] - use), total);
+    const float f = total == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - use) / total;
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+    if (infinite && wave == 0) {
+        for (int t = 0; t < blocks; ++t) {
+            if (range.all(at(t), at(t) + 31)) continue;  // (as it was)
+            for (int j = at(t); j < min(at(t) + 32, keys); ++j) add_infinite<T, DB>(vp + (int64_t)j * a.lv.stride_n, sees(a, keys, p, j), half, acc);
+        }
+    }
+    float *join = (float *)lds;                          // (all values have been read: the barrier above)
+#pragma unroll
+    for (int d = 0; d < DB; ++d)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            *(float4 *)(join + (wave * 32 + col) * (D + 4) + d * 32 + 8 * g + 4 * half) =
+                make_float4(acc[d][4 * g], acc[d][4 * g + 1], acc[d][4 * g + 2], acc[d][4 * g + 3]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < 32 * D / 4; c += kThreads) {
+        const int row = c / (D / 4), ch = c % (D / 4) * 4;
+        if (i0 + row >= a.n) break;
+        float4 s = *(const float4 *)(join + row * (D + 4) + ch);
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            const float4 x = *(const float4 *)(join + (w * 32 + row) * (D + 4) + ch);
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        store4((O *)a.o + (int64_t)b * a.lo.stride_b + (int64_t)(i0 + row) * a.lo.stride_n + (int64_t)h * a.lo.stride_h + ch, s.x, s.y, s.z, s.w);
+    }
+    if (a.lse && threadIdx.x < 32 && iq < a.n)
+        a.lse[(int64_t)bh * a.n + iq] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
+}
+
+// Few: too few workgroups of 128 queries to fill the chip's 256 units.  us, few and many, window 128 of 256 tokens, 12 heads: batch 1
+// 6.8 and 10.9, 8 (192 workgroups) 9.1 and 11.4, 16 (384) 14.9 and 12.2; 16 heads of 100 tokens, batch 16 (256) 9.0 and 8.3.  d = 128,
+// whose keys do not fit the registers twice: batch 1 10.4 and 15.5, 4 (96) 16.1 and 15.9, 16 47 and 20.  fp32, bound by its
+// matrix rate: batch 4 16.7 and 27.5, 16 (384) 38.7 and 37.4.
+bool few_queries(const WindowArgs &a)
+{
+    const int64_t groups = (int64_t)a.B * a.Hq * ((a.n + kQueries - 1) / kQueries);
+    return groups < (a.io_dtype == LASAD_F32 ? 384 : a.d == 128 ? 96 : 256);
+}
+
 }  // namespace
 
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s)
 {
     if (a.n == 0) return hipSuccess;
-    const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kQueries - 1) / kQueries));
+    const int64_t heads = (int64_t)a.B * a.Hq;
+    if (few_queries(a)) {
+        const dim3 grid(launch_grid(heads, (a.n + 31) / 32));
+#define LASAD_WF(T, O, D) window_forward_few_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
+        LASAD_WINDOW_DISPATCH(LASAD_WF);
+#undef LASAD_WF
+        return hipGetLastError();
+    }
+    const dim3 grid(launch_grid(heads, (a.n + kQueries - 1) / kQueries));
 #define LASAD_WF(T, O, D) window_forward_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
     LASAD_WINDOW_DISPATCH(LASAD_WF);
 #undef LASAD_WF
