@@ -44,10 +44,12 @@ struct WindowArgs {
     float scale;
     float *delta;                      // backward workspace: [B, Hq, n] rows' sums of d_o o
     float *parts;                      // backward workspace: partial dk and dv of the sinks' key tiles
-    int sink_tiles, sink_parts;        // plan of the backward's key pass (window_plan)
+    int key_tile, sink_tiles, sink_parts;              // plan of the backward's key pass: keys of a tile, tiles with sinks, parts of each
 };
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s);
+hipError_t launch_window_dq_few(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_dkv_few(const WindowArgs &a, hipStream_t s);
 size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int window, int sinks);
 
 // One token against a cache [B, Hk, cap, d]: key j lies in row j < sinks ? j : sinks + (j - sinks) mod (cap - sinks).

@@ -100,6 +100,14 @@ __device__ inline float both_halves_sum(float x)
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Between a wavefront's writes to its own LDS and its other lanes' reads: the hardware keeps a wavefront's LDS operations in order, the
+// compiler has to as well.
+__device__ inline void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // row of a lane's register i in a 32 x 32 block
 __device__ inline int block_row(int i, int half) { return 8 * (i >> 2) + 4 * half + (i & 3); }
 

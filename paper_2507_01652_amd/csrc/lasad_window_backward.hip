@@ -421,19 +421,19 @@ __global__ void __launch_bounds__(kThreads)
 window_sink_sum_kernel(WindowArgs a)
 {
     const int q = a.d / 4;                               // pieces of a row
-    const int64_t total = (int64_t)a.B * a.Hk * a.sink_tiles * 2 * kTile * q;
+    const int64_t total = (int64_t)a.B * a.Hk * a.sink_tiles * 2 * a.key_tile * q;
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (id >= total) return;
     const int c = (int)(id % q) * 4;
-    const int row = (int)(id / q % kTile), which = (int)(id / q / kTile % 2);
-    const int64_t tile = id / q / kTile / 2;             // (b, hk, sink tile)
-    const int j = (int)(tile % a.sink_tiles) * kTile + row;
+    const int row = (int)(id / q % a.key_tile), which = (int)(id / q / a.key_tile % 2);
+    const int64_t tile = id / q / a.key_tile / 2;             // (b, hk, sink tile)
+    const int j = (int)(tile % a.sink_tiles) * a.key_tile + row;
     if (j >= a.m) return;
     const int bh = (int)(tile / a.sink_tiles), b = bh / a.Hk, hk = bh % a.Hk;
-    const float *p = a.parts + (tile * a.sink_parts * 2 + which) * kTile * a.d + (int64_t)row * a.d + c;
+    const float *p = a.parts + (tile * a.sink_parts * 2 + which) * a.key_tile * a.d + (int64_t)row * a.d + c;
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i < a.sink_parts; ++i) {
-        const float4 x = *(const float4 *)(p + (int64_t)i * 2 * kTile * a.d);
+        const float4 x = *(const float4 *)(p + (int64_t)i * 2 * a.key_tile * a.d);
         s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
     }
     const lasad_layout_t &l = which ? a.ldv : a.ldk;
@@ -442,19 +442,30 @@ window_sink_sum_kernel(WindowArgs a)
     store4(out, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
-// Key tiles with sinks and the parts they are cut into.  In steps of 64 queries: an ordinary tile takes (window + 128) / 64, one
-// with sinks n / 64.  Uncut it ends last where it takes longer than an ordinary one and than half of what the chip's 512
-// workgroup slots have to do anyway; a part takes about that long.  At most 1024 parts, which bounds the workspace.
-void plan(int64_t heads, int n, int m, int window, int sinks, int &tiles, int &parts)
+// Few keys (queries): too few workgroups of 128 to fill the chip's 256 units; a workgroup then has 32.  us, few and many, window 128
+// of 256 tokens, 12 heads: batch 2 20.0 and 27.6, 4 (96 workgroups) 22.5 and 28.1, 6 (144) 29.3 and 28.4, 8 33.8 and 28.6; 4 heads of
+// 4096, window 1024 (128) 52 and 80.  d = 128: 2 (48) 30 and 45, 4 (96) 47 and 45, 6 65 and 47.  fp32: 4 58 and 82, 8 (192) 96 and 85.
+bool few(int64_t heads, int64_t count, int d) { return heads * ((count + kTile - 1) / kTile) < (d == 128 ? 96 : 144); }
+
+// The key pass' tiles, those with sinks, and the parts they are cut into.  In steps of 64 queries: an ordinary tile takes
+// (window + tile) / 64, one with sinks n / 64.  Uncut it ends last where it takes longer than an ordinary one and than half of what
+// the chip's 512 workgroup slots have to do anyway; a part takes about that long.  At most 1024 parts, which bounds the workspace.
+struct Plan {
+    int tile, sink_tiles, parts;
+};
+Plan plan(int64_t heads, int d, int n, int m, int window, int sinks)
 {
-    tiles = (int)(((int64_t)(sinks < m ? sinks : m) + kTile - 1) / kTile);
-    const int64_t all = ((int64_t)m + kTile - 1) / kTile, sink = (n + 63) / 64, near = ((int64_t)window + kTile + 63) / 64;
+    Plan r;
+    r.tile = few(heads, m, d) ? 32 : kTile;
+    r.sink_tiles = (int)(((int64_t)(sinks < m ? sinks : m) + r.tile - 1) / r.tile);
+    const int64_t all = ((int64_t)m + r.tile - 1) / r.tile, sink = (n + 63) / 64, near = ((int64_t)window + r.tile + 63) / 64;
     const int64_t ordinary = near < sink ? near : sink;
-    const int64_t slot = heads * ((all - tiles) * ordinary + tiles * sink) / 512;
+    const int64_t slot = heads * ((all - r.sink_tiles) * ordinary + r.sink_tiles * sink) / 512;
     const int64_t long_enough = ordinary > slot / 2 ? ordinary : slot / 2;
-    const int64_t want = long_enough > 0 ? (sink + long_enough - 1) / long_enough : 1, most = tiles > 0 ? 1024 / (heads * tiles) : 1;
-    parts = (int)(want > most ? most : want);
-    parts = parts < 1 ? 1 : parts > 64 ? 64 : parts;
+    const int64_t want = long_enough > 0 ? (sink + long_enough - 1) / long_enough : 1, most = r.sink_tiles > 0 ? 1024 / (heads * r.sink_tiles) : 1;
+    const int64_t parts = want > most ? most : want;
+    r.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    return r;
 }
 
 size_t delta_bytes(int B, int Hq, int n) { return ((size_t)B * Hq * n * sizeof(float) + 255) / 256 * 256; }
@@ -463,33 +474,41 @@ size_t delta_bytes(int B, int Hq, int n) { return ((size_t)B * Hq * n * sizeof(f
 
 size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int window, int sinks)
 {
-    int tiles, parts;
-    plan((int64_t)B * Hk, n, m, window, sinks, tiles, parts);
-    return delta_bytes(B, Hq, n) + (parts > 1 ? (size_t)B * Hk * tiles * parts * 2 * kTile * d * sizeof(float) : 0);
+    const Plan r = plan((int64_t)B * Hk, d, n, m, window, sinks);
+    return delta_bytes(B, Hq, n) + (r.parts > 1 ? (size_t)B * Hk * r.sink_tiles * r.parts * 2 * r.tile * d * sizeof(float) : 0);
 }
 
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
 {
     a.delta = (float *)workspace;
     a.parts = (float *)((char *)workspace + delta_bytes(a.B, a.Hq, a.n));
-    plan((int64_t)a.B * a.Hk, a.n, a.m, a.window, a.sinks, a.sink_tiles, a.sink_parts);
+    const Plan r = plan((int64_t)a.B * a.Hk, a.d, a.n, a.m, a.window, a.sinks);
+    a.key_tile = r.tile; a.sink_tiles = r.sink_tiles; a.sink_parts = r.parts;
+    hipError_t e = hipSuccess;
     if (a.n > 0) {
-        const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kTile - 1) / kTile));
+        if (few((int64_t)a.B * a.Hq, a.n, a.d)) {
+            e = launch_window_dq_few(a, s);
+        } else {
+            const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kTile - 1) / kTile));
 #define LASAD_WQ(T, O, D) window_dq_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
-        LASAD_WINDOW_DISPATCH(LASAD_WQ);
+            LASAD_WINDOW_DISPATCH(LASAD_WQ);
 #undef LASAD_WQ
-        const hipError_t e = hipGetLastError();
+            e = hipGetLastError();
+        }
         if (e != hipSuccess) return e;
     }
-    const int units = a.sink_tiles * a.sink_parts + (a.m + kTile - 1) / kTile - a.sink_tiles;
-    if (units == 0) return hipSuccess;
-    const dim3 grid(launch_grid((int64_t)a.B * a.Hk, units));
+    if (a.m == 0) return hipSuccess;
+    if (r.tile == 32) {
+        e = launch_window_dkv_few(a, s);
+    } else {
+        const dim3 grid(launch_grid((int64_t)a.B * a.Hk, r.sink_tiles * r.parts + (a.m + kTile - 1) / kTile - r.sink_tiles));
 #define LASAD_WK(T, O, D) window_dkv_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
-    LASAD_WINDOW_DISPATCH(LASAD_WK);
+        LASAD_WINDOW_DISPATCH(LASAD_WK);
 #undef LASAD_WK
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.sink_tiles > 0 && a.sink_parts > 1) {
-        const int64_t total = (int64_t)a.B * a.Hk * a.sink_tiles * 2 * kTile * (a.d / 4);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && r.sink_tiles > 0 && r.parts > 1) {
+        const int64_t total = (int64_t)a.B * a.Hk * r.sink_tiles * 2 * r.tile * (a.d / 4);
         const dim3 sums((unsigned)((total + kThreads - 1) / kThreads));
         if (a.out_dtype == LASAD_BF16) window_sink_sum_kernel<uint16_t><<<sums, dim3(kThreads), 0, s>>>(a);
         else window_sink_sum_kernel<float><<<sums, dim3(kThreads), 0, s>>>(a);

@@ -271,10 +271,9 @@ window_forward_few_kernel(WindowArgs a)
 #pragma unroll
         for (int f = 0; f < NF; ++f) s = M::mma(kr[f], q[f], s);
         if (t + W < blocks) load(t + W);
-        // (the rows are this wavefront's own: its LDS operations are in order)
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
         forward_block<T, D>(s, vt, j0, range, edge, scale2, lane, m, l, acc);
-        __builtin_amdgcn_wave_barrier();
+        wave_lds_order();
     }
     l = both_halves_sum(l);
     if (half == 0) { tops[wave][col] = m; sums[wave][col] = l; }

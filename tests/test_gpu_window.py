@@ -40,6 +40,10 @@ CASES = [
     (BF, BF, 64, 6, 2, 1, 0, 1100, 1100, 100, 4, None),                  # the sinks' queries in parts
     (F, F, 64, 2, 1, 1, 0, 700, 700, 64, 130, None),                     # two tiles of sinks, in parts
 ]
+# The same masks with heads enough for workgroups of 128 queries and keys (the ones above have 32): (case, batch rows, heads, key heads)
+MANY = [(CASES[i], B, Hq, Hk) for i, B, Hq, Hk in ((0, 12, 16, 16), (1, 16, 12, 12), (2, 9, 32, 16), (3, 13, 16, 16), (6, 8, 32, 16), (7, 8, 32, 32),
+                                                   (8, 16, 16, 8), (9, 8, 32, 16), (10, 16, 16, 16), (11, 32, 16, 8), (12, 32, 16, 16), (13, 10, 16, 16),
+                                                   (14, 16, 32, 16), (15, 13, 16, 8), (16, 16, 32, 16), (17, 4, 12, 4), (18, 4, 24, 24))]
 IDS = [f"{str(c[0])[6:]}-{str(c[1])[6:]}-d{c[2]}-{c[3]}x{c[4]}-B{c[5]}-{c[6]}+{c[7]}of{c[8]}-w{c[9]}-s{c[10]}{'-lens' if c[11] else ''}" for c in CASES]
 
 
@@ -76,6 +80,30 @@ def test_forward(lasad, c):
     check(lse, want_lse, lse_bound, "lse")
     none = ~mask.any(-1)
     assert (o.cpu()[none] == 0).all()
+
+
+@pytest.mark.parametrize("many", MANY, ids=lambda m: f"{str(m[0][0])[6:]}-d{m[0][2]}-{m[2]}x{m[3]}-B{m[1]}-{m[0][6]}+{m[0][7]}of{m[0][8]}-w{m[0][9]}-s{m[0][10]}")
+def test_many_heads(lasad, many):
+    """Forward and backward, with the reference's 64-bit arithmetic on the GPU."""
+    c, B, Hq, Hk = many
+    lens = None if c[11] is None else (c[11] * B)[:B]
+    c = (*c[:3], Hq, Hk, B, *c[6:11], lens)
+    q, k, v, mask = inputs(c)
+    do = ref.draw(q.shape, q.dtype, 55)
+    dev, mask = [t.cuda() for t in (q, k, v, do)], mask.cuda()
+    kw = dict(start_pos=c[6], kv_lens=lens_of(c))
+    o, lse = lasad.lasad_forward_window(*dev[:3], c[9], c[10], want_lse=True, **kw)
+    o32 = lasad.lasad_forward_window(*dev[:3], c[9], c[10], out_dtype=F, **kw)
+    got = lasad.lasad_backward_window(*dev[:3], o, lse, dev[3], c[9], c[10], grad_dtype=c[1], **kw)
+    x = [t.double() for t in dev]
+    want, want_lse = ref.window_forward(*x[:3], mask, c[2] ** -0.5)
+    bound, lse_bound = ref.window_forward_bounds(*x[:3], mask, c[2] ** -0.5, c[0], F, want, want_lse)
+    check(o32, want.cpu(), bound.cpu(), "o")
+    check(lse, want_lse.cpu(), lse_bound.cpu(), "lse")
+    assert torch.equal(o, o32.to(c[0]))
+    grads = ref.window_backward(*x, mask, c[2] ** -0.5)
+    for g, w, b, what in zip(got, grads, ref.window_backward_bounds(*x, mask, c[2] ** -0.5, c[0], c[1], grads), ("dq", "dk", "dv")):
+        check(g, w.cpu(), b.cpu(), what)
 
 
 @pytest.mark.parametrize("c", CASES, ids=IDS)
@@ -134,13 +162,14 @@ def test_views_heads_first_and_broadcast_inputs(lasad, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
-def test_what_is_not_seen_has_no_part(lasad, dtype, value):
+@pytest.mark.parametrize("B", [2, 160])
+def test_what_is_not_seen_has_no_part(lasad, dtype, value, B):
     """Keys past a row's length, past the last query and before all windows hold `value`: nothing changes.  One key in the middle
     does: only its own queries change."""
-    B, n, m, start, w, s, d = 2, 150, 400, 130, 40, 2, 64
+    n, m, start, w, s, d = 150, 400, 130, 40, 2, 64
     q, k, v = ref.draw((B, n, 2, d), dtype, 1), ref.draw((B, m, 1, d), dtype, 2), ref.draw((B, m, 1, d), dtype, 3)
     do = ref.draw(q.shape, dtype, 4)
-    lens = [400, 200]
+    lens = [400, 200] + [400] * (B - 2)
     mask = ref.seen_mask(n, m, start, w, s, lens, B)
     kw = dict(start_pos=start, kv_lens=torch.tensor(lens, dtype=torch.int32, device="cuda"))
 
