@@ -234,12 +234,12 @@ int64_t back_tile(int64_t total)
     return t < 4 ? 4 : t > kBackTile ? kBackTile : t;
 }
 
-// Four wavefronts take the workgroup's tokens in turn, group after group of 64 / LPR heads, so that a lane's head stays the
+// Four wavefronts take the workgroup's tokens in turn, group after group of 64 / LPR of its `share` of the heads, so that a lane's head stays the
 // same over its tokens and the weight gradient stays in its registers.  Per head they are added up over the wavefronts at
 // the end of a group, shared ones at the end of the workgroup; a second kernel adds the workgroups' sums in their order.
 template <int BF16, int OBF16, int D, int SHARED>
 __global__ void __launch_bounds__(kThreads)
-qk_backward_kernel(QkArgs a, int tile)
+qk_backward_kernel(QkArgs a, int tile, int share)
 {
     constexpr int LPR = D / 8, P = D / 2, RPW = 64 / LPR;
     constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4;
@@ -258,7 +258,8 @@ qk_backward_kernel(QkArgs a, int tile)
     float accq[8], acck[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) accq[e] = acck[e] = 0.f;
-    for (int g0 = 0; g0 < heads; g0 += RPW) {
+    const int g_end = min(heads, (int)(blockIdx.y + 1) * share);
+    for (int g0 = blockIdx.y * share; g0 < g_end; g0 += RPW) {
         const int h = g0 + lane / LPR;
         const int x = h < a.heads[0] ? 0 : 1, hx = h - (x ? a.heads[0] : 0);
         float w[8], acc[8];
@@ -325,7 +326,7 @@ qk_backward_kernel(QkArgs a, int tile)
             const int x = i / D, c = i % D;
             float sum = 0.f;
             for (int r = 0; r < 4 * RPW; ++r) sum += red[x * 2048 + ((c & 7) * 4 + r / RPW) * 64 + (r % RPW) * LPR + c / 8];
-            a.partial[(int64_t)blockIdx.x * 2 * D + i] = sum;
+            a.partial[((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 2 * D + i] = sum;
         }
     }
 }
@@ -364,22 +365,33 @@ qk_weight_kernel(const float *partial, int64_t rows, int columns, int q_columns,
 
 }  // namespace
 
+// Heads of a workgroup: all of them, or a share in whole groups where the tokens alone do not make 512 workgroups.
+static int head_share(int64_t groups, int heads, int d)
+{
+    const int rows = 512 / d, pieces = (heads + rows - 1) / rows;            // heads of a group, groups
+    int64_t parts = groups > 0 ? 512 / groups : 1;
+    parts = parts < 1 ? 1 : parts > pieces ? pieces : parts;
+    return (int)((pieces + parts - 1) / parts) * rows;
+}
+
 size_t qk_partial_bytes(int64_t tokens, int heads, int d, int shared)
 {
     const int64_t tile = back_tile(tokens), groups = (tokens + tile - 1) / tile;
-    return (size_t)groups * (shared ? 2 : heads) * d * sizeof(float);
+    const int share = head_share(groups, heads, d);
+    return (size_t)groups * (shared ? 2 * ((heads + share - 1) / share) : heads) * d * sizeof(float);
 }
 
 hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s)
 {
     const int64_t total = (int64_t)a.B * a.n, tile = back_tile(total), groups = (total + tile - 1) / tile;
     const bool want = a.norm && (a.dw[0] || a.dw[1]);
+    const int heads = a.heads[0] + a.heads[1], share = head_share(groups, heads, a.d);
     QkArgs b = a;
     if (!want) b.partial = nullptr;
     if (groups > 0) {
-        const dim3 grid((unsigned)groups), block(kThreads);
-#define LASAD_QK(I, O, D) (a.shared ? (void)(qk_backward_kernel<I, O, D, 1><<<grid, block, 0, s>>>(b, (int)tile)) \
-                                    : (void)(qk_backward_kernel<I, O, D, 0><<<grid, block, 0, s>>>(b, (int)tile)))
+        const dim3 grid((unsigned)groups, (unsigned)((heads + share - 1) / share)), block(kThreads);
+#define LASAD_QK(I, O, D) (a.shared ? (void)(qk_backward_kernel<I, O, D, 1><<<grid, block, 0, s>>>(b, (int)tile, share)) \
+                                    : (void)(qk_backward_kernel<I, O, D, 0><<<grid, block, 0, s>>>(b, (int)tile, share)))
 #define LASAD_QK_D(I, O) (a.d == 32 ? LASAD_QK(I, O, 32) : a.d == 64 ? LASAD_QK(I, O, 64) : LASAD_QK(I, O, 128))
         if (a.io_dtype == LASAD_BF16) { if (a.out_dtype == LASAD_BF16) LASAD_QK_D(1, 1); else LASAD_QK_D(1, 0); }
         else LASAD_QK_D(0, 0);
@@ -389,8 +401,9 @@ hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s)
         if (e != hipSuccess) return e;
     }
     if (want) {
-        const int columns = (a.shared ? 2 : a.heads[0] + a.heads[1]) * a.d;
-        qk_weight_kernel<<<dim3(columns / 32), dim3(kThreads), 0, s>>>(a.partial, groups, columns, (a.shared ? 1 : a.heads[0]) * a.d,
+        const int columns = (a.shared ? 2 : heads) * a.d;
+        const int64_t rows = a.shared ? groups * ((heads + share - 1) / share) : groups;
+        qk_weight_kernel<<<dim3(columns / 32), dim3(kThreads), 0, s>>>(a.partial, rows, columns, (a.shared ? 1 : a.heads[0]) * a.d,
                                                                  a.dw[0], a.dw[1]);
         return hipGetLastError();
     }

@@ -15,7 +15,7 @@ namespace lasad {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kWaves = 4;                // of the join
 constexpr float kLog2e = 1.4426950408889634f;
 
 template <int BF16, int VEC>
@@ -50,6 +50,20 @@ __device__ inline float row_sum(float x)
     return x;
 }
 
+// x of the lanes that hold the same channels (lane % LPT) combined, in every one of them.  The rotations by 4 and 8 lanes are inside 16.
+template <int LPT, typename Op>
+__device__ inline float over_slots(float x, Op op)
+{
+    if (LPT <= 4) x = op(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, true)));
+    if (LPT <= 8) x = op(x, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, true)));
+    if (LPT <= 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return op(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // What a batch row at position `pos` sees: keys 0 .. far - 1, then near .. pos; false: the row is inactive.
 struct Seen {
     int far, near, count;              // count: both together
@@ -77,8 +91,8 @@ __device__ inline int cache_row(const WindowStepArgs &a, const Seen &s, int t)
 }
 
 // Workgroup: one key head of one batch row (blockIdx.x), one chunk of at most GC of its query heads (y), one split (z).
-template <int BF16, int OBF16, int D, int GC>
-__global__ void __launch_bounds__(kThreads)
+template <int BF16, int OBF16, int D, int GC, int WAVES>
+__global__ void __launch_bounds__(WAVES * 64)
 window_step_kernel(WindowStepArgs a)
 {
     constexpr int VEC = BF16 ? 8 : 4, LPT = D / VEC, TPW = 64 / LPT, UNROLL = 4, ELT = BF16 ? 2 : 4;
@@ -101,7 +115,7 @@ window_step_kernel(WindowStepArgs a)
         for (int e = 0; e < VEC; ++e) q[g][e] *= a.scale * kLog2e;
     }
     // this split's keys; its share in whole steps of the workgroup
-    constexpr int STEP = kWaves * UNROLL * TPW;
+    constexpr int STEP = WAVES * UNROLL * TPW;
     const int share = ((s.count + a.splits - 1) / a.splits + STEP - 1) / STEP * STEP;
     const int t0 = min(s.count, (int)blockIdx.z * share), t1 = min(s.count, t0 + share);
     // (the own row's old contents are not read by this call: its key comes from the arguments)
@@ -172,22 +186,17 @@ window_step_kernel(WindowStepArgs a)
     }
 
     // join the groups of lanes, then the wavefronts
-    __shared__ float red[kWaves][GC][D + 2];
+    __shared__ float red[WAVES][GC][D + 2];
 #pragma unroll
     for (int g = 0; g < GC; ++g) {
-        float top = m[g];
-#pragma unroll
-        for (int off = LPT; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+        const auto add = [](float x, float y) { return x + y; };
+        const float top = over_slots<LPT>(m[g], [](float x, float y) { return fmaxf(x, y); });
         const float f = __builtin_amdgcn_exp2f(m[g] - (top == -INFINITY ? 0.f : top));
-        l[g] *= f;
-#pragma unroll
-        for (int off = LPT; off < 64; off <<= 1) l[g] += __shfl_xor(l[g], off);
+        l[g] = over_slots<LPT>(l[g] * f, add);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            acc[g][e] *= f;
-#pragma unroll
-            for (int off = LPT; off < 64; off <<= 1) acc[g][e] += __shfl_xor(acc[g][e], off);
-            if (slot == 0) red[wave][g][piece * VEC + e] = acc[g][e];
+            const float x = over_slots<LPT>(acc[g][e] * f, add);
+            if (slot == 0) red[wave][g][piece * VEC + e] = x;
         }
         if (lane == 0) {
             red[wave][g][D] = top;
@@ -195,16 +204,16 @@ window_step_kernel(WindowStepArgs a)
         }
     }
     __syncthreads();
-    for (int i = tid; i < GC * D; i += kThreads) {
+    for (int i = tid; i < GC * D; i += WAVES * 64) {
         const int g = i / D, c = i % D;
         if (g0 + g >= G) continue;
         float top = red[0][g][D];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) top = fmaxf(top, red[w][g][D]);
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red[w][g][D]);
         const float use = top == -INFINITY ? 0.f : top;
         float sum = 0.f, o = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float f = __builtin_amdgcn_exp2f(red[w][g][D] - use);
             sum = fmaf(red[w][g][D + 1], f, sum);
             o = fmaf(red[w][g][c], f, o);
@@ -268,17 +277,24 @@ window_join_kernel(WindowStepArgs a)
     else ((float *)a.o)[row * D + e] = r;
 }
 
-template <int BF16, int OBF16, int D>
-hipError_t launch(const WindowStepArgs &a, hipStream_t s)
+template <int BF16, int OBF16, int D, int WAVES>
+void launch_step(const WindowStepArgs &a, hipStream_t s)
 {
     const int G = a.Hq / a.Hk;
     const unsigned x = (unsigned)(a.B * a.Hk), z = (unsigned)a.splits;
-#define LASAD_WS(GC) window_step_kernel<BF16, OBF16, D, GC><<<dim3(x, (G + GC - 1) / GC, z), dim3(kThreads), 0, s>>>(a)
+#define LASAD_WS(GC) window_step_kernel<BF16, OBF16, D, GC, WAVES><<<dim3(x, (G + GC - 1) / GC, z), dim3(WAVES * 64), 0, s>>>(a)
     if (G == 1) LASAD_WS(1);
     else if (G == 2) LASAD_WS(2);
     else if (G == 3) LASAD_WS(3);
     else LASAD_WS(4);
 #undef LASAD_WS
+}
+
+template <int BF16, int OBF16, int D>
+hipError_t launch(const WindowStepArgs &a, hipStream_t s)
+{
+    if ((int64_t)a.B * a.Hk * a.splits <= 256) launch_step<BF16, OBF16, D, 8>(a, s);
+    else launch_step<BF16, OBF16, D, 4>(a, s);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         window_join_kernel<OBF16, D><<<dim3((unsigned)(a.B * a.Hq)), dim3(kThreads), 0, s>>>(a);
@@ -289,14 +305,16 @@ hipError_t launch(const WindowStepArgs &a, hipStream_t s)
 
 }  // namespace
 
-// Splits of a call whose rows see up to `seen` keys: enough workgroups for the chip's 256 units twice, none for less than
-// 512 keys.
+// Splits of a call whose rows see up to `seen` keys: enough workgroups for the chip's 256 units twice, of at least 256 keys each; the
+// join's launch costs as much as 700 keys more in a workgroup (12 heads, us without and with: 1024 keys 7.1 and 8.0, 2048 10.5 and
+// 8.1, 16384 73 and 13), and two splits of many heads gain nothing (256 heads of 4096 keys 40 and 43).
 int window_step_splits(int B, int Hk, int64_t seen)
 {
     const int64_t heads = (int64_t)B * Hk;
     int64_t n = 512 / heads;
-    if (n > seen / 512) n = seen / 512;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    if (seen < 1536 || n < 4) return 1;
+    if (n > seen / 256) n = seen / 256;
+    return (int)(n > 64 ? 64 : n);
 }
 
 size_t window_step_bytes(int B, int Hq, int d, int splits)
