@@ -12,6 +12,12 @@
 // memory alone are the angles: a sine and a cosine cost some 60 operations, four pairs to a lane's 16 bytes.  All heads
 // of a token share them, so a workgroup forms the table of its tokens in LDS first, one pair to a thread.  The angle is
 // formed in fp64 as turns and reduced there (position 2^30 leaves 2^-23 turns), the sine of the rest in fp32.
+//
+// Measured, bf16, d = 64: 4 x 4096 tokens of 48 heads (201 MB) 35 us a launch and 45 in a stream of them on inputs that are not
+// cached, 4.5 TB/s where a copy of 1 GiB reaches 4.94; backward of 32 x 576 tokens of 32 heads (235 MB with the workgroups' weight
+// sums) 40 us, and 4.7 for the second kernel.  One token of 24 heads 3 us.  Stores past the caches take the stream of forwards to
+// 39.4 us, but what reads the outputs next then finds none of them in the 256 MB in front of the memory (with the attention after
+// it: 96 MB of outputs 96 us and 105 so, 192 MB 192 and 195, 768 MB 747 and 740), so they are ordinary ones.
 #include "lasad_attention.h"
 #include "lasad_mfma_util.h"
 
@@ -234,9 +240,9 @@ int64_t back_tile(int64_t total)
     return t < 4 ? 4 : t > kBackTile ? kBackTile : t;
 }
 
-// Four wavefronts take the workgroup's tokens in turn, group after group of 64 / LPR of its `share` of the heads, so that a lane's head stays the
-// same over its tokens and the weight gradient stays in its registers.  Per head they are added up over the wavefronts at
-// the end of a group, shared ones at the end of the workgroup; a second kernel adds the workgroups' sums in their order.
+// Four wavefronts take the workgroup's tokens in turn, group after group of 64 / LPR of its `share` of the heads, so that a lane's
+// head stays the same over its tokens and the weight gradient stays in its registers.  Per head they are added up over the
+// wavefronts at the end of a group, shared ones at the end of the workgroup; a second kernel adds the workgroups' sums in their order.
 template <int BF16, int OBF16, int D, int SHARED>
 __global__ void __launch_bounds__(kThreads)
 qk_backward_kernel(QkArgs a, int tile, int share)

@@ -6,6 +6,15 @@
 // then those of the window), staged in LDS twice, the next tile's loads in flight over the products of the present one.
 // Sums are fp32; the only rounding between q, k, v and o is that of 2^(s - m) to the storage type as the second product's
 // operand (bf16: half a step of 2^-8, of terms of one sign; l is added up from the unrounded ones).
+//
+// Measured, bf16, d = 64, 4 x 24 heads of 4096 tokens, window 1024, 16 sinks: 142 us, 640 TFLOP/s of the pairs that are seen (91.4
+// GFLOP; a product of 8192^3 reaches 1221).  No unit is full there: the vector units issue 62 % of the time (16 exponentials,
+// 16 multiply-adds, 16 additions, 9 maxima, 8 conversions a block of 32 x 32, some 110 with the edges and addresses), the matrix cores
+// are busy for 31 %, LDS for 32 %; a block is one chain of products, maximum, exponentials and products, 0.6 us for a wavefront
+// alone, and four wavefronts a SIMD hide 60 % of it.  Timed without a part (us): tile loads and stores 114, exponentials 126,
+// the second product 120.  512 heads of 576 tokens, window 144: 49 us for 260 MB, 5.2 TB/s, near the memory's rate.
+// Took longer, in the first case's us: 64 queries a wavefront 181, eight wavefronts to a tile 155, all of a head's queries launched
+// together 151, priorities of wavefronts 143 to 151.  Tiles loaded straight into LDS came to 138 before the rearrangement they need.
 #include "lasad_window.h"
 
 namespace lasad {

@@ -8,6 +8,10 @@
 // A group of lanes keeps maximum, sum and output of its rows for every query head of the group; they are joined over the
 // groups by cross-lane exchange, over the wavefronts in LDS, and, where few heads have many rows, over `splits` workgroups
 // by a second kernel.
+//
+// Measured, bf16, d = 64: 64 rows, 24 heads over 8, 1040 keys (116 MB) 23 us, 5.0 TB/s; 2 rows of 16 heads, 16448 keys (135 MB)
+// 22 us, 6.1 TB/s (part of it cached), and 3.8 for the join; one row of 12 heads, 129 keys 4.1 us, which is a launch and two
+// memory latencies.  A large copy reaches 4.94 TB/s.
 #include "lasad_attention.h"
 #include "lasad_mfma_util.h"
 
