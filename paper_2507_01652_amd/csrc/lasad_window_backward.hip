@@ -6,7 +6,8 @@
 // that changes from run to run.
 //
 // Query pass: as in the forward, 32 queries to a wavefront, the seen key tiles staged in LDS.  It also forms delta.
-// Key pass: 32 keys to a wavefront, 128 of one head to a workgroup, which walks the tiles of the queries that see any of them,
+// Key pass: 16 keys to a wavefront and 64 of one head to a workgroup (lasad_window_backward_keys.hip; fp32, here: 32 and 128), which walks
+// the tiles of the queries that see any of them,
 // head after head of the group.  Ordinary keys are seen from `window` positions on, the sinks from all later ones: their
 // tiles are cut into parts of about an ordinary tile's work, whose sums a small kernel adds up in their order.
 // In the key pass -lse / scale and -delta are what the sums of the first two products start from, so that an entry costs a product and
@@ -16,11 +17,9 @@
 // of dS 1.7e-3, o's 0.7e-3, together 2.5e-3; dS as two operands would take the second part and cost a quarter to a third more products.
 //
 // Measured, bf16, d = 64: 2 x 24 heads over 8 of 4096 tokens, window 1024, 16 sinks: query pass 102 us (68.5 GFLOP of three products,
-// 670 TFLOP/s), key pass 157 (four, 580) and 4.8 for the parts; 512 heads of 576 tokens, window 144: 75 (4.5 TB/s) and 104 (3.3).  Neither
-// the matrix cores (30 and 26 % of the time) nor LDS (26 and 30) nor the vector units (40 and 28) are full: a block is one chain of
-// products, exponentials and products, and there are registers for three (two) wavefronts a SIMD to hide it: the key pass needs 229.
-// Took longer, in the key pass' us: three wavefronts a SIMD 240 (spills), two blocks side by side 214 (spills), operands read late 172 to 181;
-// in the query pass sums that start from -lse and -delta (spills).
+// 670 TFLOP/s); 512 heads of 576 tokens, window 144: 75 (4.5 TB/s).  Neither the matrix cores (30 % of the time) nor LDS (26) nor the vector
+// units (40) are full: a block is one chain of products, exponentials and products, and there are registers for three wavefronts a SIMD
+// to hide it.  Sums that start from -lse and -delta, as in the key pass, spill.  4.8 us for the sum of the parts.
 #include "lasad_window.h"
 
 namespace lasad {
@@ -198,20 +197,15 @@ window_dq_kernel(WindowArgs a)
 
 // One block of 32 queries (positions from pb on, rows of qt and gt, their -lse / scale and -delta) for a wavefront's keys: P and dS, and
 // their products with d_o and q.
-template <typename T, int D>
-__device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (&k)[D / Mat<T>::KF], const typename Mat<T>::F (&v)[D / Mat<T>::KF],
-                                 const T *qt, const T *gt, const float *shift, const float *delta, int pb, int keys, int w0, const Edge &edge,
+template <int D>
+__device__ inline void dkv_block(const WindowArgs &a, const float4 (&k)[D / 8], const float4 (&v)[D / 8],
+                                 const float *qt, const float *gt, const float *shift, const float *delta, int pb, int keys, int w0, const Edge &edge,
                                  float scale2, int lane, f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32])
 {
-    typedef Mat<T> M;
+    typedef Mat<float> M;
     typedef typename M::F F;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
-    // (bf16: all LDS reads of a product are issued before its first step)
-    constexpr bool EARLY = D <= 64 && sizeof(T) == 2;
     const int half = lane >> 5, col = lane & 31;
-    F qf[NF], gf[NF], qc[M::GROUPS][DB], gc[M::GROUPS][DB];
-#pragma unroll
-    for (int f = 0; f < NF; ++f) { qf[f] = M::row(qt + col * LD, f, half); gf[f] = M::row(gt + col * LD, f, half); }
     f32x16 s, dp;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -219,21 +213,10 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
         s[4 * r] = x.x; s[4 * r + 1] = x.y; s[4 * r + 2] = x.z; s[4 * r + 3] = x.w;
         dp[4 * r] = y.x; dp[4 * r + 1] = y.y; dp[4 * r + 2] = y.z; dp[4 * r + 3] = y.w;
     }
-    const auto columns = [&]() {
 #pragma unroll
-        for (int r = 0; r < M::GROUPS; ++r)
-#pragma unroll
-            for (int d = 0; d < DB; ++d) {
-                gc[r][d] = M::column(gt, LD, d * 32, r, lane);
-                qc[r][d] = M::column(qt, LD, d * 32, r, lane);
-            }
-    };
-    if (EARLY) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int f = 0; f < NF; ++f) { s = M::mma(qf[f], k[f], s); dp = M::mma(gf[f], v[f], dp); }
-    if (EARLY) {
-        columns();
-        __builtin_amdgcn_sched_barrier(0);
+    for (int f = 0; f < NF; ++f) {
+        s = M::mma(M::row(qt + col * LD, f, half), k[f], s);
+        dp = M::mma(M::row(gt + col * LD, f, half), v[f], dp);
     }
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -245,26 +228,26 @@ __device__ inline void dkv_block(const WindowArgs &a, const typename Mat<T>::F (
         hide(s, edge, pb, half, last_edge, first_edge, 0.f);
         hide(dp, edge, pb, half, last_edge, first_edge, 0.f);
     }
-    if (!EARLY) columns();
 #pragma unroll
     for (int r = 0; r < M::GROUPS; ++r) {
         const F pf = M::pack(s, r), df = M::pack(dp, r);
 #pragma unroll
         for (int d = 0; d < DB; ++d) {
-            dv[d] = M::mma(gc[r][d], pf, dv[d]);
-            dk[d] = M::mma(qc[r][d], df, dk[d]);
+            dv[d] = M::mma(M::column(gt, LD, d * 32, r, lane), pf, dv[d]);
+            dk[d] = M::mma(M::column(qt, LD, d * 32, r, lane), df, dk[d]);
         }
     }
 }
 
 // Workgroups: first the sinks' key tiles, part after part, then the others.
-template <typename T, typename O, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads, D <= 64 ? 2 : 1)
-window_dkv_kernel(WindowArgs a)
+window_dkv_f32_kernel(WindowArgs a)
 {
+    typedef float T;
     typedef Mat<T> M;
-    typedef typename M::F F;
-    constexpr int QT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, QB = QT / 32, DB = D / 32, NF = D / M::KF;
+    typedef float4 F;
+    constexpr int QT = 32, LD = D + M::PAD, QB = QT / 32, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = QT / RPP;
     __shared__ __align__(16) T tile[2][2][QT * LD];
     __shared__ __align__(16) float stat[2][2][QT];       // -lse / scale and -delta of a tile's queries
@@ -378,7 +361,7 @@ window_dkv_kernel(WindowArgs a)
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
             if (!sees_none(a, keys, p0 + 32 * qb, p0 + 32 * qb + 31, w0, w1))
-                dkv_block<T, D>(a, k, v, qt + qb * 32 * LD, gt + qb * 32 * LD, stat[t & 1][0] + 32 * qb, stat[t & 1][1] + 32 * qb, p0 + 32 * qb,
+                dkv_block<D>(a, k, v, qt + qb * 32 * LD, gt + qb * 32 * LD, stat[t & 1][0] + 32 * qb, stat[t & 1][1] + 32 * qb, p0 + 32 * qb,
                                 keys, w0, edge, scale2, lane, dk, dv);
         if (t + 1 < steps) store((t + 1) & 1, ti);
         __syncthreads();
@@ -412,8 +395,8 @@ window_dkv_kernel(WindowArgs a)
         return;
     }
     if (jk >= a.m) return;
-    O *dkp = (O *)a.dk + (int64_t)b * a.ldk.stride_b + (int64_t)jk * a.ldk.stride_n + (int64_t)hk * a.ldk.stride_h;
-    O *dvp = (O *)a.dv + (int64_t)b * a.ldv.stride_b + (int64_t)jk * a.ldv.stride_n + (int64_t)hk * a.ldv.stride_h;
+    float *dkp = (float *)a.dk + (int64_t)b * a.ldk.stride_b + (int64_t)jk * a.ldk.stride_n + (int64_t)hk * a.ldk.stride_h;
+    float *dvp = (float *)a.dv + (int64_t)b * a.ldv.stride_b + (int64_t)jk * a.ldv.stride_n + (int64_t)hk * a.ldv.stride_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -451,25 +434,37 @@ window_sink_sum_kernel(WindowArgs a)
     store4(out, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
-// Few keys (queries): too few workgroups of 128 to fill the chip's 256 units; a workgroup then has 32.  us, few and many, window 128
-// of 256 tokens, 12 heads: batch 2 20.0 and 27.6, 4 (96 workgroups) 22.5 and 28.1, 6 (144) 29.3 and 28.4, 8 33.8 and 28.6; 4 heads of
-// 4096, window 1024 (128) 52 and 80.  d = 128: 2 (48) 30 and 45, 4 (96) 47 and 45, 6 65 and 47.  fp32: 4 58 and 82, 8 (192) 96 and 85.
+// Few queries (fp32: or keys): too few workgroups of 128 to fill the chip's 256 units; a workgroup then has 32.  us, few and many: query
+// pass, d = 64, all of 2048 tokens seen: 96 workgroups 27 and 44, 144 43 and 47, 384 61 and 53; window 256: 96 12.6 and 15.6, 144 21 and 17; 256
+// tokens, window 32: 144 11.4 and 12.0, 256 14.9 and 12.8.  d = 128, window 256: 64 14 and 24, 96 26 and 25, 144 47 and 28.  Both passes in
+// fp32, window 128 of 256 tokens, 12 heads: batch 4 (96) 58 and 82, 8 (192) 96 and 85.
 bool few(int64_t heads, int64_t count, int d) { return heads * ((count + kTile - 1) / kTile) < (d == 128 ? 96 : 144); }
+
+// The same of keys in bf16, where a workgroup of 64 walks the `steps` tiles of 64 queries that see an ordinary key tile: one of 32, whose four
+// wavefronts share them out, pays where there are several.  us, few and many, d = 64, counted in 128 keys: 2048 tokens, all seen, 96 28 and
+// 51, 144 48 and 55, 384 69 and 60; window 256 (5 steps) 64 11.9 and 12.9, 96 15.0 and 13.3; window 32 (2) 48 8.2 and 8.2, 96 9.9
+// and 8.5.  d = 128, window 256: 64 17 and 20, 96 33 and 20; all seen 96 42 and 78, 144 95 and 87.
+bool few_keys(int64_t heads, int64_t m, int64_t steps)
+{
+    return heads * ((m + 127) / 128) < (steps < 4 ? 0 : steps < 16 ? 72 : 128);
+}
 
 // The key pass' tiles, those with sinks, and the parts they are cut into.  In steps of 64 queries: an ordinary tile takes
 // (window + tile) / 64, one with sinks n / 64.  Uncut it ends last where it takes longer than an ordinary one and than half of what
-// the chip's 512 workgroup slots have to do anyway; a part takes about that long.  At most 1024 parts, which bounds the workspace.
+// the chip's 512 workgroup slots (of 64 keys: 1024) have to do anyway; a part takes about that long.  At most 1024 parts, which bounds the workspace.
 struct Plan {
     int tile, sink_tiles, parts;
 };
-Plan plan(int64_t heads, int d, int n, int m, int window, int sinks)
+Plan plan(int io_dtype, int64_t heads, int d, int n, int m, int window, int sinks)
 {
     Plan r;
-    r.tile = few(heads, m, d) ? 32 : kTile;
+    const int64_t sink = (n + 63) / 64;
+    const auto ordinary_steps = [&](int tile) { const int64_t near = ((int64_t)window + tile + 63) / 64; return near < sink ? near : sink; };
+    if (io_dtype == LASAD_BF16) r.tile = few_keys(heads, m, ordinary_steps(kWindowKeyTile)) ? 32 : kWindowKeyTile;
+    else r.tile = few(heads, m, d) ? 32 : kTile;
     r.sink_tiles = (int)(((int64_t)(sinks < m ? sinks : m) + r.tile - 1) / r.tile);
-    const int64_t all = ((int64_t)m + r.tile - 1) / r.tile, sink = (n + 63) / 64, near = ((int64_t)window + r.tile + 63) / 64;
-    const int64_t ordinary = near < sink ? near : sink;
-    const int64_t slot = heads * ((all - r.sink_tiles) * ordinary + r.sink_tiles * sink) / 512;
+    const int64_t all = ((int64_t)m + r.tile - 1) / r.tile, ordinary = ordinary_steps(r.tile);
+    const int64_t slot = heads * ((all - r.sink_tiles) * ordinary + r.sink_tiles * sink) / (r.tile == kWindowKeyTile ? 1024 : 512);
     const int64_t long_enough = ordinary > slot / 2 ? ordinary : slot / 2;
     const int64_t want = long_enough > 0 ? (sink + long_enough - 1) / long_enough : 1, most = r.sink_tiles > 0 ? 1024 / (heads * r.sink_tiles) : 1;
     const int64_t parts = want > most ? most : want;
@@ -483,15 +478,20 @@ size_t delta_bytes(int B, int Hq, int n) { return ((size_t)B * Hq * n * sizeof(f
 
 size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int window, int sinks)
 {
-    const Plan r = plan((int64_t)B * Hk, d, n, m, window, sinks);
-    return delta_bytes(B, Hq, n) + (r.parts > 1 ? (size_t)B * Hk * r.sink_tiles * r.parts * 2 * r.tile * d * sizeof(float) : 0);
+    size_t parts = 0;                                    // (whichever type needs more)
+    for (int type : {LASAD_F32, LASAD_BF16}) {
+        const Plan r = plan(type, (int64_t)B * Hk, d, n, m, window, sinks);
+        const size_t bytes = (size_t)B * Hk * r.sink_tiles * r.parts * 2 * r.tile * d * sizeof(float);
+        if (r.parts > 1 && bytes > parts) parts = bytes;
+    }
+    return delta_bytes(B, Hq, n) + parts;
 }
 
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
 {
     a.delta = (float *)workspace;
     a.parts = (float *)((char *)workspace + delta_bytes(a.B, a.Hq, a.n));
-    const Plan r = plan((int64_t)a.B * a.Hk, a.d, a.n, a.m, a.window, a.sinks);
+    const Plan r = plan(a.io_dtype, (int64_t)a.B * a.Hk, a.d, a.n, a.m, a.window, a.sinks);
     a.key_tile = r.tile; a.sink_tiles = r.sink_tiles; a.sink_parts = r.parts;
     hipError_t e = hipSuccess;
     if (a.n > 0) {
@@ -509,11 +509,13 @@ hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
     if (a.m == 0) return hipSuccess;
     if (r.tile == 32) {
         e = launch_window_dkv_few(a, s);
+    } else if (a.io_dtype == LASAD_BF16) {
+        e = launch_window_dkv_bf16(a, s);
     } else {
         const dim3 grid(launch_grid((int64_t)a.B * a.Hk, r.sink_tiles * r.parts + (a.m + kTile - 1) / kTile - r.sink_tiles));
-#define LASAD_WK(T, O, D) window_dkv_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
-        LASAD_WINDOW_DISPATCH(LASAD_WK);
-#undef LASAD_WK
+        if (a.d == 32) window_dkv_f32_kernel<32><<<grid, dim3(kThreads), 0, s>>>(a);
+        else if (a.d == 64) window_dkv_f32_kernel<64><<<grid, dim3(kThreads), 0, s>>>(a);
+        else window_dkv_f32_kernel<128><<<grid, dim3(kThreads), 0, s>>>(a);
         e = hipGetLastError();
     }
     if (e == hipSuccess && r.sink_tiles > 0 && r.parts > 1) {
