@@ -38,6 +38,7 @@ SOURCES = [
     "lasad_qk.hip",
     "lasad_window_forward.hip",
     "lasad_window_backward.hip",
+    "lasad_window_backward_queries.hip",
     "lasad_window_backward_keys.hip",
     "lasad_window_backward_few.hip",
     "lasad_window_step.hip",

@@ -52,6 +52,7 @@ hipError_t launch_window_dq_few(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_dkv_few(const WindowArgs &a, hipStream_t s);
 constexpr int kWindowKeyTile = 64;     // keys of a workgroup of launch_window_dkv_bf16
 hipError_t launch_window_dkv_bf16(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_dq_bf16(const WindowArgs &a, hipStream_t s);
 size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int window, int sinks);
 
 // One token against a cache [B, Hk, cap, d]: key j lies in row j < sinks ? j : sinks + (j - sinks) mod (cap - sinks).

@@ -5,9 +5,8 @@
 // queries gives dk and dv.  One pass would save two of the seven products and add dq up by atomics, in an order
 // that changes from run to run.
 //
-// Query pass: as in the forward, 32 queries to a wavefront, the seen key tiles staged in LDS.  It also forms delta.
-// Key pass: 16 keys to a wavefront and 64 of one head to a workgroup (lasad_window_backward_keys.hip; fp32, here: 32 and 128), which walks
-// the tiles of the queries that see any of them,
+// Query pass: as in the forward, the seen key tiles staged in LDS.  It also forms delta.
+// Key pass: a workgroup has keys of one head and walks the tiles of the queries that see any of them,
 // head after head of the group.  Ordinary keys are seen from `window` positions on, the sinks from all later ones: their
 // tiles are cut into parts of about an ordinary tile's work, whose sums a small kernel adds up in their order.
 // In the key pass -lse / scale and -delta are what the sums of the first two products start from, so that an entry costs a product and
@@ -16,10 +15,10 @@
 // was stored.  In the root mean square (16 heads of 576 tokens, window 144, unit variances) storing dq costs 1.7e-3 of it, the rounding
 // of dS 1.7e-3, o's 0.7e-3, together 2.5e-3; dS as two operands would take the second part and cost a quarter to a third more products.
 //
-// Measured, bf16, d = 64: 2 x 24 heads over 8 of 4096 tokens, window 1024, 16 sinks: query pass 102 us (68.5 GFLOP of three products,
-// 670 TFLOP/s); 512 heads of 576 tokens, window 144: 75 (4.5 TB/s).  Neither the matrix cores (30 % of the time) nor LDS (26) nor the vector
-// units (40) are full: a block is one chain of products, exponentials and products, and there are registers for three wavefronts a SIMD
-// to hide it.  Sums that start from -lse and -delta, as in the key pass, spill.  4.8 us for the sum of the parts.
+// bf16: lasad_window_backward_queries.hip and lasad_window_backward_keys.hip, 16 queries (keys) to a wavefront and 64 to a workgroup.
+// fp32, here: 32 and 128.  Products of 32 x 32 x 2 bound it, and two wavefronts a SIMD (175 and 230 registers of d = 64) that hide little
+// of what is between them: 2 x 20 heads of 1024 tokens, window 256, query pass 78 us and key pass 100, 48 and 50 TFLOP/s of the pairs that
+// are seen (a product of 8192^3: 154); the tiles of 128 cover half as many pairs again.
 #include "lasad_window.h"
 
 namespace lasad {
@@ -29,12 +28,11 @@ namespace {
 constexpr int kThreads = 256, kTile = 128;               // queries (keys) of a workgroup
 
 // One block of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: dS, and its product with k.
-template <typename T, int D>
-__device__ inline void dq_block(const typename Mat<T>::F (&q)[D / Mat<T>::KF], const typename Mat<T>::F (&g)[D / Mat<T>::KF],
-                                const T *kt, const T *vt, int j0, const Range &range, const Edge &edge, float scale2, float lse2, float delta,
+template <int D>
+__device__ inline void dq_block(const float4 (&q)[D / 8], const float4 (&g)[D / 8], const float *kt, const float *vt, int j0, const Range &range, const Edge &edge, float scale2, float lse2, float delta,
                                 int lane, f32x16 (&acc)[D / 32])
 {
-    typedef Mat<T> M;
+    typedef Mat<float> M;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
     const int half = lane >> 5, col = lane & 31;
     f32x16 s = zeros16(), dp = zeros16();
@@ -49,19 +47,20 @@ __device__ inline void dq_block(const typename Mat<T>::F (&q)[D / Mat<T>::KF], c
     if (top_edge || bottom_edge) hide(s, edge, j0, half, top_edge, bottom_edge, 0.f);
 #pragma unroll
     for (int r = 0; r < M::GROUPS; ++r) {
-        const typename M::F ds = M::pack(s, r);
+        const float4 ds = M::pack(s, r);
 #pragma unroll
         for (int d = 0; d < DB; ++d) acc[d] = M::mma(M::column(kt, LD, d * 32, r, lane), ds, acc[d]);
     }
 }
 
-template <typename T, typename O, int D>
-__global__ void __launch_bounds__(kThreads, D > 64 ? 1 : sizeof(T) == 2 || D == 32 ? 3 : 2)
-window_dq_kernel(WindowArgs a)
+template <int D>
+__global__ void __launch_bounds__(kThreads, D > 64 ? 1 : D == 32 ? 3 : 2)
+window_dq_f32_kernel(WindowArgs a)
 {
+    typedef float T;
     typedef Mat<T> M;
-    typedef typename M::F F;
-    constexpr int KT = sizeof(T) == 2 ? 64 : 32, LD = D + M::PAD, DB = D / 32, NF = D / M::KF;
+    typedef float4 F;
+    constexpr int KT = 32, LD = D + M::PAD, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = KT / RPP;
     __shared__ __align__(16) T tile[2][2][KT * LD];
     __shared__ int infinite;                             // whether a key that was taken out of a tile was not finite
@@ -165,7 +164,7 @@ window_dq_kernel(WindowArgs a)
 #pragma unroll 1
         for (int b = 0; b < KT; b += 32)
             if (mine.some(j0 + b, j0 + b + 31))
-                dq_block<T, D>(q, g, kt + b * LD, vt + b * LD, j0 + b, mine, edge, scale2, lse2, delta, lane, acc);
+                dq_block<D>(q, g, kt + b * LD, vt + b * LD, j0 + b, mine, edge, scale2, lse2, delta, lane, acc);
         if (t + 1 < tiles) store(j1, (t + 1) & 1);
         __syncthreads();
         j0 = j1;
@@ -186,7 +185,7 @@ window_dq_kernel(WindowArgs a)
         }
     }
     if (iq >= a.n) return;
-    O *dq = (O *)a.dq + (int64_t)b * a.ldq.stride_b + (int64_t)iq * a.ldq.stride_n + (int64_t)h * a.ldq.stride_h;
+    float *dq = (float *)a.dq + (int64_t)b * a.ldq.stride_b + (int64_t)iq * a.ldq.stride_n + (int64_t)h * a.ldq.stride_h;
 #pragma unroll
     for (int d = 0; d < DB; ++d)
 #pragma unroll
@@ -434,20 +433,19 @@ window_sink_sum_kernel(WindowArgs a)
     store4(out, s.x * f, s.y * f, s.z * f, s.w * f);
 }
 
-// Few queries (fp32: or keys): too few workgroups of 128 to fill the chip's 256 units; a workgroup then has 32.  us, few and many: query
-// pass, d = 64, all of 2048 tokens seen: 96 workgroups 27 and 44, 144 43 and 47, 384 61 and 53; window 256: 96 12.6 and 15.6, 144 21 and 17; 256
-// tokens, window 32: 144 11.4 and 12.0, 256 14.9 and 12.8.  d = 128, window 256: 64 14 and 24, 96 26 and 25, 144 47 and 28.  Both passes in
-// fp32, window 128 of 256 tokens, 12 heads: batch 4 (96) 58 and 82, 8 (192) 96 and 85.
-bool few(int64_t heads, int64_t count, int d) { return heads * ((count + kTile - 1) / kTile) < (d == 128 ? 96 : 144); }
+// Few queries or keys: too few workgroups to fill the chip's 256 units; a workgroup then has 32 of them and its wavefronts share out the
+// walk.  us, few and many.  fp32, both passes, window 128 of 256 tokens, 12 heads: batch 4 (96 workgroups of 128) 58 and 82, 8 96 and 85;
+// d = 128, whose wavefronts fill a SIMD alone, by a smaller count.
+bool few_f32(int64_t heads, int64_t count, int d) { return heads * ((count + kTile - 1) / kTile) < (d == 128 ? 96 : 144); }
 
-// The same of keys in bf16, where a workgroup of 64 walks the `steps` tiles of 64 queries that see an ordinary key tile: one of 32, whose four
-// wavefronts share them out, pays where there are several.  us, few and many, d = 64, counted in 128 keys: 2048 tokens, all seen, 96 28 and
-// 51, 144 48 and 55, 384 69 and 60; window 256 (5 steps) 64 11.9 and 12.9, 96 15.0 and 13.3; window 32 (2) 48 8.2 and 8.2, 96 9.9
-// and 8.5.  d = 128, window 256: 64 17 and 20, 96 33 and 20; all seen 96 42 and 78, 144 95 and 87.
-bool few_keys(int64_t heads, int64_t m, int64_t steps)
-{
-    return heads * ((m + 127) / 128) < (steps < 4 ? 0 : steps < 16 ? 72 : 128);
-}
+// bf16, counted in 128 queries, by the walk's tiles of 64 keys too.  d = 64: 2048 tokens, all seen, 96 26 and 33, 144 43 and 36; window
+// 256 (5 tiles) 64 9.2 and 10.6, 96 13.0 and 11.4; window 32 64 6.8 and 8.0, 96 9.3 and 9.0.  d = 128, window 256: 64 14 and 16, 96 26 and
+// 16; all seen 96 37 and 50, 144 88 and 58.
+bool few_queries(int64_t heads, int64_t n, int64_t tiles) { return heads * ((n + 127) / 128) < (tiles < 16 ? 68 : 128); }
+
+// The same of keys: 2048 tokens, all seen, 96 28 and 51, 144 48 and 55; window 256 64 11.9 and 12.9, 96 15.0 and 13.3; window 32 (2 tiles) 48
+// 8.2 and 8.2, 96 9.9 and 8.5.  d = 128, window 256: 64 17 and 20, 96 33 and 20; all seen 96 42 and 78, 144 95 and 87.
+bool few_keys(int64_t heads, int64_t m, int64_t tiles) { return heads * ((m + 127) / 128) < (tiles < 4 ? 0 : tiles < 16 ? 72 : 128); }
 
 // The key pass' tiles, those with sinks, and the parts they are cut into.  In steps of 64 queries: an ordinary tile takes
 // (window + tile) / 64, one with sinks n / 64.  Uncut it ends last where it takes longer than an ordinary one and than half of what
@@ -461,7 +459,7 @@ Plan plan(int io_dtype, int64_t heads, int d, int n, int m, int window, int sink
     const int64_t sink = (n + 63) / 64;
     const auto ordinary_steps = [&](int tile) { const int64_t near = ((int64_t)window + tile + 63) / 64; return near < sink ? near : sink; };
     if (io_dtype == LASAD_BF16) r.tile = few_keys(heads, m, ordinary_steps(kWindowKeyTile)) ? 32 : kWindowKeyTile;
-    else r.tile = few(heads, m, d) ? 32 : kTile;
+    else r.tile = few_f32(heads, m, d) ? 32 : kTile;
     r.sink_tiles = (int)(((int64_t)(sinks < m ? sinks : m) + r.tile - 1) / r.tile);
     const int64_t all = ((int64_t)m + r.tile - 1) / r.tile, ordinary = ordinary_steps(r.tile);
     const int64_t slot = heads * ((all - r.sink_tiles) * ordinary + r.sink_tiles * sink) / (r.tile == kWindowKeyTile ? 1024 : 512);
@@ -495,13 +493,16 @@ hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
     a.key_tile = r.tile; a.sink_tiles = r.sink_tiles; a.sink_parts = r.parts;
     hipError_t e = hipSuccess;
     if (a.n > 0) {
-        if (few((int64_t)a.B * a.Hq, a.n, a.d)) {
+        const int64_t heads = (int64_t)a.B * a.Hq, seen = (int64_t)a.window + 64 < a.start_pos + a.n ? (int64_t)a.window + 64 : a.start_pos + a.n;
+        if (a.io_dtype == LASAD_BF16 ? few_queries(heads, a.n, (seen + 63) / 64) : few_f32(heads, a.n, a.d)) {
             e = launch_window_dq_few(a, s);
+        } else if (a.io_dtype == LASAD_BF16) {
+            e = launch_window_dq_bf16(a, s);
         } else {
             const dim3 grid(launch_grid((int64_t)a.B * a.Hq, (a.n + kTile - 1) / kTile));
-#define LASAD_WQ(T, O, D) window_dq_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
-            LASAD_WINDOW_DISPATCH(LASAD_WQ);
-#undef LASAD_WQ
+            if (a.d == 32) window_dq_f32_kernel<32><<<grid, dim3(kThreads), 0, s>>>(a);
+            else if (a.d == 64) window_dq_f32_kernel<64><<<grid, dim3(kThreads), 0, s>>>(a);
+            else window_dq_f32_kernel<128><<<grid, dim3(kThreads), 0, s>>>(a);
             e = hipGetLastError();
         }
         if (e != hipSuccess) return e;

@@ -25,18 +25,6 @@ __device__ inline float of_row(int x)
     return __int_as_float(__builtin_amdgcn_update_dpp(0, x, 0x150 + L, 0xf, 0xf, true));
 }
 
-// Which query and which channels a lane has is free, as long as both operands of a product agree, and goes by LDS, 64 banks.  Row
-// 4 quad + i of a product of 16 queries is query 4 i + first_row(quad) of them: lanes 0 .. 31 read eight rows by columns, eight dwords of
-// each, and even rows, like odd ones, lie 8 banks apart (36 dwords a row of 64 channels).  By rows, 16 bytes a lane, lanes 0-3, 12-15
-// and 20-27 read together, then 4-11, 16-19 and 28-31: with channels 32 apart in neighbouring quads the two share no bank (d >= 64).
-__device__ inline int first_row(int quad) { return 2 * (quad & 1) + (quad >> 1); }
-// first of a lane's eight channels in reduction step f
-template <int D>
-__device__ inline int channel(int f, int quad)
-{
-    return D == 32 ? 8 * quad : 32 * (quad & 1) + 8 * (quad >> 1) + 16 * (f & 1) + 64 * (f >> 1);
-}
-
 // One block of 32 queries (positions from pb on, rows of qt and gt, their -lse / scale and -delta) for a wavefront's 16 keys.
 template <int D>
 __device__ inline void dkv_block(const WindowArgs &a, const Frag (&k)[D / 32], const Frag (&v)[D / 32], const uint16_t *qt, const uint16_t *gt,
