@@ -37,6 +37,7 @@ SOURCES = [
     "lasad_api_attention.hip",
     "lasad_qk.hip",
     "lasad_window_forward.hip",
+    "lasad_window_forward_16.hip",
     "lasad_window_backward.hip",
     "lasad_window_backward_queries.hip",
     "lasad_window_backward_keys.hip",

@@ -47,6 +47,7 @@ struct WindowArgs {
     int key_tile, sink_tiles, sink_parts;              // plan of the backward's key pass: keys of a tile, tiles with sinks, parts of each
 };
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s);
+hipError_t launch_window_forward_16(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s);
 hipError_t launch_window_dq_few(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_dkv_few(const WindowArgs &a, hipStream_t s);

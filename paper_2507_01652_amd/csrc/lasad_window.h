@@ -78,10 +78,11 @@ template <> struct Mat<float> {
     static __device__ inline float dot(const F &a, const F &b) { return fmaf(a.x, b.x, fmaf(a.y, b.y, fmaf(a.z, b.z, a.w * b.w))); }
 };
 
-// The backward's products of 16 x 16 in bf16 (a quad is 16 lanes).  Which rows and which channels a lane has is free, as long as both
-// operands of a product agree, and goes by LDS, 64 banks.  Row 4 quad + i of a product of 16 queries (keys) is number 4 i + first_row(quad)
-// of them: lanes 0 .. 31 read eight rows by columns, eight dwords of each, and even rows, like odd ones, lie 8 banks apart (36 dwords a row of 64 channels).  By rows, 16 bytes a lane, lanes 0-3, 12-15
-// and 20-27 read together, then 4-11, 16-19 and 28-31: with channels 32 apart in neighbouring quads the two share no bank (d >= 64).
+// Products of 16 x 16 in bf16 (a quad is 16 lanes).  Which rows and which channels a lane has is free, as long as both operands of a
+// product agree, and goes by LDS, 64 banks.  Row 4 quad + i of a product of 16 queries (keys) is number 4 i + first_row(quad) of them: lanes
+// 0 .. 31 read eight rows by columns, eight dwords of each, and even rows, like odd ones, lie 8 banks apart (36 dwords a row of 64
+// channels).  By rows, 16 bytes a lane, lanes 0-3, 12-15 and 20-27 read together, then 4-11, 16-19 and 28-31: with channels 32 apart in
+// neighbouring quads the two share no bank (d >= 64).
 __device__ inline int first_row(int quad) { return 2 * (quad & 1) + (quad >> 1); }
 // first of a lane's eight channels in reduction step f
 template <int D>
@@ -91,6 +92,7 @@ __device__ inline int channel(int f, int quad)
 }
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.f;          // by how much (a power of two) a score may pass the forward's running maximum
 
 __device__ inline f32x16 zeros16()
 {

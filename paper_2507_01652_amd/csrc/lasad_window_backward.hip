@@ -29,8 +29,8 @@ constexpr int kThreads = 256, kTile = 128;               // queries (keys) of a 
 
 // One block of 32 keys (from j0 on, rows of kt and vt) for a wavefront's queries: dS, and its product with k.
 template <int D>
-__device__ inline void dq_block(const float4 (&q)[D / 8], const float4 (&g)[D / 8], const float *kt, const float *vt, int j0, const Range &range, const Edge &edge, float scale2, float lse2, float delta,
-                                int lane, f32x16 (&acc)[D / 32])
+__device__ inline void dq_block(const float4 (&q)[D / 8], const float4 (&g)[D / 8], const float *kt, const float *vt, int j0, const Range &range,
+                                const Edge &edge, float scale2, float lse2, float delta, int lane, f32x16 (&acc)[D / 32])
 {
     typedef Mat<float> M;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;

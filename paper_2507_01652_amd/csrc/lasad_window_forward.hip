@@ -22,7 +22,6 @@ namespace lasad {
 namespace {
 
 constexpr int kThreads = 256, kQueries = 128;
-constexpr float kSlack = 8.f;
 
 // One block of 32 keys (from j0 on, scores s, values in the rows of vt) for a wavefront's queries: exponentials, products with v.
 // Blocks are taken one after the other, not two at a time: with 16 scores a lane (and not 32) four wavefronts fit a SIMD, which hide
@@ -328,14 +327,22 @@ window_forward_few_kernel(WindowArgs a)
         a.lse[(int64_t)bh * a.n + iq] = total == 0.f ? -INFINITY : (top + log2f(total)) * kLn2;
 }
 
-// Few: too few workgroups of 128 queries to fill the chip's 256 units.  us, few and many, window 128 of 256 tokens, 12 heads: batch 1
-// 6.8 and 10.9, 8 (192 workgroups) 9.1 and 11.4, 16 (384) 14.9 and 12.2; 16 heads of 100 tokens, batch 16 (256) 9.0 and 8.3.  d = 128,
-// whose keys do not fit the registers twice: batch 1 10.4 and 15.5, 4 (96) 16.1 and 15.9, 16 47 and 20.  fp32, bound by its
-// matrix rate: batch 4 16.7 and 27.5, 16 (384) 38.7 and 37.4.
-bool few_queries(const WindowArgs &a)
+// Which kernel, by the number of workgroups that 128 queries each would make, heads counted in eights as they are dealt out.  Few: one
+// of 32, whose wavefronts share out the keys, fills the chip's 256 units sooner, and pays for longer where the walk over the keys is long.
+// us, few, 16 queries a wavefront, 32 and 128 a workgroup.  d = 64, window 256 of 2048 tokens: 96 workgroups 9.8 10.2 13.9, 256 16.1 13.1
+// 14.7, 384 20.6 16.0 18.4, 640 29 22.9 23.4, 1024 43 31 28; all seen: 256 30 36 41, 384 39 38 44, 1024 92 68 54; window 32 of 256: 192 8.1 8.8
+// 10.5, 256 10.4 9.1 10.6.  d = 32, window 256: 256 9.4 10.5 12.0, 384 13.0 12.5 14.3, 1024 24 22 21; all seen: 640 35 34 39.  d = 128, window
+// 256: 64 12.3 13.8 19.4, 96 22 14 20, 384 63 23 27, 4096 643 207 201; all seen: 96 29 46 60, 192 70 51 59.  fp32, bound by its matrix rate:
+// window 128 of 256 tokens, 12 heads, batch 4 (96) 16.7 and 27.5, 16 (384) 38.7 and 37.4.
+enum Kernel { FEW, MIDDLING, MANY };
+Kernel choose(const WindowArgs &a)
 {
-    const int64_t groups = (int64_t)a.B * a.Hq * ((a.n + kQueries - 1) / kQueries);
-    return groups < (a.io_dtype == LASAD_F32 ? 384 : a.d == 128 ? 96 : 256);
+    const int64_t heads = (int64_t)a.B * a.Hq, groups = (heads < 8 ? heads : (heads + 7) / 8 * 8) * ((a.n + kQueries - 1) / kQueries);
+    if (a.io_dtype == LASAD_F32) return groups < 384 ? FEW : MANY;
+    const int64_t last = (int64_t)a.start_pos + a.n, seen = (int64_t)a.window + 64 < last ? (int64_t)a.window + 64 : last;
+    const bool far = seen >= 1024;
+    const int few = a.d == 32 ? (far ? 640 : 384) : a.d == 64 ? (far ? 320 : 200) : (far ? 128 : 72);
+    return groups < few ? FEW : a.d == 128 || groups < 768 ? MIDDLING : MANY;
 }
 
 }  // namespace
@@ -344,16 +351,24 @@ hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s)
 {
     if (a.n == 0) return hipSuccess;
     const int64_t heads = (int64_t)a.B * a.Hq;
-    if (few_queries(a)) {
+    const Kernel kernel = choose(a);
+    if (kernel == FEW) {
         const dim3 grid(launch_grid(heads, (a.n + 31) / 32));
 #define LASAD_WF(T, O, D) window_forward_few_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
         LASAD_WINDOW_DISPATCH(LASAD_WF);
 #undef LASAD_WF
         return hipGetLastError();
     }
+    if (kernel == MIDDLING) return launch_window_forward_16(a, s);
     const dim3 grid(launch_grid(heads, (a.n + kQueries - 1) / kQueries));
 #define LASAD_WF(T, O, D) window_forward_kernel<T, O, D><<<grid, dim3(kThreads), 0, s>>>(a)
-    LASAD_WINDOW_DISPATCH(LASAD_WF);
+    if (a.io_dtype == LASAD_F32) {
+        if (a.d == 32) LASAD_WF(float, float, 32); else if (a.d == 64) LASAD_WF(float, float, 64); else LASAD_WF(float, float, 128);
+    } else if (a.out_dtype == LASAD_BF16) {
+        if (a.d == 32) LASAD_WF(uint16_t, uint16_t, 32); else LASAD_WF(uint16_t, uint16_t, 64);
+    } else {
+        if (a.d == 32) LASAD_WF(uint16_t, float, 32); else LASAD_WF(uint16_t, float, 64);
+    }
 #undef LASAD_WF
     return hipGetLastError();
 }
