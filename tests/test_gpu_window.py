@@ -44,6 +44,10 @@ CASES = [
 MANY = [(CASES[i], B, Hq, Hk) for i, B, Hq, Hk in ((0, 12, 16, 16), (1, 16, 12, 12), (2, 9, 32, 16), (3, 13, 16, 16), (6, 8, 32, 16), (7, 8, 32, 32),
                                                    (8, 16, 16, 8), (9, 8, 32, 16), (10, 16, 16, 16), (11, 32, 16, 8), (12, 32, 16, 16), (13, 10, 16, 16),
                                                    (14, 16, 32, 16), (15, 13, 16, 8), (16, 16, 32, 16), (17, 4, 12, 4), (18, 4, 24, 24))]
+# and enough for the forward's workgroups of 128 in bf16 (those above have 64)
+MANY += [(CASES[i], B, Hq, Hk) for i, B, Hq, Hk in ((0, 25, 16, 16), (1, 34, 12, 12), (2, 17, 16, 8), (4, 100, 16, 16), (5, 50, 16, 8), (6, 13, 32, 16), (7, 13, 32, 32),
+                                                   (8, 25, 16, 8), (9, 25, 16, 16), (10, 50, 16, 16), (11, 50, 16, 8), (12, 50, 16, 16), (13, 13, 32, 16),
+                                                   (17, 8, 12, 4))]
 IDS = [f"{str(c[0])[6:]}-{str(c[1])[6:]}-d{c[2]}-{c[3]}x{c[4]}-B{c[5]}-{c[6]}+{c[7]}of{c[8]}-w{c[9]}-s{c[10]}{'-lens' if c[11] else ''}" for c in CASES]
 
 
@@ -162,7 +166,7 @@ def test_views_heads_first_and_broadcast_inputs(lasad, dtype):
 
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
-@pytest.mark.parametrize("B", [2, 160])
+@pytest.mark.parametrize("B", [2, 160, 200])
 def test_what_is_not_seen_has_no_part(lasad, dtype, value, B):
     """Keys past a row's length, past the last query and before all windows hold `value`: nothing changes.  One key in the middle
     does: only its own queries change."""
