@@ -5,10 +5,10 @@
 // other's chains of products, exponentials and products.  Queries and d_o are then read from LDS twice as often, which has room for it once
 // no two lanes meet in a bank (`first_row`).
 //
-// Measured, bf16, d = 64: 512 heads of 576 tokens, window 144 78 us (32 keys a wavefront 104); 2 x 8 key heads, each shared by three, of
-// 4096 tokens, window 1024, 16 sinks 153 us, 600 TFLOP/s of the pairs that are seen (155), matrix cores busy for 30 % of the time, LDS
-// for 39, vector units for 43; d = 128, 60 x 6 key heads of 48 tokens 15 us (29).  Bank conflicts cost 3 to 5 %, eight wavefronts to a
-// workgroup (128 keys) 10 % in the first case.
+// Measured, bf16, d = 64: 512 heads of 576 tokens, window 144 75 us (32 keys a wavefront 104); 2 x 8 key heads, each shared by three, of
+// 4096 tokens, window 1024, 16 sinks 150 us, 610 TFLOP/s of the pairs that are seen (155), matrix cores busy for 30 % of the time, LDS
+// for 39, vector units for 43; d = 128, 60 x 6 key heads of 48 tokens 15 us (29).  Bank conflicts cost 3 to 5 %, a rolled loop over a
+// tile's blocks 3, eight wavefronts to a workgroup (128 keys) 10 % in the first case.
 #include "lasad_window.h"
 
 namespace lasad {
@@ -200,7 +200,7 @@ window_dkv_bf16_kernel(WindowArgs a)
         if (t + 1 < steps && ++ti == t_count) { ti = 0; ++hi; }
         load(ti, hi);                                    // (the last tile once more rather than a branch around loads in flight)
         const T *qt = tile[t & 1][0], *gt = tile[t & 1][1];
-#pragma unroll 1
+#pragma unroll
         for (int qb = 0; qb < QB; ++qb)
             if (!sees_none(a, keys, p0 + 32 * qb, p0 + 32 * qb + 31, w0, w1))
                 dkv_block<D>(a, k, v, qt + qb * 32 * LD, gt + qb * 32 * LD, stat[t & 1][0] + 32 * qb, stat[t & 1][1] + 32 * qb, p0 + 32 * qb,
