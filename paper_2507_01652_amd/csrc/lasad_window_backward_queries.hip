@@ -3,8 +3,8 @@
 // A wavefront has 16 queries and takes 32 keys at a time, in products of 16 x 16, as the key pass does and for the same reasons: four
 // wavefronts a SIMD instead of three, no two lanes in a bank, and 64 queries a workgroup, which leaves fewer units without one.
 //
-// Measured, bf16, d = 64: 512 heads of 576 tokens, window 144 70 us (32 queries a wavefront, 128 a workgroup: 75), 4.8 TB/s of what the
-// former reads and writes; 2 x 24 heads over 8 of 4096 tokens, window 1024, 16 sinks 105 us, 650 TFLOP/s of the pairs that are seen (104);
+// Measured, bf16, d = 64: 512 heads of 576 tokens, window 144 70 us (32 queries a wavefront, 128 a workgroup: 75): 424 MB, half of it
+// k and v again for the next tile, at 6.1 TB/s; all of a head's queries launched together 65, but 111 in the next; 2 x 24 heads over 8 of 4096 tokens, window 1024, 16 sinks 105 us, 650 TFLOP/s of the pairs that are seen (104);
 // 12 heads of 2048 tokens, window 256 14 us (18), d = 128 22 (29).
 #include "lasad_window.h"
 
