@@ -1,11 +1,11 @@
-// The backward of the window attention for few queries or keys (lasad_window_backward.hip has the formulas and the passes for many):
+// The backward of the window attention for few queries or keys (lasad_window_backward.hip has the formulas, the choice and what is for many):
 // a workgroup has 32 queries (keys) of one head, and its four wavefronts take the blocks of keys (queries) in turn, each with sums of
 // its own, which are added up at the end.  A block's rows go from memory to the first products' operands and, from the same registers,
 // to the wavefront's own LDS, whose columns the last products read; no barrier before the end.
 //
-// Bound by latency: a call is one chain of loads and products a wavefront.  Measured, bf16, d = 64, query and key pass, us: 24 heads of
-// 512 tokens, window 512: 12.2 and 12.8 (workgroups of 128: 16.4 and 19.3), 6 of 2048, all seen: 26 and 28 (44 and 52); fp32, 16 over 8 heads
-// of 229 tokens, bound by its matrix rate: 16 and 30.
+// Bound by latency: a call is one chain of loads and products a wavefront.  Measured, bf16, d = 64, query and key pass, us: 6 heads of 2048
+// tokens, all seen, 26 and 28 (workgroups of 64: 33 and 51), 4 heads, window 256, 9.2 and 11.9 (10.6 and 12.9); fp32, 16 over 8 heads of
+// 229 tokens, bound by its matrix rate: 16 and 30.
 #include "lasad_window.h"
 
 namespace lasad {
