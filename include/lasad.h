@@ -496,7 +496,7 @@ int lasad_forward_qk(const void *q, const void *k, void *q_out, void *k_out,
  *   dq_weight, dk_weight   fp32, laid out like the weights ([heads, d] or, shared, [d]; a NULL weight has the gradient at
  *                          ones); overwritten.  NULL: not formed.  Both must be NULL with norm_eps < 0.
  *   workspace              lasad_backward_qk_workspace_bytes(...) bytes, 16-byte aligned; needed (else LASAD_ERR_WORKSPACE) if a
- *                          weight gradient is wanted and n_tokens > 0.
+ *                          weight gradient is wanted and n_tokens > 0.  The query answers 0 for sizes that the call refuses.
  * The sums have a fixed order: results are deterministic.
  */
 size_t lasad_backward_qk_workspace_bytes(int B, int n_q_heads, int n_k_heads, int n_tokens, int d, int shared_weight);

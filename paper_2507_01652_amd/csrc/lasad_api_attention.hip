@@ -11,6 +11,13 @@ namespace {
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+// Whether check_sizes lets these through.  A size query answers 0 where the call would be refused: it is asked first.
+bool known_sizes(int B, int n_q_heads, int n_k_heads, int d, int64_t n_tokens)
+{
+    return B >= 1 && n_q_heads >= 1 && n_k_heads >= 1 && n_q_heads <= 65535 && n_k_heads <= 65535 && (d == 32 || d == 64 || d == 128) &&
+           n_tokens >= 0 && B * n_tokens <= 0x7fffffff;
+}
+
 // What all calls have: sizes and types.  (B * n_tokens rows of a launch are counted in 32 bits.)
 int check_sizes(int B, int n_q_heads, int n_k_heads, int d, int64_t n_tokens, int io_dtype, int out_dtype)
 {
@@ -170,7 +177,7 @@ int lasad_decode_step_qk(const void *q, const void *k, void *q_out, void *k_out,
 
 size_t lasad_backward_qk_workspace_bytes(int B, int n_q_heads, int n_k_heads, int n_tokens, int d, int shared_weight)
 {
-    if (B < 1 || n_q_heads < 1 || n_k_heads < 1 || n_tokens < 1 || d < 1) return 0;
+    if (!known_sizes(B, n_q_heads, n_k_heads, d, n_tokens) || n_tokens == 0) return 0;
     return lasad::qk_partial_bytes((int64_t)B * n_tokens, n_q_heads + n_k_heads, d, shared_weight != 0);
 }
 
