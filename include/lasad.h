@@ -455,6 +455,8 @@ int lasad_backward_layer_norm(const void *q_pre, const void *z, const void *v, c
 /*
  * The operators of a softmax layer between the linear-attention layers: norms and rotation of its query and key heads
  * (below), and attention with a window and sinks.
+ * A launch has fewer than 2^24 workgroups of 256 threads; calls that would need more are LASAD_ERR_UNSUPPORTED.  A workgroup has 32 to
+ * 128 queries (keys) of one head, a key head of one row of a step, 512 / d tokens of the norms' forward or 32 of their backward.
  *
  * Rotation of the d / 2 pairs of a head's channels by a token's raster position p = r * W + c (0-indexed):
  *   LASAD_ROPE_1D  pair i turns by p base^(-2i/d)

@@ -11,6 +11,11 @@ namespace {
 
 bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+// Calls with more workgroups than a launch may have are refused.
+int too_many() { return fail(LASAD_ERR_UNSUPPORTED, "B * heads * tokens overflows the launch grid"); }
+bool fits(int64_t heads, int64_t units) { return heads <= lasad::kMostGroups && heads * (units < 1 ? 1 : units) <= lasad::kMostGroups; }
+int check_groups(int64_t groups) { return groups > lasad::kMostGroups ? too_many() : LASAD_OK; }
+
 // Whether check_sizes lets these through.  A size query answers 0 where the call would be refused: it is asked first.
 bool known_sizes(int B, int n_q_heads, int n_k_heads, int d, int64_t n_tokens)
 {
@@ -107,6 +112,7 @@ int qk_forward(const void *q, const void *k, void *q_out, void *k_out,
     a.heads[0] = n_q_heads; a.heads[1] = n_k_heads;
     a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.B = B; a.n = n_tokens; a.d = d;
     a.start_pos = start_pos; a.pos_rows = pos_rows; a.shared = shared_weight != 0;
+    if (int rc = check_groups(lasad::qk_forward_groups((int64_t)B * n_tokens, d))) return rc;
     const hipError_t e = lasad::launch_qk_forward(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail(name, e);
     return LASAD_OK;
@@ -128,9 +134,8 @@ int check_window_sizes(int B, int n_q_heads, int n_k_heads, int d, int start_pos
     if (int rc = check_window(n_q_heads, n_k_heads, window, sinks, scale)) return rc;
     if (n_keys < 0 || start_pos < 0) return fail(LASAD_ERR_INVALID_ARG, "n_keys = %d, start_pos = %d", n_keys, start_pos);
     if ((int64_t)start_pos + n_tokens > 1 << 30 || n_keys > 1 << 30) return fail(LASAD_ERR_UNSUPPORTED, "positions beyond 2^30");
-    // (workgroups of 128 queries or keys; a key head's sink tiles have up to 64 each)
-    if (((int64_t)n_tokens / 128 + 9) * B * n_q_heads > 0x7fffffff || ((int64_t)n_keys / 128 + 9) * B * n_k_heads * 64 > 0x7fffffff)
-        return fail(LASAD_ERR_UNSUPPORTED, "B * heads * tokens overflows the launch grid");
+    // (no kernel has more than 128 queries or keys a workgroup; what is launched in fact is counted once it is known)
+    if (!fits((int64_t)B * n_q_heads, (n_tokens + 127) / 128) || !fits((int64_t)B * n_k_heads, (n_keys + 127) / 128)) return too_many();
     return LASAD_OK;
 }
 
@@ -227,6 +232,7 @@ int lasad_backward_qk(const void *q, const void *k, const void *d_q, const void 
     a.io_dtype = io_dtype; a.out_dtype = grad_dtype; a.B = B; a.n = n_tokens; a.d = d;
     a.start_pos = start_pos; a.shared = shared_weight != 0;
     a.dw[0] = dq_weight; a.dw[1] = dk_weight; a.partial = (float *)workspace;
+    if (int rc = check_groups(lasad::qk_backward_groups((int64_t)B * n_tokens))) return rc;
     const hipError_t e = lasad::launch_qk_backward(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_backward_qk launch", e);
     return LASAD_OK;
@@ -257,6 +263,7 @@ int lasad_forward_window(const void *q, const void *k, const void *v, void *o, f
                                       kv_lens, scale);
     a.o = o; a.lse = lse;
     a.lq = *q_layout; a.lk = *k_layout; a.lv = *v_layout; a.lo = *o_layout;
+    if (int rc = check_groups(lasad::window_forward_groups(a))) return rc;
     const hipError_t e = lasad::launch_window_forward(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_forward_window launch", e);
     return LASAD_OK;
@@ -316,6 +323,7 @@ int lasad_backward_window(const void *q, const void *k, const void *v, const voi
     a.dq = dq; a.dk = dk; a.dv = dv;
     a.lq = *q_layout; a.lk = *k_layout; a.lv = *v_layout; a.lo = *o_layout; a.ldo = *d_o_layout;
     a.ldq = *dq_layout; a.ldk = *dk_layout; a.ldv = *dv_layout;
+    if (int rc = check_groups(lasad::window_backward_groups(a))) return rc;
     const hipError_t e = lasad::launch_window_backward(a, workspace, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_backward_window launch", e);
     return LASAD_OK;
@@ -336,7 +344,7 @@ int lasad_decode_step_window(const void *q, const void *k, const void *v, void *
 {
     if (int rc = check_sizes(B, n_q_heads, n_k_heads, d, 1, io_dtype, out_dtype)) return rc;
     if (int rc = check_window(n_q_heads, n_k_heads, window, sinks, scale)) return rc;
-    if ((int64_t)B * n_q_heads > 0x7fffffff) return fail(LASAD_ERR_UNSUPPORTED, "B * n_q_heads overflows the launch grid");
+    if (!fits((int64_t)B * n_k_heads, 1) || (int64_t)B * n_q_heads > 0x7fffffff) return too_many();
     if (cache_tokens <= sinks) return fail(LASAD_ERR_INVALID_ARG, "a cache of %d rows has no room beside %d sinks", cache_tokens, sinks);
     if (!pos_rows && (pos < 0 || (pos >= cache_tokens && cache_tokens - sinks < window)))
         return fail(LASAD_ERR_INVALID_ARG, "pos %d does not fit a cache of %d rows (window %d, sinks %d)", pos, cache_tokens, window, sinks);

@@ -9,6 +9,10 @@ namespace lasad {
 int fail(int code, const char *fmt, ...);
 int hip_fail(const char *what, hipError_t e);
 
+// Workgroups of 256 threads that a launch may have: HIP takes fewer than 2^32 threads along an axis.  What a call would launch is
+// counted (the *_groups functions) before anything is.
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
+
 // Head norms and rotation; [0] queries, [1] keys.
 struct QkArgs {
     const void *x[2];
@@ -29,6 +33,8 @@ struct QkArgs {
 };
 hipError_t launch_qk_forward(const QkArgs &a, hipStream_t s);
 hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s);
+int64_t qk_forward_groups(int64_t tokens, int d);
+int64_t qk_backward_groups(int64_t tokens);
 size_t qk_partial_bytes(int64_t tokens, int heads, int d, int shared);
 
 // Attention with a window and sinks.  Key j is seen from position p if j <= p, j < length of the batch row, and
@@ -49,6 +55,8 @@ struct WindowArgs {
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_forward_16(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s);
+int64_t window_forward_groups(const WindowArgs &a);
+int64_t window_backward_groups(const WindowArgs &a);           // of the pass that has more
 hipError_t launch_window_dq_few(const WindowArgs &a, hipStream_t s);
 hipError_t launch_window_dkv_few(const WindowArgs &a, hipStream_t s);
 constexpr int kWindowKeyTile = 64;     // keys of a workgroup of launch_window_dkv_bf16

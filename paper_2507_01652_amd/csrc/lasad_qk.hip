@@ -213,14 +213,23 @@ qk_forward_kernel(QkArgs a, int tile)
 
 }  // namespace
 
+static int64_t forward_tile(int64_t total, int d)
+{
+    const int64_t tile = total / 1024, most = 512 / d;
+    return tile < 1 ? 1 : tile > most ? most : tile;
+}
+
+int64_t qk_forward_groups(int64_t tokens, int d)
+{
+    const int64_t tile = forward_tile(tokens, d);
+    return (tokens + tile - 1) / tile;
+}
+
 hipError_t launch_qk_forward(const QkArgs &a, hipStream_t s)
 {
-    const int64_t total = (int64_t)a.B * a.n;
+    const int64_t total = (int64_t)a.B * a.n, tile = forward_tile(total, a.d);
     if (total == 0) return hipSuccess;
-    const int max_tile = 512 / a.d;
-    int64_t tile = total / 1024;
-    tile = tile < 1 ? 1 : tile > max_tile ? max_tile : tile;
-    const dim3 grid((unsigned)((total + tile - 1) / tile)), block(kThreads);
+    const dim3 grid((unsigned)qk_forward_groups(total, a.d)), block(kThreads);
 #define LASAD_QK(I, O, D) qk_forward_kernel<I, O, D><<<grid, block, 0, s>>>(a, (int)tile)
 #define LASAD_QK_D(I, O) (a.d == 32 ? (void)(LASAD_QK(I, O, 32)) : a.d == 64 ? (void)(LASAD_QK(I, O, 64)) : (void)(LASAD_QK(I, O, 128)))
     if (a.io_dtype == LASAD_BF16) { if (a.out_dtype == LASAD_BF16) LASAD_QK_D(1, 1); else LASAD_QK_D(1, 0); }
@@ -380,16 +389,22 @@ static int head_share(int64_t groups, int heads, int d)
     return (int)((pieces + parts - 1) / parts) * rows;
 }
 
+int64_t qk_backward_groups(int64_t tokens)
+{
+    const int64_t tile = back_tile(tokens);
+    return (tokens + tile - 1) / tile;
+}
+
 size_t qk_partial_bytes(int64_t tokens, int heads, int d, int shared)
 {
-    const int64_t tile = back_tile(tokens), groups = (tokens + tile - 1) / tile;
+    const int64_t groups = qk_backward_groups(tokens);
     const int share = head_share(groups, heads, d);
     return (size_t)groups * (shared ? 2 * ((heads + share - 1) / share) : heads) * d * sizeof(float);
 }
 
 hipError_t launch_qk_backward(const QkArgs &a, hipStream_t s)
 {
-    const int64_t total = (int64_t)a.B * a.n, tile = back_tile(total), groups = (total + tile - 1) / tile;
+    const int64_t total = (int64_t)a.B * a.n, tile = back_tile(total), groups = qk_backward_groups(total);
     const bool want = a.norm && (a.dw[0] || a.dw[1]);
     const int heads = a.heads[0] + a.heads[1], share = head_share(groups, heads, a.d);
     QkArgs b = a;

@@ -255,7 +255,8 @@ __device__ inline Place launch_place(unsigned index, int heads, int units)
     const int head = (int)((index & 7) * each + slot % each);
     return {head < heads ? head : -1, (int)(slot / each)};
 }
-inline unsigned launch_grid(int64_t heads, int64_t units) { return (unsigned)(heads < 8 ? heads * units : (heads + 7) / 8 * 8 * units); }
+inline int64_t launch_groups(int64_t heads, int64_t units) { return heads < 8 ? heads * units : (heads + 7) / 8 * 8 * units; }
+inline unsigned launch_grid(int64_t heads, int64_t units) { return (unsigned)launch_groups(heads, units); }     // (kMostGroups at most)
 
 // Four consecutive results of a lane, as they leave the registers.
 template <typename O>

@@ -443,6 +443,12 @@ bool few_f32(int64_t heads, int64_t count, int d) { return heads * ((count + kTi
 // 16; all seen 96 37 and 50, 144 88 and 58.
 bool few_queries(int64_t heads, int64_t n, int64_t tiles) { return heads * ((n + 127) / 128) < (tiles < 16 ? 68 : 128); }
 
+bool few_query_pass(const WindowArgs &a)
+{
+    const int64_t heads = (int64_t)a.B * a.Hq, seen = (int64_t)a.window + 64 < a.start_pos + a.n ? (int64_t)a.window + 64 : a.start_pos + a.n;
+    return a.io_dtype == LASAD_BF16 ? few_queries(heads, a.n, (seen + 63) / 64) : few_f32(heads, a.n, a.d);
+}
+
 // The same of keys: 2048 tokens, all seen, 96 28 and 51, 144 48 and 55; window 256 64 11.9 and 12.9, 96 15.0 and 13.3; window 32 (2 tiles) 48
 // 8.2 and 8.2, 96 9.9 and 8.5.  d = 128, window 256: 64 17 and 20, 96 33 and 20; all seen 96 42 and 78, 144 95 and 87.
 bool few_keys(int64_t heads, int64_t m, int64_t tiles) { return heads * ((m + 127) / 128) < (tiles < 4 ? 0 : tiles < 16 ? 72 : 128); }
@@ -485,6 +491,15 @@ size_t window_backward_bytes(int B, int Hq, int Hk, int d, int n, int m, int win
     return delta_bytes(B, Hq, n) + parts;
 }
 
+int64_t window_backward_groups(const WindowArgs &a)
+{
+    const Plan r = plan(a.io_dtype, (int64_t)a.B * a.Hk, a.d, a.n, a.m, a.window, a.sinks);
+    const int64_t heads = (int64_t)a.B * a.Hq, queries = few_query_pass(a) ? 32 : a.io_dtype == LASAD_BF16 ? 64 : kTile;
+    const int64_t q = launch_groups(heads, (a.n + queries - 1) / queries);
+    const int64_t k = launch_groups((int64_t)a.B * a.Hk, (int64_t)r.sink_tiles * r.parts + (a.m + r.tile - 1) / r.tile - r.sink_tiles);
+    return q > k ? q : k;
+}
+
 hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
 {
     a.delta = (float *)workspace;
@@ -493,8 +508,7 @@ hipError_t launch_window_backward(WindowArgs &a, void *workspace, hipStream_t s)
     a.key_tile = r.tile; a.sink_tiles = r.sink_tiles; a.sink_parts = r.parts;
     hipError_t e = hipSuccess;
     if (a.n > 0) {
-        const int64_t heads = (int64_t)a.B * a.Hq, seen = (int64_t)a.window + 64 < a.start_pos + a.n ? (int64_t)a.window + 64 : a.start_pos + a.n;
-        if (a.io_dtype == LASAD_BF16 ? few_queries(heads, a.n, (seen + 63) / 64) : few_f32(heads, a.n, a.d)) {
+        if (few_query_pass(a)) {
             e = launch_window_dq_few(a, s);
         } else if (a.io_dtype == LASAD_BF16) {
             e = launch_window_dq_bf16(a, s);

@@ -347,6 +347,13 @@ Kernel choose(const WindowArgs &a)
 
 }  // namespace
 
+int64_t window_forward_groups(const WindowArgs &a)
+{
+    const Kernel kernel = choose(a);
+    const int64_t queries = kernel == FEW ? 32 : kernel == MIDDLING ? 64 : kQueries;
+    return launch_groups((int64_t)a.B * a.Hq, (a.n + queries - 1) / queries);
+}
+
 hipError_t launch_window_forward(const WindowArgs &a, hipStream_t s)
 {
     if (a.n == 0) return hipSuccess;
