@@ -560,6 +560,7 @@ int lasad_forward_window(const void *q, const void *k, const void *v, void *o, f
  *   dq, dk, dv       like q, k, v, type grad_dtype (fp32, or bf16 with bf16 inputs), strides of their own; overwritten
  *                    (keys that nobody sees: 0); must not overlap the inputs or each other.
  *   workspace        lasad_backward_window_workspace_bytes(...) bytes, 16-byte aligned; required (else LASAD_ERR_WORKSPACE).
+ *                    The query answers 0 for sizes that the call refuses.
  * The sums have a fixed order: results are deterministic.
  */
 size_t lasad_backward_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int n_keys,
@@ -587,7 +588,7 @@ int lasad_backward_window(const void *q, const void *k, const void *v, const voi
  *                     (its output and its cache are not written).  NULL: pos for all.
  *   workspace         lasad_decode_step_window_workspace_bytes(...) bytes, 16-byte aligned: few heads with many keys are
  *                     then dealt out over several workgroups.  NULL: they are not (same results up to rounding); a smaller
- *                     one is LASAD_ERR_WORKSPACE.
+ *                     one is LASAD_ERR_WORKSPACE.  The query answers 0 for sizes that the call refuses.
  */
 size_t lasad_decode_step_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int cache_tokens, int window,
                                                 int sinks);

@@ -118,6 +118,12 @@ int qk_forward(const void *q, const void *k, void *q_out, void *k_out,
     return LASAD_OK;
 }
 
+// No kernel has more than 128 queries or keys a workgroup; what is launched in fact is counted once it is known.
+bool fit(int B, int n_q_heads, int n_k_heads, int n_tokens, int n_keys)
+{
+    return fits((int64_t)B * n_q_heads, (n_tokens + 127) / 128) && fits((int64_t)B * n_k_heads, (n_keys + 127) / 128);
+}
+
 int check_window(int n_q_heads, int n_k_heads, int window, int sinks, float scale)
 {
     if (n_q_heads % n_k_heads) return fail(LASAD_ERR_INVALID_ARG, "%d query heads cannot share %d key heads evenly", n_q_heads, n_k_heads);
@@ -134,8 +140,7 @@ int check_window_sizes(int B, int n_q_heads, int n_k_heads, int d, int start_pos
     if (int rc = check_window(n_q_heads, n_k_heads, window, sinks, scale)) return rc;
     if (n_keys < 0 || start_pos < 0) return fail(LASAD_ERR_INVALID_ARG, "n_keys = %d, start_pos = %d", n_keys, start_pos);
     if ((int64_t)start_pos + n_tokens > 1 << 30 || n_keys > 1 << 30) return fail(LASAD_ERR_UNSUPPORTED, "positions beyond 2^30");
-    // (no kernel has more than 128 queries or keys a workgroup; what is launched in fact is counted once it is known)
-    if (!fits((int64_t)B * n_q_heads, (n_tokens + 127) / 128) || !fits((int64_t)B * n_k_heads, (n_keys + 127) / 128)) return too_many();
+    if (!fit(B, n_q_heads, n_k_heads, n_tokens, n_keys)) return too_many();
     return LASAD_OK;
 }
 
@@ -272,7 +277,8 @@ int lasad_forward_window(const void *q, const void *k, const void *v, void *o, f
 size_t lasad_backward_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int n_keys,
                                              int window, int sinks)
 {
-    if (B < 1 || n_q_heads < 1 || n_k_heads < 1 || d < 1 || n_tokens < 1 || n_keys < 0 || window < 1 || sinks < 0) return 0;
+    if (!known_sizes(B, n_q_heads, n_k_heads, d, n_tokens) || n_q_heads % n_k_heads || n_tokens < 1 || n_tokens > 1 << 30 || n_keys < 0 ||
+        n_keys > 1 << 30 || window < 1 || sinks < 0 || !fit(B, n_q_heads, n_k_heads, n_tokens, n_keys)) return 0;
     return lasad::window_backward_bytes(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks);
 }
 
@@ -332,7 +338,8 @@ int lasad_backward_window(const void *q, const void *k, const void *v, const voi
 size_t lasad_decode_step_window_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int cache_tokens, int window,
                                                 int sinks)
 {
-    if (B < 1 || n_q_heads < 1 || n_k_heads < 1 || d < 1 || cache_tokens < 1 || window < 1 || sinks < 0) return 0;
+    if (!known_sizes(B, n_q_heads, n_k_heads, d, 1) || n_q_heads % n_k_heads || window < 1 || sinks < 0 || cache_tokens <= sinks ||
+        !fits((int64_t)B * n_k_heads, 1)) return 0;
     const int64_t seen = (int64_t)window + sinks < cache_tokens ? (int64_t)window + sinks : cache_tokens;
     return lasad::window_step_bytes(B, n_q_heads, d, lasad::window_step_splits(B, n_k_heads, seen));
 }

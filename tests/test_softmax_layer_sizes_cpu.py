@@ -30,6 +30,22 @@ def test_the_head_norms_backward_with_a_wide_head(d):
         binding.lasad_backward_qk(q, k, q, k, 3, 3)
 
 
+@pytest.mark.parametrize("sizes", [
+    (2, 4, 2, 48, 9, 9, 4, 1), (2, 4, 2, 0, 9, 9, 4, 1), (0, 4, 2, 64, 9, 9, 4, 1), (2, 3, 2, 64, 9, 9, 4, 1), (2, 4, 2, 64, 0, 9, 4, 1),
+    (2, 4, 2, 64, 9, -1, 4, 1), (2, 4, 2, 64, 9, 9, 0, 1), (2, 4, 2, 64, 9, 9, 4, -1), (1, 4, 2, 64, (1 << 30) + 1, 9, 4, 1),
+    (1, 4, 2, 64, 9, (1 << 30) + 1, 4, 1), (1 << 24, 1, 1, 64, 1, 1, 4, 1), (MOST, MOST, MOST, MOST, MOST, MOST, MOST, MOST),
+    # (heads x tiles with sinks: 2^64, which is 0 in 64 bits)
+    (1 << 30, 1 << 30, 1 << 30, 64, 4, 1024, 4, 1024), (1 << 20, 1 << 16, 1 << 20, 64, 2, MOST, 512, MOST)])
+def test_the_window_attention_query_for_sizes_that_are_refused(sizes):
+    assert binding.lasad_backward_window_workspace_bytes(*sizes) == 0
+
+
+@pytest.mark.parametrize("sizes", [(1, 4, 2, 48, 9000, 8000, 4), (1, 4, 3, 64, 9000, 8000, 4), (0, 4, 2, 64, 9000, 8000, 4), (1, 4, 2, 64, 9000, 0, 4),
+                                   (1, 4, 2, 64, 9000, 8000, -1), (1, 4, 2, 64, 4000, 8000, 4000), (1, MOST, MOST, 64, 9000, 8000, 4)])
+def test_the_step_query_for_sizes_that_are_refused(sizes):
+    assert binding.lasad_decode_step_window_workspace_bytes(*sizes) == 0
+
+
 by, L = ctypes.byref, binding.Layout
 
 
