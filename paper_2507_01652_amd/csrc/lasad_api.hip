@@ -505,14 +505,14 @@ int lasad_backward_chunked_carried(const void *q, const void *k, const void *v, 
 
 size_t lasad_backward_gated_workspace_bytes(int B, int n_heads, int n_tokens, int d)
 {
-    if (B < 1 || n_heads < 1 || n_tokens < 1 || d < 1) return 0;
+    if (B < 1 || n_heads < 1 || n_tokens < 1 || n_tokens > 1 << 30 || d < 1) return 0;      // (a grid has 2^30 tokens at most)
     return lasad::backward_gated_workspace_bytes((int64_t)B * n_heads, n_tokens, d) +
            lasad::backward_gated_bounds_bytes((int64_t)B * n_heads, n_tokens, d);
 }
 
 size_t lasad_backward_gated_carried_workspace_bytes(int B, int n_heads, int n_tokens, int d)
 {
-    if (B < 1 || n_heads < 1 || n_tokens < 1 || d < 1) return 0;
+    if (B < 1 || n_heads < 1 || n_tokens < 1 || n_tokens > 1 << 30 || d < 1) return 0;      // (a grid has 2^30 tokens at most)
     return lasad_backward_gated_workspace_bytes(B, n_heads, n_tokens, d) +
            lasad::backward_gated_carried_extra_bytes((int64_t)B * n_heads, d);
 }
@@ -633,7 +633,7 @@ static bool bad_strides(const lasad_layout_t *l, int vec)
 size_t lasad_backward_layer_workspace_bytes(int B, int n_heads, int n_tokens, int d, int io_dtype,
                                             const lasad_layout_t *in_layout)
 {
-    if (B < 1 || n_heads < 1 || n_tokens < 1 || d < 1 || !in_layout) return 0;
+    if (B < 1 || n_heads < 1 || n_tokens < 1 || n_tokens > 1 << 30 || d < 1 || !in_layout) return 0;
     if (in_layout->stride_b < 0 || in_layout->stride_n < 0 || in_layout->stride_h < 0) return 0;
     return lasad::backward_layer_workspace_bytes(B, n_heads, n_tokens, d, io_dtype, *in_layout);
 }
