@@ -9,8 +9,10 @@
 // Key pass: a workgroup has keys of one head and walks the tiles of the queries that see any of them,
 // head after head of the group.  Ordinary keys are seen from `window` positions on, the sinks from all later ones: their
 // tiles are cut into parts of about an ordinary tile's work, whose sums a small kernel adds up in their order.
-// In the key pass -lse / scale and -delta are what the sums of the first two products start from, so that an entry costs a product and
-// an exponential for P and one more product for dS.
+// In the key pass -delta is what the sums of the second product start from, and in bf16 -lse / scale those of the first, so that an entry
+// costs a product and an exponential for P and one more product for dS.  A sum that starts there is carried, and rounded, at the size of
+// lse / scale, 44 for lse 5.5 and d = 64, where the scores' own is about 8: nothing beside bf16's operands (2^-8), but in fp32 twice the
+// error of dk and dv (256 keys, emulated: 7.4e-7 and 3.8e-7).  There it starts from 0 and lse enters the multiply-add before the exponential.
 // P and dS are rounded to the storage type as operands (bf16: half a step of 2^-8); all sums are fp32.  delta is formed from o as it
 // was stored.  In the root mean square (16 heads of 576 tokens, window 144, unit variances) storing dq costs 1.7e-3 of it, the rounding
 // of dS 1.7e-3, o's 0.7e-3, together 2.5e-3; dS as two operands would take the second part and cost a quarter to a third more products.
@@ -194,22 +196,21 @@ window_dq_f32_kernel(WindowArgs a)
                    acc[d][4 * r + 3] * a.scale);
 }
 
-// One block of 32 queries (positions from pb on, rows of qt and gt, their -lse / scale and -delta) for a wavefront's keys: P and dS, and
-// their products with d_o and q.
+// One block of 32 queries (positions from pb on, rows of qt and gt, their lse (in powers of two) and -delta) for a wavefront's keys: P and
+// dS, and their products with d_o and q.
 template <int D>
 __device__ inline void dkv_block(const WindowArgs &a, const float4 (&k)[D / 8], const float4 (&v)[D / 8],
-                                 const float *qt, const float *gt, const float *shift, const float *delta, int pb, int keys, int w0, const Edge &edge,
+                                 const float *qt, const float *gt, const float *lse2, const float *delta, int pb, int keys, int w0, const Edge &edge,
                                  float scale2, int lane, f32x16 (&dk)[D / 32], f32x16 (&dv)[D / 32])
 {
     typedef Mat<float> M;
     typedef typename M::F F;
     constexpr int LD = D + M::PAD, NF = D / M::KF, DB = D / 32;
     const int half = lane >> 5, col = lane & 31;
-    f32x16 s, dp;
+    f32x16 s = zeros16(), dp;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-        const float4 x = *(const float4 *)(shift + 8 * r + 4 * half), y = *(const float4 *)(delta + 8 * r + 4 * half);
-        s[4 * r] = x.x; s[4 * r + 1] = x.y; s[4 * r + 2] = x.z; s[4 * r + 3] = x.w;
+        const float4 y = *(const float4 *)(delta + 8 * r + 4 * half);
         dp[4 * r] = y.x; dp[4 * r + 1] = y.y; dp[4 * r + 2] = y.z; dp[4 * r + 3] = y.w;
     }
 #pragma unroll
@@ -218,9 +219,14 @@ __device__ inline void dkv_block(const WindowArgs &a, const float4 (&k)[D / 8], 
         dp = M::mma(M::row(gt + col * LD, f, half), v[f], dp);
     }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(s[i] * scale2);
-        dp[i] *= s[i];
+    for (int r = 0; r < 4; ++r) {
+        const float4 x = *(const float4 *)(lse2 + 8 * r + 4 * half);
+        const float l[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s[4 * r + i] = __builtin_amdgcn_exp2f(fmaf(s[4 * r + i], scale2, -l[i]));
+            dp[4 * r + i] *= s[4 * r + i];
+        }
     }
     const bool first_edge = pb < w0 + 31 || w0 + 31 >= keys, last_edge = pb + 31 - w0 >= a.window;
     if (first_edge || last_edge) {
@@ -249,7 +255,7 @@ window_dkv_f32_kernel(WindowArgs a)
     constexpr int QT = 32, LD = D + M::PAD, QB = QT / 32, DB = D / 32, NF = D / M::KF;
     constexpr int PPR = D / M::VEC, RPP = kThreads / PPR, N = QT / RPP;
     __shared__ __align__(16) T tile[2][2][QT * LD];
-    __shared__ __align__(16) float stat[2][2][QT];       // -lse / scale and -delta of a tile's queries
+    __shared__ __align__(16) float stat[2][2][QT];       // lse (in powers of two) and -delta of a tile's queries
     __shared__ int infinite;                             // whether a row that was taken out of a tile was not finite
 
     const int kt = (a.m + kTile - 1) / kTile;
@@ -280,7 +286,7 @@ window_dkv_f32_kernel(WindowArgs a)
     f32x16 dk[DB], dv[DB];
 #pragma unroll
     for (int d = 0; d < DB; ++d) dk[d] = dv[d] = zeros16();
-    const float scale2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
+    const float scale2 = a.scale * kLog2e;
     const Edge edge = key_edge(a, keys, jk);
 
     // queries that see any key of the tile, in tiles of QT counted from the first query; this part's share of them
@@ -343,7 +349,7 @@ window_dkv_f32_kernel(WindowArgs a)
             *(uint4 *)(tile[buf][0] + (row0 + i * RPP) * LD + col0) = qr[i];
             *(uint4 *)(tile[buf][1] + (row0 + i * RPP) * LD + col0) = gr[i];
         }
-        if (threadIdx.x < 2 * QT) stat[buf][threadIdx.x / QT][threadIdx.x % QT] = threadIdx.x < QT ? -sr * inv_scale : -sr;
+        if (threadIdx.x < 2 * QT) stat[buf][threadIdx.x / QT][threadIdx.x % QT] = threadIdx.x < QT ? sr * kLog2e : -sr;
     };
     if (threadIdx.x == 0) infinite = 0;
     if (steps > 0) load(0, 0);

@@ -181,7 +181,8 @@ window_dkv_few_kernel(WindowArgs a)
     const int j0 = kti * 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int jk = j0 + col, keys = min(valid_keys(a, b), a.start_pos + a.n);
-    const float scale2 = a.scale * kLog2e, inv_scale = 1.0f / a.scale;
+    // (what lse is in the place where it enters: fp32 the exponential's multiply-add, bf16 the sums that the scores start from)
+    const float scale2 = a.scale * kLog2e, lse_unit = sizeof(T) == 4 ? kLog2e : -1.0f / a.scale;
     const Edge edge = key_edge(a, keys, jk);
 
     // blocks of 32 queries that see any of the keys, and this part's share of them
@@ -242,27 +243,39 @@ window_dkv_few_kernel(WindowArgs a)
             if (bad) infinite = 1;
             if (behind) sr = half ? 0.f : INFINITY;
         }
-        stat[wave][half][col] = half ? -sr : -sr * inv_scale;
+        stat[wave][half][col] = half ? -sr : sr * lse_unit;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             *(uint4 *)(qt + col * LD + f * M::KF + M::VEC * half) = __builtin_bit_cast(uint4, qr[f]);
             *(uint4 *)(gt + col * LD + f * M::KF + M::VEC * half) = __builtin_bit_cast(uint4, gr[f]);
         }
         wave_lds_order();
-        f32x16 s, dp;
+        f32x16 s = zeros16(), dp;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const float4 x = *(const float4 *)(stat[wave][0] + 8 * r + 4 * half), y = *(const float4 *)(stat[wave][1] + 8 * r + 4 * half);
-            s[4 * r] = x.x; s[4 * r + 1] = x.y; s[4 * r + 2] = x.z; s[4 * r + 3] = x.w;
+            const float4 y = *(const float4 *)(stat[wave][1] + 8 * r + 4 * half);
             dp[4 * r] = y.x; dp[4 * r + 1] = y.y; dp[4 * r + 2] = y.z; dp[4 * r + 3] = y.w;
+            if constexpr (sizeof(T) == 2) {
+                const float4 x = *(const float4 *)(stat[wave][0] + 8 * r + 4 * half);
+                s[4 * r] = x.x; s[4 * r + 1] = x.y; s[4 * r + 2] = x.z; s[4 * r + 3] = x.w;
+            }
         }
 #pragma unroll
         for (int f = 0; f < NF; ++f) { s = M::mma(qr[f], k[f], s); dp = M::mma(gr[f], v[f], dp); }
         if (t + W < steps) load(t + W);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i] = __builtin_amdgcn_exp2f(s[i] * scale2);
-            dp[i] *= s[i];
+        for (int r = 0; r < 4; ++r) {
+            float lse2[4] = {};
+            if constexpr (sizeof(T) == 4) {
+                const float4 x = *(const float4 *)(stat[wave][0] + 8 * r + 4 * half);
+                lse2[0] = x.x; lse2[1] = x.y; lse2[2] = x.z; lse2[3] = x.w;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = s[4 * r + i];
+                s[4 * r + i] = __builtin_amdgcn_exp2f(sizeof(T) == 4 ? fmaf(x, scale2, -lse2[i]) : x * scale2);
+                dp[4 * r + i] *= s[4 * r + i];
+            }
         }
         const bool first_edge = pb < j0 + 31 || j0 + 31 >= keys, last_edge = pb + 31 - j0 >= a.window;
         if (first_edge || last_edge) {
