@@ -178,6 +178,12 @@ window_step_kernel(WindowStepArgs a)
                 l[g] += x[u][g];
             }
         }
+        // (lanes behind the last key hold that key's value once more; their weight is 0, and 0 times an infinity would be NaN)
+        if (base + UNROLL * TPW > t1) {
+#pragma unroll
+            for (int u = 0; u < UNROLL; ++u)
+                if (base + u * TPW + slot >= t1) vw[u] = make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             float vf[VEC];
