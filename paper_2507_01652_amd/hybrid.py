@@ -15,6 +15,7 @@ import argparse
 
 import torch
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 from . import binding as lasad
 
@@ -29,6 +30,7 @@ class _HeadNorms(torch.autograd.Function):
         return lasad.lasad_forward_qk(q, k, *grid, q_weight, k_weight)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_q, d_k):
         q, k, q_weight, k_weight = ctx.saved_tensors
         return (*lasad.lasad_backward_qk(q, k, d_q, d_k, *ctx.grid, q_weight, k_weight), None)
@@ -43,6 +45,7 @@ class _Window(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_o):
         return (*lasad.lasad_backward_window(*ctx.saved_tensors, d_o.contiguous(), ctx.window, ctx.sinks), None, None)
 
@@ -55,6 +58,7 @@ class _Linear(torch.autograd.Function):
         return lasad.lasad_forward_layer(q_pre, z, v, *grid, norm_weight=weight)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_o):
         q_pre, z, v, weight = ctx.saved_tensors
         return (*lasad.lasad_backward_layer(q_pre, z, v, d_o.contiguous(), *ctx.grid, norm_weight=weight), None)
