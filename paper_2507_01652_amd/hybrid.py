@@ -64,14 +64,21 @@ class _Linear(torch.autograd.Function):
         return (*lasad.lasad_backward_layer(q_pre, z, v, d_o.contiguous(), *ctx.grid, norm_weight=weight), None)
 
 
+def _count_heads(width: int) -> int:
+    if width < HEAD or width % HEAD:
+        raise ValueError(f"a width of {width} is not a number of heads of {HEAD} channels")
+    return width // HEAD
+
+
 class SoftmaxLayer(torch.nn.Module):
-    """Heads of `width`, a key head for every `group` of them; sees `window` positions back and the first `sinks`."""
+    """Heads of `width`, a key head for every `group` of them (more, where that does not divide them); sees `window` positions back and
+    the first `sinks`."""
 
     def __init__(self, width: int, grid: tuple, window: int, sinks: int = 1, group: int = 2):
         super().__init__()
         self.grid, self.window, self.sinks = grid, window, sinks
-        self.hq = width // HEAD
-        self.hk = max(1, self.hq // group)
+        self.hq = _count_heads(width)
+        self.hk = max(h for h in range(1, max(1, self.hq // group) + 1) if self.hq % h == 0)
         self.project = torch.nn.Linear(width, (self.hq + 2 * self.hk) * HEAD, bias=False)
         self.out = torch.nn.Linear(width, width, bias=False)
         self.q_weight = torch.nn.Parameter(torch.ones(HEAD))
@@ -97,7 +104,7 @@ class SoftmaxLayer(torch.nn.Module):
 class LinearLayer(torch.nn.Module):
     def __init__(self, width: int, grid: tuple):
         super().__init__()
-        self.grid, self.heads = grid, width // HEAD
+        self.grid, self.heads = grid, _count_heads(width)
         self.project = torch.nn.Linear(width, 3 * width, bias=False)
         self.out = torch.nn.Linear(width, width, bias=False)
         self.o_weight = torch.nn.Parameter(torch.ones(self.heads, HEAD))

@@ -33,3 +33,18 @@ def test_a_second_derivative_is_refused(plain, function):
     g, = torch.autograd.grad(loss, x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.sum().backward()
+
+
+@pytest.mark.parametrize("width,group,heads,key_heads", [(256, 2, 4, 2), (320, 2, 5, 1), (384, 2, 6, 3), (384, 4, 6, 1), (576, 4, 9, 1), (576, 2, 9, 3),
+                                                         (640, 4, 10, 2), (64, 2, 1, 1), (256, 8, 4, 1)])
+def test_key_heads_divide_the_heads(width, group, heads, key_heads):
+    layer = hybrid.SoftmaxLayer(width, (4, 4), 5, group=group)
+    assert (layer.hq, layer.hk) == (heads, key_heads)
+    assert layer.project.out_features == (heads + 2 * key_heads) * hybrid.HEAD
+
+
+@pytest.mark.parametrize("width", (0, 32, 100, 250))
+def test_a_width_that_is_no_number_of_heads(width):
+    for make in (lambda: hybrid.SoftmaxLayer(width, (4, 4), 5), lambda: hybrid.LinearLayer(width, (4, 4))):
+        with pytest.raises(ValueError, match="heads of 64"):
+            make()
