@@ -540,7 +540,7 @@ int lasad_decode_step_qk(const void *q, const void *k, void *q_out, void *k_out,
  *   lse       [B, n_q_heads, n_tokens] fp32 or NULL.
  *   window    >= 1 (2^31 - 1: all keys up to the query's);  sinks >= 0.
  *   kv_lens   int32 [B], device: valid keys of each batch row (clamped to 0 .. n_keys); NULL: n_keys.
- *   scale     > 0 and finite.
+ *   scale     > 0, at most 2^127.
  *   d         32, 64 or 128.  Pointers 16-byte aligned, strides multiples of 8 elements (fp32: 4).
  * start_pos + n_tokens and n_keys are at most 2^30; either count may be 0.  Sums are fp32; with bf16 inputs P (and in the
  * backward dS) is rounded to bf16 as a matrix-core operand.
@@ -559,6 +559,7 @@ int lasad_forward_window(const void *q, const void *k, const void *v, void *o, f
  *   d_o              like o, strides of its own.
  *   dq, dk, dv       like q, k, v, type grad_dtype (fp32, or bf16 with bf16 inputs), strides of their own; overwritten
  *                    (keys that nobody sees: 0); must not overlap the inputs or each other.
+ *   scale            as in the forward; with bf16 inputs at least 2^-120.
  *   workspace        lasad_backward_window_workspace_bytes(...) bytes, 16-byte aligned; required (else LASAD_ERR_WORKSPACE).
  *                    The query answers 0 for sizes that the call refuses.
  * The sums have a fixed order: results are deterministic.

@@ -129,6 +129,7 @@ int check_window(int n_q_heads, int n_k_heads, int window, int sinks, float scal
     if (n_q_heads % n_k_heads) return fail(LASAD_ERR_INVALID_ARG, "%d query heads cannot share %d key heads evenly", n_q_heads, n_k_heads);
     if (window < 1 || sinks < 0) return fail(LASAD_ERR_INVALID_ARG, "window = %d, sinks = %d", window, sinks);
     if (!(scale > 0.f && scale < INFINITY)) return fail(LASAD_ERR_INVALID_ARG, "scale must be positive and finite");
+    if (scale > 0x1p127f) return fail(LASAD_ERR_UNSUPPORTED, "scale beyond 2^127");       // (times log2 e it would pass fp32)
     return LASAD_OK;
 }
 
@@ -293,6 +294,8 @@ int lasad_backward_window(const void *q, const void *k, const void *v, const voi
                           void *workspace, size_t workspace_bytes, void *hip_stream)
 {
     if (int rc = check_window_sizes(B, n_q_heads, n_k_heads, d, start_pos, n_tokens, n_keys, window, sinks, scale, io_dtype, grad_dtype)) return rc;
+    // (the bf16 kernels' scores start from -lse / scale: the logarithm of 2^30 keys over 2^-120 is 2^124.4)
+    if (io_dtype == LASAD_BF16 && scale < 0x1p-120f) return fail(LASAD_ERR_UNSUPPORTED, "scale below 2^-120 with bf16 inputs");
     const struct { const char *name; const lasad_layout_t *l; bool out, key; } layouts[] = {
         {"q", q_layout, false, false}, {"k", k_layout, false, true}, {"v", v_layout, false, true}, {"o", o_layout, false, false},
         {"d_o", d_o_layout, false, false}, {"dq", dq_layout, true, false}, {"dk", dk_layout, true, true}, {"dv", dv_layout, true, true}};

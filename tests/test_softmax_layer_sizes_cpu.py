@@ -94,3 +94,22 @@ def _step_window(B, Hq=1, Hk=1, d=64):
 def test_more_workgroups_than_a_launch_has(call, sizes):
     assert call(*sizes) == binding.ERR_UNSUPPORTED
     assert b"launch grid" in binding.load().lasad_last_error()
+
+
+def _scaled(call, scale, io):
+    q, k = L(4 * 4 * 64, 4 * 64, 64), L(4 * 2 * 64, 2 * 64, 64)
+    lib = binding.load()
+    if call == "forward":
+        return lib.lasad_forward_window(0x1000, 0x2000, 0x3000, 0x4000, None, by(q), by(k), by(k), by(q), io, io, 1, 4, 2, 64, 0, 4, 4, 64, 1, None, scale, None)
+    if call == "step":
+        return lib.lasad_decode_step_window(0x1000, 0x2000, 0x3000, 0x4000, 0x5000, 0x6000, 8, io, io, 1, 4, 2, 64, 3, None, 4, 2, scale, None, 0, None)
+    return lib.lasad_backward_window(0x1000, 0x2000, 0x3000, 0x4000, 0x5000, 0x6000, 0x7000, 0x8000, 0x9000, by(q), by(k), by(k), by(q), by(q), by(q), by(k),
+                                     by(k), io, io, 1, 4, 2, 64, 0, 4, 4, 64, 1, None, scale, 0x10000, 1 << 30, None)
+
+
+@pytest.mark.parametrize("call,scale,io", [(c, 2.0 ** 127 * 1.5, io) for c in ("forward", "backward", "step") for io in (0, 1)] +
+                         [("backward", s, 1) for s in (1e-37, 1e-38, 2e-39, 1e-45)])
+def test_scales_that_pass_fp32_on_the_way(call, scale, io):
+    """scale log2 e, and with bf16 inputs lse / scale in the backward."""
+    assert _scaled(call, scale, io) == binding.ERR_UNSUPPORTED
+    assert b"scale" in binding.load().lasad_last_error()
