@@ -245,6 +245,9 @@ __device__ inline bool row_infinite(const T *row, int lane)
 // The launch order of `units` pieces of work of each of `heads` heads.  Workgroups follow one another over the 8 L2s: with 8 heads
 // and more each L2 gets heads of its own, so that what shares keys meets there, and its workgroups take piece after piece of all its
 // heads, so that pieces that take long, which come first, do not start last.  Fewer heads are dealt out over all L2s.
+// Heads (times batch rows) between two multiples of 8 take what the larger one does, as some dies then have a head less or none: 4096
+// tokens, window 1024, forward 28.7 us for 8 heads, 34.7 for 9, 35.1 for 12, 37.0 for 16, 45.5 for 17, 47.4 for 24, backward 72, 92, 93, 95, 126
+// and 130.
 struct Place {
     int head, unit;                    // (head -1: nothing to do)
 };

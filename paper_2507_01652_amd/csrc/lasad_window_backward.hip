@@ -18,7 +18,7 @@
 // of dS 1.7e-3, o's 0.7e-3, together 2.5e-3; dS as two operands would take the second part and cost a quarter to a third more products.
 //
 // bf16: lasad_window_backward_queries.hip and lasad_window_backward_keys.hip, 16 queries (keys) to a wavefront and 64 to a workgroup.
-// fp32, here: 32 and 128.  Products of 32 x 32 x 2 bound it, and two wavefronts a SIMD (175 and 230 registers of d = 64) that hide little
+// fp32, here: 32 and 128.  Products of 32 x 32 x 2 bound it, and two wavefronts a SIMD (175 and 229 registers of d = 64) that hide little
 // of what is between them: 2 x 20 heads of 1024 tokens, window 256, query pass 78 us and key pass 100, 48 and 50 TFLOP/s of the pairs that
 // are seen (a product of 8192^3: 154); the tiles of 128 cover half as many pairs again.
 #include "lasad_window.h"

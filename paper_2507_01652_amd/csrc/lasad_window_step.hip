@@ -3,8 +3,9 @@
 // Key j lies in cache row j < sinks ? j : sinks + (j - sinks) mod (cap - sinks); the call's own key and value come from its
 // arguments and are written to their row by the same launch.
 //
-// Bound by memory: the seen rows of k and v are read once, for all query heads that share them.  A row is read by d / 8 lanes
-// (fp32: d / 4) with one 16-byte load, so a wavefront takes 64 / lanes rows at a time, four such steps of k and v in flight.
+// Bound by memory: the seen rows of k and v are read once for up to four query heads that share them; more than four are dealt out over
+// workgroups of four, each of which reads them (64 rows, 8 key heads, 1040 keys: 24 query heads 23.6 us, 32 25.8, 40 48.4, 64 47.9).  A row is
+// read by d / 8 lanes (fp32: d / 4) with one 16-byte load, so a wavefront takes 64 / lanes rows at a time, four such steps of k and v in flight.
 // A group of lanes keeps maximum, sum and output of its rows for every query head of the group; they are joined over the
 // groups by cross-lane exchange, over the wavefronts in LDS, and, where few heads have many rows, over `splits` workgroups
 // by a second kernel.
@@ -315,8 +316,9 @@ hipError_t launch(const WindowStepArgs &a, hipStream_t s)
 
 }  // namespace
 
-// Splits of a call whose rows see up to `seen` keys: enough workgroups for the chip's 256 units twice, of at least 256 keys each; the
-// join's launch costs as much as 700 keys more in a workgroup (12 heads, us without and with: 1024 keys 7.1 and 8.0, 2048 10.5 and
+// Splits of a call whose rows see up to `seen` keys: enough workgroups for the chip's 256 units twice, planned with at least 256 keys each.
+// (A workgroup takes whole steps of 128 to 512 keys of bf16, so that the last splits may have none: 43 of 64 have some for 8 heads of 16448
+// keys.)  The join's launch costs as much as 700 keys more in a workgroup (12 heads, us without and with: 1024 keys 7.1 and 8.0, 2048 10.5 and
 // 8.1, 16384 73 and 13), and two splits of many heads gain nothing (256 heads of 4096 keys 40 and 43).
 int window_step_splits(int B, int Hk, int64_t seen)
 {
