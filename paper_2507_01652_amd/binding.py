@@ -858,6 +858,13 @@ def _rows(t: torch.Tensor, what: str) -> Layout:
     return Layout(*(t.stride(i) if t.shape[i] > 1 else 0 for i in range(3)))
 
 
+def _fit(*integers: int):
+    """Integers go through ctypes as their low 32 bits; those that have more are refused."""
+    for x in integers:
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"{x} does not fit 32 bits")
+
+
 def _head_weights(q_weight, k_weight, Hq: int, Hk: int, d: int) -> bool:
     """Checks the norm weights of query and key heads; whether they are one [d] for all heads."""
     shared = None
@@ -902,6 +909,7 @@ def lasad_forward_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: int,
     lq, lk = _rows(q, "q"), _rows(k, "k")
     B, n, Hq, d = q.shape
     Hk = k.shape[2]
+    _fit(B, n, Hq, Hk, d, grid_h, grid_w, start_pos, rope, pairing)
     shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
     qo, ko = _pair_out(out, q, k, out_dtype, "out")
     lqo, lko = _rows(qo, "out"), _rows(ko, "out")
@@ -914,6 +922,7 @@ def lasad_forward_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: int,
 
 
 def lasad_backward_qk_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, n_tokens: int, d: int, shared_weight: bool) -> int:
+    _fit(B, n_q_heads, n_k_heads, n_tokens, d)
     return int(load().lasad_backward_qk_workspace_bytes(B, n_q_heads, n_k_heads, n_tokens, d, shared_weight))
 
 
@@ -936,6 +945,7 @@ def lasad_backward_qk(q: torch.Tensor, k: torch.Tensor, d_q: torch.Tensor, d_k: 
     layouts = [_rows(t, what) for t, what in ((q, "q"), (k, "k"), (d_q, "d_q"), (d_k, "d_k"))]
     B, n, Hq, d = q.shape
     Hk = k.shape[2]
+    _fit(B, n, Hq, Hk, d, grid_h, grid_w, start_pos, rope, pairing)
     shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
     dq, dk = _pair_out(grads, q, k, grad_dtype, "grads")
     layouts += [_rows(dq, "grads"), _rows(dk, "grads")]
@@ -980,6 +990,7 @@ def lasad_decode_step_qk(q: torch.Tensor, k: torch.Tensor, grid_h: int, grid_w: 
     B, Hq, d = q.shape
     Hk = k.shape[1]
     pos, pos_rows = _step_position(pos, B)
+    _fit(B, Hq, Hk, d, grid_h, grid_w, pos, rope, pairing)
     shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
     qo, ko = _pair_out(out, q, k, out_dtype, "out")
     if not qo.is_contiguous() or not ko.is_contiguous():
@@ -1019,6 +1030,7 @@ def lasad_forward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, wind
             return done if want_lse else done[0]
     lq, lk, lv = _window_inputs(q, k, v, kv_lens)
     B, n, Hq, d = q.shape
+    _fit(*q.shape, *k.shape, window, sinks, start_pos)
     if out is None:
         out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
     elif out.shape != q.shape:
@@ -1035,6 +1047,7 @@ def lasad_forward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, wind
 
 def lasad_backward_window_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, n_tokens: int, n_keys: int, window: int,
                                           sinks: int) -> int:
+    _fit(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks)
     return int(load().lasad_backward_window_workspace_bytes(B, n_q_heads, n_k_heads, d, n_tokens, n_keys, window, sinks))
 
 
@@ -1052,6 +1065,7 @@ def lasad_backward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: 
     lq, lk, lv = _window_inputs(q, k, v, kv_lens)
     B, n, Hq, d = q.shape
     m, Hk = k.shape[1:3]
+    _fit(*q.shape, *k.shape, window, sinks, start_pos)
     for t in (o, d_o):
         if t.shape != q.shape or t.dtype != q.dtype:
             raise ValueError("o and d_o must have q's shape and dtype")
@@ -1079,6 +1093,7 @@ def lasad_backward_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: 
 
 def lasad_decode_step_window_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, cache_tokens: int, window: int,
                                              sinks: int) -> int:
+    _fit(B, n_q_heads, n_k_heads, d, cache_tokens, window, sinks)
     return int(load().lasad_decode_step_window_workspace_bytes(B, n_q_heads, n_k_heads, d, cache_tokens, window, sinks))
 
 
@@ -1103,6 +1118,7 @@ def lasad_decode_step_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
         raise ValueError("the caches must be [B, Hk, rows, d] in q's dtype")
     rows = k_cache.shape[2]
     pos, pos_rows = _step_position(pos, B)
+    _fit(*q.shape, Hk, rows, pos, window, sinks)
     if out is None:
         out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
     elif out.shape != q.shape or not out.is_contiguous():
