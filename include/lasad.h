@@ -598,6 +598,78 @@ int lasad_decode_step_window(const void *q, const void *k, const void *v, void *
                              int pos, const int32_t *pos_rows, int window, int sinks, float scale,
                              void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * A cache of keys and values in pages, held in 8 bits.  A page has the keys and the values of 64 positions of one row, for every key head, as
+ * e4m3 codes (finite up to 448, 0x7f and 0xff NaN) with a scale for each page and head: k = code * scale.
+ *   k_pages   [n_pages, n_k_heads, 64, d] bytes:  position t of the page, channel c.
+ *   v_pages   [n_pages, n_k_heads, d, 64] bytes:  channel c, position t = 16 b + 4 g + i (b, g, i in 0 .. 3) at 16 g + 4 b + i.
+ *   k_scales, v_scales  [n_pages, n_k_heads] fp32; 0: all codes of the page are 0.
+ *   table     int32, device: row b's positions 64 j .. 64 j + 63 lie in page table[b * table_stride + j], j < table_pages.  A number that
+ *             is none of the pool's (-1, say: given back once it has left the window) is not read or written: its keys are not seen.
+ * Pages that a call appends to belong to one row; others may lie in the tables of several (a common beginning).  What lies behind the
+ * positions that have been appended may be anything.
+ *
+ * Rows.  A call has new tokens of B rows, one row's behind the other's: row b has tokens row_starts[b] .. row_starts[b + 1] - 1
+ * (row_starts int32 [B + 1], device, not falling; tokens outside belong to no row, and what belongs to them is left as it was), at positions
+ * pos_rows[b], pos_rows[b] + 1, ..  (pos_rows int32 [B], device; NULL: pos for all).  row_starts NULL: one token a row, n_tokens = B.  A row
+ * with a position that is negative, off the grid or behind the table is inactive: nothing is written for it.
+ */
+typedef struct {
+    uint8_t *k_pages, *v_pages;
+    float *k_scales, *v_scales;
+    int32_t n_pages;
+    int32_t table_pages;
+    const int32_t *table;
+    int64_t table_stride;
+} lasad_pages_t;
+
+/*
+ * Appends new tokens to the rows' pages, with the norms and the rotation of lasad_forward_qk on the way; queries are normed and turned too.
+ *   q, k, v   [n_tokens, heads, d], type io_dtype, strides of their own (stride_n, stride_h; stride_b is not read).  q NULL: keys and
+ *             values alone (q_layout, q_out, q_out_layout, n_q_heads are not read).  v is taken as it is.
+ *   q_out     like q, type out_dtype (fp32, or bf16 with bf16 inputs); may be q itself with the same type and strides.
+ * Of each page that gets tokens, and each key head, with y the new k (or v) in fp32 and A their largest finite magnitude: the scale is
+ * max(A / 448, 2^-126) (0 if A is 0) if the page holds no earlier token (its first new one is at its position 0) or its scale is 0; otherwise it
+ * grows by the smallest power of two, 1 included, with which A <= 448 scale, and the earlier codes are divided by it.  code = y / scale,
+ * rounded to nearest even; NaN and infinities become NaN.
+ * Weights, norm_eps, rope, pairing, rope_base, d, alignments: as in lasad_forward_qk.  n_tokens may be 0; n_tokens * n_q_heads <= 2^30.
+ */
+int lasad_append_pages(const void *q, const void *k, const void *v, void *q_out,
+                       const lasad_layout_t *q_layout, const lasad_layout_t *k_layout, const lasad_layout_t *v_layout,
+                       const lasad_layout_t *q_out_layout, const lasad_pages_t *pages,
+                       int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d, int grid_h, int grid_w,
+                       int n_tokens, const int32_t *row_starts, int pos, const int32_t *pos_rows,
+                       const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
+                       int rope, int pairing, float rope_base, void *hip_stream);
+
+/*
+ * lasad_forward_window over the pages: the query at position p sees key j of its row if  j <= p,  and  p - j < window or j < sinks.
+ *   q, o      [n_tokens, n_q_heads, d], types io_dtype and out_dtype, strides of their own; the tokens' keys have been appended.
+ *   workspace lasad_forward_pages_workspace_bytes(...) bytes (one_each: row_starts is NULL), 16-byte aligned: few queries with many keys are
+ *             then dealt out over several workgroups.  NULL: they are not (same results up to rounding); a smaller one is
+ *             LASAD_ERR_WORKSPACE.  The query answers 0 for sizes that the call refuses.
+ * A query that sees nothing has o = 0.  Codes enter the products exactly; with bf16 queries P is rounded to bf16 as a matrix-core operand, everything
+ * else is fp32.  window, sinks, scale, shared key heads: as in lasad_forward_window.  Results are deterministic.
+ */
+size_t lasad_forward_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int one_each, int table_pages,
+                                           int window, int sinks);
+int lasad_forward_pages(const void *q, void *o, const lasad_layout_t *q_layout, const lasad_layout_t *o_layout, const lasad_pages_t *pages,
+                        int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d,
+                        int n_tokens, const int32_t *row_starts, int pos, const int32_t *pos_rows, int window, int sinks, float scale,
+                        void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Both for one token of every row: q, k (before their norms and rotation) and v [B, heads, d] contiguous; k and v are appended, o
+ * [B, n_q_heads, d] contiguous is the attention of the token over its row's pages, its own key among them.
+ */
+size_t lasad_decode_step_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int table_pages, int window, int sinks);
+int lasad_decode_step_pages(const void *q, const void *k, const void *v, void *o, const lasad_pages_t *pages,
+                            int io_dtype, int out_dtype, int B, int n_q_heads, int n_k_heads, int d, int grid_h, int grid_w,
+                            int pos, const int32_t *pos_rows,
+                            const float *q_weight, const float *k_weight, int shared_weight, float norm_eps,
+                            int rope, int pairing, float rope_base, int window, int sinks, float scale,
+                            void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* Reason for the last non-OK status returned on this thread (static storage). */
 const char *lasad_last_error(void);
 

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -35,6 +36,8 @@ EXPORTS = (
     "lasad_forward_qk", "lasad_backward_qk_workspace_bytes", "lasad_backward_qk", "lasad_decode_step_qk",
     "lasad_forward_window", "lasad_backward_window_workspace_bytes", "lasad_backward_window",
     "lasad_decode_step_window_workspace_bytes", "lasad_decode_step_window",
+    "lasad_append_pages", "lasad_forward_pages_workspace_bytes", "lasad_forward_pages",
+    "lasad_decode_step_pages_workspace_bytes", "lasad_decode_step_pages",
     "lasad_last_error", "lasad_version",
 )
 
@@ -47,6 +50,11 @@ class LasadError(RuntimeError):
 
 class Layout(ctypes.Structure):
     _fields_ = [("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64), ("stride_h", ctypes.c_int64)]
+
+
+class PagesStruct(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("k_pages", "v_pages", "k_scales", "v_scales")] + [
+        ("n_pages", ctypes.c_int32), ("table_pages", ctypes.c_int32), ("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -140,6 +148,17 @@ def load() -> ctypes.CDLL:
     lib.lasad_decode_step_window_workspace_bytes.restype = ctypes.c_size_t
     lib.lasad_decode_step_window.argtypes = [vp] * 6 + [ci] * 8 + [vp, ci, ci, cf, vp, ctypes.c_size_t, vp]
     lib.lasad_decode_step_window.restype = ci
+    pp = ctypes.POINTER(PagesStruct)
+    lib.lasad_append_pages.argtypes = [vp] * 4 + [lp] * 4 + [pp] + [ci] * 9 + [vp, ci, vp, vp, vp, ci, cf, ci, ci, cf, vp]
+    lib.lasad_append_pages.restype = ci
+    lib.lasad_forward_pages_workspace_bytes.argtypes = [ci] * 9
+    lib.lasad_forward_pages_workspace_bytes.restype = ctypes.c_size_t
+    lib.lasad_forward_pages.argtypes = [vp] * 2 + [lp] * 2 + [pp] + [ci] * 7 + [vp, ci, vp, ci, ci, cf, vp, ctypes.c_size_t, vp]
+    lib.lasad_forward_pages.restype = ci
+    lib.lasad_decode_step_pages_workspace_bytes.argtypes = [ci] * 7
+    lib.lasad_decode_step_pages_workspace_bytes.restype = ctypes.c_size_t
+    lib.lasad_decode_step_pages.argtypes = [vp] * 4 + [pp] + [ci] * 9 + [vp, vp, vp, ci, cf, ci, ci, cf, ci, ci, cf, vp, ctypes.c_size_t, vp]
+    lib.lasad_decode_step_pages.restype = ci
     lib.lasad_last_error.argtypes = []
     lib.lasad_last_error.restype = ctypes.c_char_p
     lib.lasad_version.argtypes = []
@@ -1131,6 +1150,170 @@ def lasad_decode_step_window(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, 
     _check(load().lasad_decode_step_window(
         _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(k_cache), _ptr(v_cache), rows, _dtype_code(q), _dtype_code(out), B, Hq, Hk, d,
         pos, _ptr(pos_rows), window, sinks, _scale(scale, q),
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+# ---- a cache in pages, held in 8 bits ----
+
+PAGE = 64                              # positions of a page
+
+
+class Pages(NamedTuple):
+    """A pool of pages (see include/lasad.h): k [n_pages, Hk, 64, d] and v [n_pages, Hk, d, 64] of e4m3 codes, fp32 scales [n_pages, Hk]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+
+
+def new_pages(n_pages: int, n_k_heads: int, d: int, device="cuda") -> Pages:
+    """A pool of empty pages."""
+    codes = [torch.empty(shape, dtype=torch.float8_e4m3fn, device=device) for shape in ((n_pages, n_k_heads, PAGE, d), (n_pages, n_k_heads, d, PAGE))]
+    return Pages(*codes, *(torch.empty((n_pages, n_k_heads), dtype=torch.float32, device=device) for _ in range(2)))
+
+
+def _pages(pages, table, Hk: int, d: int, B: int) -> PagesStruct:
+    k, v, k_scales, v_scales = pages
+    n = k.shape[0]
+    for t, shape in ((k, (n, Hk, PAGE, d)), (v, (n, Hk, d, PAGE))):
+        if tuple(t.shape) != shape or t.dtype != torch.float8_e4m3fn or not t.is_contiguous():
+            raise ValueError("the pages must be contiguous float8_e4m3fn, [n_pages, Hk, 64, d] of k and [n_pages, Hk, d, 64] of v")
+    for t in (k_scales, v_scales):
+        if tuple(t.shape) != (n, Hk) or t.dtype != torch.float32 or not t.is_contiguous():
+            raise ValueError("the scales must be contiguous fp32 [n_pages, Hk]")
+    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("the table must be int32 [B, pages] with unit stride along the pages")
+    _fit(n, table.shape[1])
+    _reachable(k, v, k_scales, v_scales, table)
+    return PagesStruct(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), n, table.shape[1], _ptr(table), table.stride(0) if B > 1 else 0)
+
+
+def _packed(t: torch.Tensor, what: str) -> Layout:
+    """Strides of packed tokens [T, heads, d]."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{what} must be [tokens, heads, d] with unit stride along d")
+    if t.numel() == 0:
+        return Layout(0, t.shape[1] * t.shape[2], t.shape[2])
+    return Layout(0, *(t.stride(i) if t.shape[i] > 1 else 0 for i in range(2)))
+
+
+def _row_starts(row_starts, B: int):
+    if row_starts is not None and (row_starts.dtype != torch.int32 or tuple(row_starts.shape) != (B + 1,) or not row_starts.is_contiguous()):
+        raise ValueError("row_starts must be contiguous int32 [B + 1]")
+
+
+def lasad_append_pages(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, pages: Pages, table: torch.Tensor, pos,
+                       grid_h: int, grid_w: int, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                       norm_eps: float = 1e-6, rope: int = ROPE_2D, pairing: int = PAIR_ADJACENT, rope_base: float = 10000.0,
+                       row_starts: torch.Tensor | None = None, out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                       stream=None):
+    """Appends the new tokens of the table's rows to their pages (see include/lasad.h), keys normed and rotated by raster position as in
+    lasad_forward_qk.  q [T, Hq, d], k, v [T, Hk, d]: views of packed tokens; row_starts: int32 [B + 1] on the device, None: one token a row;
+    pos: position of the rows' first new token, an integer or an int32 tensor [B] on the device (off the grid or the table: inactive); table:
+    int32 [B, pages].  Returns the normed and rotated queries (None without q); `out` may give them, q itself for in place."""
+    if k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("k and v must have one shape and dtype")
+    lk, lv = _packed(k, "k"), _packed(v, "v")
+    T, Hk, d = k.shape
+    B = table.shape[0]
+    p = _pages(pages, table, Hk, d, B)
+    _row_starts(row_starts, B)
+    pos, pos_rows = _step_position(pos, B)
+    Hq, lq, lo = 0, None, None
+    if q is None:
+        if out is not None or q_weight is not None:
+            raise ValueError("out or q_weight without q")
+    else:
+        lq = _packed(q, "q")
+        Hq = q.shape[1]
+        if q.shape[0] != T or q.shape[2] != d or q.dtype != k.dtype:
+            raise ValueError("q must share a dtype and every dimension but the heads with k")
+        if out is None:
+            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+        elif out.shape != q.shape:
+            raise ValueError("out has the wrong shape")
+        lo = _packed(out, "out")
+    _fit(T, Hq, Hk, d, B, grid_h, grid_w, pos, rope, pairing)
+    shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
+    _reachable(q, k, v, out, q_weight, k_weight, row_starts, pos_rows)
+    _check(load().lasad_append_pages(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), lq and ctypes.byref(lq), ctypes.byref(lk), ctypes.byref(lv), lo and ctypes.byref(lo), ctypes.byref(p),
+        _dtype_code(k), _dtype_code(k if out is None else out), B, Hq, Hk, d, grid_h, grid_w, T, _ptr(row_starts), pos, _ptr(pos_rows),
+        _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base, _stream(stream)))
+    return out
+
+
+def lasad_forward_pages_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, n_tokens: int, one_each: bool, table_pages: int,
+                                        window: int, sinks: int) -> int:
+    _fit(B, n_q_heads, n_k_heads, d, n_tokens, table_pages, window, sinks)
+    return int(load().lasad_forward_pages_workspace_bytes(B, n_q_heads, n_k_heads, d, n_tokens, bool(one_each), table_pages, window, sinks))
+
+
+def lasad_forward_pages(q: torch.Tensor, pages: Pages, table: torch.Tensor, pos, window: int, sinks: int = 0,
+                        row_starts: torch.Tensor | None = None, scale: float | None = None,
+                        out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                        workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
+    """lasad_forward_window of packed queries [T, Hq, d] (normed and rotated, their keys appended) over the rows' pages; rows, positions and
+    table as in lasad_append_pages.  Queries of inactive rows and of none are left as they were in `out`."""
+    lq = _packed(q, "q")
+    T, Hq, d = q.shape
+    B, Hk = table.shape[0], pages[0].shape[1]
+    p = _pages(pages, table, Hk, d, B)
+    _row_starts(row_starts, B)
+    pos, pos_rows = _step_position(pos, B)
+    _fit(T, Hq, Hk, d, B, pos, window, sinks)
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError("out has the wrong shape")
+    lo = _packed(out, "out")
+    if workspace is None and use_workspace:
+        need = lasad_forward_pages_workspace_bytes(B, Hq, Hk, d, T, row_starts is None, table.shape[1], window, sinks)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    _reachable(q, out, row_starts, pos_rows, workspace)
+    _check(load().lasad_forward_pages(
+        _ptr(q), _ptr(out), ctypes.byref(lq), ctypes.byref(lo), ctypes.byref(p), _dtype_code(q), _dtype_code(out), B, Hq, Hk, d, T,
+        _ptr(row_starts), pos, _ptr(pos_rows), window, sinks, _scale(scale, q),
+        _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
+    return out
+
+
+def lasad_decode_step_pages_workspace_bytes(B: int, n_q_heads: int, n_k_heads: int, d: int, table_pages: int, window: int, sinks: int) -> int:
+    _fit(B, n_q_heads, n_k_heads, d, table_pages, window, sinks)
+    return int(load().lasad_decode_step_pages_workspace_bytes(B, n_q_heads, n_k_heads, d, table_pages, window, sinks))
+
+
+def lasad_decode_step_pages(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pages: Pages, table: torch.Tensor, pos,
+                            grid_h: int, grid_w: int, window: int, sinks: int = 0,
+                            q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, norm_eps: float = 1e-6,
+                            rope: int = ROPE_2D, pairing: int = PAIR_ADJACENT, rope_base: float = 10000.0, scale: float | None = None,
+                            out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+                            workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
+    """One token of every row: q [B, Hq, d], k, v [B, Hk, d] contiguous, as they leave the projection; norms, rotation, append to the
+    pages and attention over them.  pos and table as in lasad_append_pages; an inactive row's output is not written."""
+    B, Hq, d = q.shape
+    _same(k, (v,), "k and v must be contiguous [B, Hk, d] of one shape and dtype")
+    if not q.is_contiguous() or k.dim() != 3 or k.shape[0] != B or k.shape[2] != d or k.dtype != q.dtype:
+        raise ValueError("q must be contiguous [B, Hq, d], k and v [B, Hk, d], of one dtype")
+    Hk = k.shape[1]
+    p = _pages(pages, table, Hk, d, B)
+    pos, pos_rows = _step_position(pos, B)
+    _fit(*q.shape, Hk, grid_h, grid_w, pos, rope, pairing, window, sinks)
+    shared = _head_weights(q_weight, k_weight, Hq, Hk, d)
+    if out is None:
+        out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=q.device)
+    elif out.shape != q.shape or not out.is_contiguous():
+        raise ValueError("out must be contiguous [B, Hq, d]")
+    if workspace is None and use_workspace:
+        need = lasad_decode_step_pages_workspace_bytes(B, Hq, Hk, d, table.shape[1], window, sinks)
+        if need:
+            workspace = _scratch(need, q.device, stream)
+    _reachable(q, k, v, out, q_weight, k_weight, pos_rows, workspace)
+    _check(load().lasad_decode_step_pages(
+        _ptr(q), _ptr(k), _ptr(v), _ptr(out), ctypes.byref(p), _dtype_code(q), _dtype_code(out), B, Hq, Hk, d, grid_h, grid_w, pos, _ptr(pos_rows),
+        _ptr(q_weight), _ptr(k_weight), shared, norm_eps, rope, pairing, rope_base, window, sinks, _scale(scale, q),
         _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)))
     return out
 

@@ -43,6 +43,9 @@ SOURCES = [
     "lasad_window_backward_keys.hip",
     "lasad_window_backward_few.hip",
     "lasad_window_step.hip",
+    "lasad_api_pages.hip",
+    "lasad_pages_append.hip",
+    "lasad_pages_attend.hip",
 ]
 
 # Packed-fp32 instruction selection is switched off for every HIP translation unit.

@@ -18,102 +18,13 @@
 // sums) 40 us, and 4.7 for the second kernel.  One token of 24 heads 3 us.  Stores past the caches take the stream of forwards to
 // 39.4 us, but what reads the outputs next then finds none of them in the 256 MB in front of the memory (with the attention after
 // it: 96 MB of outputs 96 us and 105 so, 192 MB 192 and 195, 768 MB 747 and 740), so they are ordinary ones.
-#include "lasad_attention.h"
-#include "lasad_mfma_util.h"
+#include "lasad_heads.h"
 
 namespace lasad {
 
 namespace {
 
 constexpr int kThreads = 256;
-
-template <int BF16>
-__device__ inline void load8(const char *p, float (&f)[8])
-{
-    if (BF16) {
-        const uint4 w = *(const uint4 *)p;
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            f[2 * e] = __uint_as_float(ww[e] << 16);
-            f[2 * e + 1] = __uint_as_float(ww[e] & 0xffff0000u);
-        }
-    } else {
-        const float4 lo = *(const float4 *)p, hi = *(const float4 *)(p + 16);
-        f[0] = lo.x; f[1] = lo.y; f[2] = lo.z; f[3] = lo.w;
-        f[4] = hi.x; f[5] = hi.y; f[6] = hi.z; f[7] = hi.w;
-    }
-}
-
-template <int BF16>
-__device__ inline void store8(char *p, const float (&f)[8])
-{
-    if (BF16) {
-        *(uint4 *)p = make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
-    } else {
-        *(float4 *)p = make_float4(f[0], f[1], f[2], f[3]);
-        *(float4 *)(p + 16) = make_float4(f[4], f[5], f[6], f[7]);
-    }
-}
-
-template <int CTRL>
-__device__ inline float dpp_add(float x)
-{
-    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
-}
-
-// Sum over the LPR lanes (4, 8 or 16, aligned) of a row, in every one of them.
-template <int LPR>
-__device__ inline float row_sum(float x)
-{
-    x = dpp_add<0xB1>(x);                        // lane ^ 1
-    x = dpp_add<0x4E>(x);                        // lane ^ 2
-    if (LPR >= 8) x = dpp_add<0x141>(x);         // mirrored in 8 lanes: the other four (which are equal by now)
-    if (LPR >= 16) x = dpp_add<0x140>(x);        // mirrored in 16 lanes
-    return x;
-}
-
-// What a lane needs to turn its 8 channels with the table of its token.
-struct Turn {
-    int base;            // first table entry
-    int partner;         // halves: lane distance to the other member of the pairs
-    float sign;          // halves: -1 where this lane holds the first members
-};
-
-template <int D>
-__device__ inline Turn lane_turn(const QkArgs &a, int piece)
-{
-    constexpr int LPR = D / 8;
-    Turn t = {4 * piece, 0, 1.f};
-    if (a.pairing == LASAD_PAIR_HALVES) {
-        t.partner = a.rope == LASAD_ROPE_2D ? LPR / 4 : LPR / 2;
-        const bool first = (piece & t.partner) == 0;
-        t.sign = first ? -1.f : 1.f;
-        t.base = a.rope == LASAD_ROPE_2D ? (piece / (LPR / 2)) * (D / 4) + (piece % (LPR / 4)) * 8 : (piece % (LPR / 2)) * 8;
-    }
-    return t;
-}
-
-// y turned in place; inverse: by the opposite angles.
-__device__ inline void turn8(const float2 *cs, const Turn &t, bool inverse, float (&y)[8])
-{
-    if (t.partner == 0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 c = cs[t.base + i];
-            const float s = inverse ? -c.y : c.y, p = y[2 * i], q = y[2 * i + 1];
-            y[2 * i] = p * c.x - q * s;
-            y[2 * i + 1] = p * s + q * c.x;
-        }
-    } else {
-        const float sg = inverse ? -t.sign : t.sign;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 c = cs[t.base + i];
-            y[i] = y[i] * c.x + __shfl_xor(y[i], t.partner) * (sg * c.y);
-        }
-    }
-}
 
 // The table of `count` tokens from `first` on: cosines and sines, byte offsets of the tokens (queries, keys), whether the
 // token is on the grid.
@@ -128,10 +39,7 @@ __device__ inline void make_tables(const QkArgs &a, int64_t first, int count, in
     constexpr int P = D / 2;
     const int tid = threadIdx.x;
     const int pair = tid % P;
-    const int k = a.rope == LASAD_ROPE_2D ? pair % (D / 4) : pair;
-    // turns a position: base^(-k / pairs of an axis) / (2 pi)
-    const double f = a.rope == LASAD_ROPE_NONE ? 0.0
-                   : exp2(-(double)k * a.log2_base / (a.rope == LASAD_ROPE_2D ? D / 4 : P)) * 0.15915494309189533577;
+    const double f = pair_turns<D>(a.rope, pair, a.log2_base);
     for (int t = tid / P; t < count; t += kThreads / P) {
         const uint32_t token = (uint32_t)(first + t), b = token / (uint32_t)a.n, i = token - b * (uint32_t)a.n;
         int pos = a.start_pos + (int)i;
@@ -152,15 +60,7 @@ __device__ inline void make_tables(const QkArgs &a, int64_t first, int count, in
             o.on = on;
             tok[t] = o;
         }
-        if (a.rope != LASAD_ROPE_NONE) {
-            int p = pos;
-            if (a.rope == LASAD_ROPE_2D) p = pair < D / 4 ? pos / a.grid_w : pos % a.grid_w;
-            const double turns = (double)p * f;
-            const float r = (float)(turns - rint(turns));            // -0.5 .. 0.5
-            float s, c;
-            sincospif(2.0f * r, &s, &c);
-            cs[t * P + pair] = make_float2(c, s);
-        }
+        if (a.rope != LASAD_ROPE_NONE) cs[t * P + pair] = pair_angle<D>(a.rope, pair, pos, a.grid_w, f);
     }
 }
 
@@ -180,7 +80,7 @@ qk_forward_kernel(QkArgs a, int tile)
 
     const int heads = a.heads[0] + a.heads[1];
     const int piece = threadIdx.x % LPR;
-    const Turn turn = lane_turn<D>(a, piece);
+    const Turn turn = lane_turn<D>(a.rope, a.pairing, piece);
     int t = (threadIdx.x / LPR) / heads, h = (threadIdx.x / LPR) % heads;
     const int step_t = SLOTS / heads, step_h = SLOTS % heads;
     while (t < count) {
@@ -268,7 +168,7 @@ qk_backward_kernel(QkArgs a, int tile, int share)
 
     const int heads = a.heads[0] + a.heads[1];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, piece = lane % LPR;
-    const Turn turn = lane_turn<D>(a, piece);
+    const Turn turn = lane_turn<D>(a.rope, a.pairing, piece);
     const bool want = a.partial != nullptr;
     float accq[8], acck[8];
 #pragma unroll

@@ -1,0 +1,602 @@
+"""The paged 8-bit cache on the GPU against the 64-bit reference: appends, attention over the pages, steps; types, head layouts, rows of any
+length anywhere in their pages, masks, pages that are not there, numbers that are not finite, views, streams, graph replays."""
+import math
+
+import pytest
+import torch
+
+import pages_reference as pr
+import softmax_layer_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+BF, F = torch.bfloat16, torch.float32
+EPS, BASE = 1e-6, 10000.0
+LAST = 2 ** 31 - 1
+
+
+@pytest.fixture(scope="module")
+def lasad():
+    assert torch.cuda.is_available()
+    from paper_2507_01652_amd import binding
+    binding.load()
+    return binding
+
+
+def table_of(rows, n_pages, seed, spare=1, width=None):
+    """A table of shuffled pages for rows (first, n, pos), those of every position up to the last."""
+    need = [(max(p, 0) + n + pr.PAGE - 1) // pr.PAGE for _, n, p in rows]
+    order = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed)).tolist()
+    table = torch.full((len(rows), width or max(need) + spare), -1, dtype=torch.int32)
+    for b, n in enumerate(need):
+        for j in range(min(n, table.shape[1])):
+            table[b, j] = order.pop()
+    return table
+
+
+def starts_of(rows):
+    return torch.tensor([r[0] for r in rows] + [rows[-1][0] + rows[-1][1]], dtype=torch.int32)
+
+
+def packed(lengths, positions, lead=0):
+    rows, at = [], lead
+    for n, p in zip(lengths, positions):
+        rows.append((at, n, p))
+        at += n
+    return rows
+
+
+def on_gpu(table, rows, one_each=False):
+    return table.cuda(), torch.tensor([r[2] for r in rows], dtype=torch.int32).cuda(), None if one_each else starts_of(rows).cuda()
+
+
+def cpu(pages):
+    return [t.clone().cpu() for t in pages]
+
+
+def project(T, Hq, Hk, d, dtype, seed, scale=1.0):
+    """q, k, v as views of one projection, on the GPU."""
+    return ref.draw((T, Hq + 2 * Hk, d), dtype, seed, scale).cuda().split((Hq, Hk, Hk), 1)
+
+
+def weights(Hq, Hk, d, kind, seed=5):
+    if kind is None:
+        return None, None
+    shapes = ((d,), (d,)) if kind == "shared" else ((Hq, d), (Hk, d))
+    return tuple(1 + 0.2 * ref.draw(s, F, seed + i) for i, s in enumerate(shapes))
+
+
+def cuda(t):
+    return None if t is None else t.cuda()
+
+
+def expected(x, w, rows, T, grid_w, rope, halves, eps, dtype):
+    """Normed and rotated heads in fp64 and the kernel's bound of them (before they are stored)."""
+    positions = torch.zeros(T, dtype=torch.long)
+    for first, n, p in rows:
+        if n > 0 and p >= 0:
+            positions[first:first + n] = p + torch.arange(n)
+    x = x.cpu().double()
+    w = None if w is None else w.double()
+    y = ref.qk_row(x, w, positions, grid_w, rope, halves, BASE, eps)
+    return y, ref.qk_forward_bound(x, w, rope, halves, eps, F, y, int(positions.max()))
+
+
+# dtype, out dtype, d, Hq, Hk, lengths, positions, grid_w, rope, halves, weights, eps
+APPENDS = [
+    (BF, BF, 64, 2, 2, [130], [0], 16, 2, False, "shared", EPS),
+    (BF, F, 64, 6, 2, [5, 0, 64, 1, 200], [61, 3, 64, 127, 40], 23, 2, True, "heads", EPS),
+    (F, F, 64, 4, 1, [3, 77, 65], [0, 1, 63], 24, 1, False, "shared", EPS),
+    (F, F, 64, 5, 5, [64, 63], [128, 129], 24, 1, True, None, EPS),
+    (BF, BF, 32, 3, 3, [100, 2], [7, 62], 9, 2, True, "heads", EPS),
+    (F, F, 32, 4, 2, [1, 1, 1], [0, 31, 63], 9, 2, False, "shared", EPS),
+    (BF, BF, 128, 4, 2, [70, 64, 9], [3, 0, 500], 100, 2, False, "shared", EPS),
+    (F, F, 128, 2, 1, [129], [62], 100, 1, True, "heads", EPS),
+    (BF, BF, 64, 3, 1, [50, 14], [10, 50], 16, 0, False, None, -1.0),                      # as they are
+    (BF, BF, 64, 3, 1, [50, 14], [10, 50], 16, 2, False, None, -1.0),                      # rotation alone
+    (F, F, 64, 2, 2, [90], [1000000], 4096, 2, False, "shared", EPS),                      # far positions
+    (BF, BF, 64, 1, 1, [0, 0, 1, 0], [5, 5, 5, 5], 16, 2, False, "shared", EPS),           # one token in all
+]
+
+
+@pytest.mark.parametrize("case", range(len(APPENDS)))
+def test_append(lasad, case):
+    dt, odt, d, Hq, Hk, lengths, positions, W, rope, halves, kind, eps = APPENDS[case]
+    rows = packed(lengths, positions, lead=2)
+    T = rows[-1][0] + rows[-1][1] + 3                      # tokens before the first row and behind the last belong to none
+    far = max(positions) // pr.PAGE if max(positions) > 10000 else 0
+    pool = 40 if not far else 8
+    if far:                                                # pages of the last positions alone, the others given back
+        table = torch.full((len(rows), far + 4), -1, dtype=torch.int32)
+        table[0, far:] = torch.arange(4, dtype=torch.int32)
+    else:
+        table = table_of(rows, pool, 3)
+    pages = pr.filled_pool(lasad, pool, Hk, d, 11)
+    # (pages of positions that no earlier call has filled hold anything)
+    before = cpu(pages)
+    q, k, v = project(T, Hq, Hk, d, dt, 20 + case)
+    wq, wk = weights(Hq, Hk, d, kind)
+    t, pos, starts = on_gpu(table, rows)
+    H = (max(p + n for p, n in zip(positions, lengths)) + W) // W + 1
+    mark = torch.full((T, Hq, d), 7.0, dtype=odt, device="cuda")
+    out = lasad.lasad_append_pages(q, k, v, pages, t, pos, H, W, cuda(wq), cuda(wk), eps, rope, int(halves), BASE, row_starts=starts, out=mark)
+    assert out is mark
+    yk, ek = expected(k, wk, rows, T, W, rope, halves, eps, dt)
+    pr.check_append(before, cpu(pages), table, rows, H * W, yk, ek, v.cpu().double())
+    yq, eq = expected(q, wq, rows, T, W, rope, halves, eps, dt)
+    on = pr.written(rows, table, H * W, T)
+    got = out.cpu().double()
+    assert (got[~on] == 7.0).all()
+    assert ((got - yq).abs() <= eq + ref.stored(odt, yq))[on].all()
+    # keys and values alone leave the same pages
+    again = lasad.Pages(*(x.clone().cuda() for x in before))
+    assert lasad.lasad_append_pages(None, k, v, again, t, pos, H, W, None, cuda(wk), eps, rope, int(halves), BASE, row_starts=starts) is None
+    for a, b in zip(cpu(again), cpu(pages)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_append_many_rows(lasad):
+    """More rows than a wavefront looks at in one go, most of them empty or a token long."""
+    for B in (63, 64, 65, 200, 5000):
+        gen = torch.Generator().manual_seed(B)
+        lengths = torch.randint(0, 3, (B,), generator=gen).tolist()
+        lengths[B // 2] = 70
+        positions = torch.randint(0, 100, (B,), generator=gen).tolist()
+        rows = packed(lengths, positions)
+        T = sum(lengths)
+        table = table_of(rows, 4 * B, 1)
+        pages = pr.filled_pool(lasad, 4 * B, 1, 32, 2)
+        before = cpu(pages)
+        q, k, v = project(T, 1, 1, 32, F, 3)
+        t, pos, starts = on_gpu(table, rows)
+        lasad.lasad_append_pages(q, k, v, pages, t, pos, 30, 10, row_starts=starts)
+        yk, ek = expected(k, None, rows, T, 10, 2, False, EPS, F)
+        pr.check_append(before, cpu(pages), table, rows, 300, yk, ek, v.cpu().double())
+
+
+def test_append_inactive_rows_and_missing_pages(lasad):
+    """Rows off the grid or behind the table and page numbers that are none of the pool's: nothing of them is written."""
+    rows = packed([5, 5, 70, 4, 66, 1, 3], [-1, 126, 60, 0, 0, 2 ** 31 - 1, 120])
+    T, Hk, d = rows[-1][0] + rows[-1][1], 2, 64
+    table = torch.tensor([[0, 1], [2, 3], [4, -1], [10 ** 9, 5], [-2 ** 31, 6], [7, 8], [9, 99]], dtype=torch.int32)
+    pages = pr.filled_pool(lasad, 12, Hk, d, 4)
+    before = cpu(pages)
+    q, k, v = project(T, 4, Hk, d, BF, 9)
+    t, pos, starts = on_gpu(table, rows)
+    for grid in ((16, 16), (1, 121)):                      # in the second one the last row leaves the grid, and the third
+        mark = torch.full((T, 4, d), 7.0, dtype=BF, device="cuda")
+        lasad.lasad_append_pages(q, k, v, pages, t, pos, *grid, row_starts=starts, out=mark)
+        yk, ek = expected(k, None, rows, T, grid[1], 2, False, EPS, BF)
+        now = cpu(pages)
+        pr.check_append(before, now, table, rows, grid[0] * grid[1], yk, ek, v.cpu().double())
+        on = pr.written(rows, table, grid[0] * grid[1], T)
+        assert (mark.cpu()[~on] == 7.0).all() and (mark.cpu()[on] != 7.0).any(-1).any(-1).all()
+        before = now
+
+
+def test_append_token_by_token(lasad):
+    """A page filled by single tokens that grow: its scale grows by powers of two, earlier codes with it; and by the bounds of one
+    rounding where nothing leaves the normal codes."""
+    d, Hk, n = 64, 3, 130
+    table = torch.tensor([[2, 0, 1], [4, 5, 3]], dtype=torch.int32)
+    pages = pr.new_pool(lasad, 6, Hk, d)
+    x = ref.draw((n, 2, 3 * Hk, d), F, 1) * (1.05 ** torch.arange(n))[:, None, None, None]
+    x[:5] = 0.0                                            # a page that begins with zeros
+    x = x.cuda()
+    for i in range(n):
+        q, k, v = x[i].split((Hk, Hk, Hk), 1)
+        before = cpu(pages)
+        lasad.lasad_append_pages(q, k, v, pages, table.cuda(), i, 30, 10, norm_eps=-1.0)
+        rows = [(0, 1, i), (1, 1, i)]
+        yk, ek = expected(k, None, rows, 2, 10, 2, False, -1.0, F)
+        pr.check_append(before, cpu(pages), table, rows, 300, yk, ek, v.cpu().double())
+    k, v = pr.values(pages)
+    for b in range(2):
+        got = torch.cat([v[int(table[b, j])].transpose(0, 1) for j in range(3)])[:n]
+        want = x[:, b, 2 * Hk:].cpu().double()
+        scale = torch.cat([pages[3].cpu().double()[int(table[b, j])].expand(pr.PAGE, Hk) for j in range(3)])[:n]
+        # the first rounding, and one more below the smallest normal code of the last scale
+        assert ((got - want).abs() <= want.abs() * 2.0 ** -4 * (1 + 4 * pr.U) + 2 * 2.0 ** -10 * scale[..., None]).all()
+
+
+@pytest.mark.parametrize("size", [1e-44, 1e-39, 1e-36, 1e-30, 1.0, 1e30, 3e38])
+def test_append_sizes(lasad, size):
+    """Numbers of any size, without the norm; the least scale is 2^-126."""
+    x = (ref.draw((70, 3, 64), torch.float64, 3).clamp(-1, 1) * size).to(F)
+    rows = packed([70], [40])
+    table = torch.tensor([[1, 0]], dtype=torch.int32)
+    pages = pr.new_pool(lasad, 2, 1, 64)
+    lasad.lasad_append_pages(None, *x[:1, 1:].expand(40, 2, 64).contiguous().cuda().split((1, 1), 1), pages, table.cuda(), 0, 16, 16, norm_eps=-1.0,
+                             rope=0, row_starts=torch.tensor([0, 40], dtype=torch.int32).cuda())
+    before = cpu(pages)
+    q, k, v = x.cuda().split((1, 1, 1), 1)
+    t, pos, starts = on_gpu(table, rows)
+    lasad.lasad_append_pages(q, k, v, pages, t, pos, 16, 16, norm_eps=-1.0, rope=0, row_starts=starts)
+    # (a subnormal fp32 number may count as 0)
+    flushed = torch.full((70, 1, 64), 2.0 ** -126 if size < 1e-37 else 0.0, dtype=torch.float64)
+    pr.check_append(before, cpu(pages), table, rows, 256, k.cpu().double(), flushed, v.cpu().double())
+
+
+def test_append_not_finite(lasad):
+    """NaN and infinities are held as NaN and leave the others' scale alone."""
+    x = ref.draw((100, 3, 64), F, 3)
+    x[7, 1, 3], x[20, 1, 0], x[21, 2, 63], x[99, 2, 1] = math.nan, math.inf, -math.inf, math.nan
+    x[64:100, 1] = math.nan                                # a page of NaN: scale 0
+    rows = packed([100], [0])
+    table = torch.tensor([[1, 0]], dtype=torch.int32)
+    pages = pr.new_pool(lasad, 2, 1, 64)
+    before = cpu(pages)
+    q, k, v = x.cuda().split((1, 1, 1), 1)
+    t, pos, starts = on_gpu(table, rows)
+    lasad.lasad_append_pages(q, k, v, pages, t, pos, 16, 16, norm_eps=-1.0, rope=0, row_starts=starts)
+    pr.check_append(before, cpu(pages), table, rows, 256, k.cpu().double(), torch.zeros(100, 1, 64, dtype=torch.float64), v.cpu().double())
+
+
+def test_append_in_place_and_broadcast(lasad):
+    q, k, v = project(70, 4, 2, 64, BF, 1)
+    q = q.contiguous()
+    k, v = k[:1].expand(70, 2, 64), v[:, :1].expand(70, 2, 64)              # strides of 0
+    rows = packed([30, 40], [5, 60])
+    table = table_of(rows, 6, 1)
+    t, pos, starts = on_gpu(table, rows)
+    pools = [pr.filled_pool(lasad, 6, 2, 64, 2) for _ in range(2)]
+    want = lasad.lasad_append_pages(q, k.contiguous(), v.contiguous(), pools[0], t, pos, 16, 16, row_starts=starts)
+    assert lasad.lasad_append_pages(q, k, v, pools[1], t, pos, 16, 16, row_starts=starts, out=q) is q
+    assert torch.equal(q, want)
+    for a, b in zip(*pools):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+# dtype, out dtype, d, Hq, Hk, lengths, positions, window, sinks
+ATTENDS = [
+    (BF, BF, 64, 2, 2, [130], [0], 50, 0),
+    (BF, F, 64, 6, 2, [5, 0, 64, 1, 200], [61, 3, 64, 127, 40], 96, 16),
+    (F, F, 64, 4, 1, [3, 77, 65], [0, 1, 63], 33, 3),
+    (F, F, 64, 5, 5, [64, 63], [128, 129], 2 ** 31 - 1, 0),
+    (BF, BF, 64, 5, 5, [64, 63], [128, 129], 1, 0),                                        # every query sees itself
+    (BF, BF, 64, 4, 2, [64, 63], [300, 329], 40, 2 ** 31 - 1),                             # all are sinks
+    (BF, BF, 64, 4, 2, [64, 7], [300, 329], 40, 130),                                      # sinks of three pages
+    (BF, BF, 32, 3, 3, [100, 2], [7, 62], 64, 1),
+    (F, F, 32, 4, 2, [1, 1, 1], [0, 31, 63], 65, 0),
+    (BF, BF, 128, 4, 2, [70, 64, 9], [3, 0, 500], 77, 4),
+    (F, F, 128, 2, 1, [129], [62], 63, 5),
+    (BF, BF, 64, 17, 1, [1, 2, 30], [70, 0, 200], 100, 0),                                 # more query heads a key head than a tile has columns
+    (BF, BF, 64, 48, 1, [1, 1], [70, 900], 1000, 0),
+    (BF, BF, 64, 2, 2, [3, 1], [5000, 4000], 4500, 8),                                     # long: dealt out over workgroups
+    (F, F, 64, 6, 2, [2, 1], [5000, 4000], 2 ** 30, 0),
+    (BF, F, 128, 8, 1, [1, 1], [3000, 2900], 2800, 70),
+    (BF, BF, 64, 4, 4, [600, 300], [0, 300], 128, 1),
+    (BF, BF, 32, 4, 1, [600, 300], [0, 300], 128, 70),
+    (BF, BF, 128, 4, 1, [300, 300], [0, 300], 128, 70),
+]
+
+
+@pytest.mark.parametrize("case", range(len(ATTENDS)))
+def test_attention(lasad, case):
+    dt, odt, d, Hq, Hk, lengths, positions, window, sinks = ATTENDS[case]
+    one = all(n == 1 for n in lengths)
+    rows = packed(lengths, positions, lead=0 if one else 3)
+    T = rows[-1][0] + rows[-1][1] + (0 if one else 2)
+    need = sum((p + n + 63) // 64 for _, n, p in rows)
+    table = table_of(rows, need + 3, 8)
+    pages = pr.filled_pool(lasad, need + 3, Hk, d, 12, spread=1.5)
+    spoil(pages, table, rows)
+    q = ref.draw((T, 2 * Hq, d), dt, 30 + case).cuda()[:, Hq:]             # a view
+    t, pos, starts = on_gpu(table, rows, one)
+    want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, window, sinks, d ** -0.5, dt, odt)
+    on = pr.written(rows, table, LAST, T)
+    for split in (True, False):
+        mark = torch.full((T, 2 * Hq, d), 7.0, dtype=odt, device="cuda")[:, :Hq]
+        o = lasad.lasad_forward_pages(q, pages, t, pos, window, sinks, row_starts=starts, out=mark, use_workspace=split).cpu().double()
+        assert (o[~on] == 7.0).all()
+        assert ((o - want).abs() <= bound)[on].all(), ((o - want).abs() / bound)[on].max().item()
+
+
+def spoil(pages, table, rows):
+    """NaN behind the rows' last positions."""
+    k, v = pages[0].view(torch.uint8), pages[1].view(torch.uint8)
+    for b, (_, n, p) in enumerate(rows):
+        end = p + n
+        if end % 64 and n:
+            page = int(table[b, end // 64])
+            k[page, :, end % 64:] = 0xff
+            v[page][..., pr.PLACE[end % 64:].cuda()] = 0x7f
+
+
+@pytest.mark.parametrize("lengths", [[40, 150], [600, 300]])
+@pytest.mark.parametrize("dt", [BF, F])
+def test_attention_nan_reaches_those_that_see_it(lasad, lengths, dt):
+    """A NaN code in a key or a value: the queries that see it have NaN (in that channel, or in all), the others what they have without it."""
+    d, Hq, Hk, window, sinks = 64, 4, 2, 70, 2
+    rows = packed(lengths, [100, 13])
+    T = sum(lengths)
+    need = sum((p + n + 63) // 64 for _, n, p in rows)
+    table = table_of(rows, need, 8, spare=0)
+    pages = pr.filled_pool(lasad, need, Hk, d, 12)
+    q = ref.draw((T, Hq, d), dt, 3).cuda()
+    t, pos, starts = on_gpu(table, rows)
+    clean = lasad.lasad_forward_pages(q, pages, t, pos, window, sinks, row_starts=starts).cpu()
+    for (b, j, of) in ((0, 120, "v"), (1, 1, "v"), (1, 100, "k"), (0, 64, "v"), (1, 63, "v"), (0, 139, "k")):
+        dirty = lasad.Pages(*(x.clone() for x in pages))
+        page = int(table[b, j // 64])
+        if of == "v":
+            dirty.v.view(torch.uint8)[page, 1, 5, pr.PLACE[j % 64]] = 0x7f
+        else:
+            dirty.k.view(torch.uint8)[page, 1, j % 64, 5] = 0xff
+        got = lasad.lasad_forward_pages(q, dirty, t, pos, window, sinks, row_starts=starts).cpu()
+        first, n, p = rows[b]
+        hit = torch.zeros(got.shape, dtype=torch.bool)
+        for i in range(n):
+            if j <= p + i and (p + i - j < window or j < sinks):
+                hit[first + i, 2:, 5 if of == "v" else slice(None)] = True
+        assert torch.equal(torch.isnan(got), hit), (b, j, of)
+        assert torch.equal(got[~hit], clean[~hit]), (b, j, of)
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+def test_attention_beside_a_missing_page(lasad, dt):
+    """A page missing among those that are seen, for few columns and many."""
+    d = 64
+    table = torch.tensor([[2, -1, 3, 4], [0, 5, 7, 1]], dtype=torch.int32)
+    pages = pr.filled_pool(lasad, 7, 2, d, 12)
+    for lengths, positions in (([150, 100], [60, 100]), ([1, 1], [200, 150])):
+        rows = packed(lengths, positions)
+        q = ref.draw((sum(lengths), 4, d), dt, 3).cuda()
+        t, pos, starts = on_gpu(table, rows)
+        o = lasad.lasad_forward_pages(q, pages, t, pos, 1000, row_starts=starts).cpu().double()
+        want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, 1000, 0, d ** -0.5, dt, dt)
+        assert ((o - want).abs() <= bound).all()
+
+
+def test_attention_pages_that_are_not_there(lasad):
+    """Page numbers that are none of the pool's are not seen; a row that sees nothing has 0; inactive rows (the last three) are left."""
+    rows = packed([3, 4, 70, 2, 5], [100, 10, 60, -5, 127])
+    T, d = 84, 64
+    table = torch.tensor([[-1, 0], [-1, 1], [2, 2 ** 30], [3, 4], [5, 6]], dtype=torch.int32)
+    pages = pr.filled_pool(lasad, 7, 2, d, 12)
+    for dt in (BF, F):
+        q = ref.draw((T, 4, d), dt, 3).cuda()
+        t, pos, starts = on_gpu(table, rows)
+        mark = torch.full((T, 4, d), 7.0, dtype=dt, device="cuda")
+        o = lasad.lasad_forward_pages(q, pages, t, pos, 1000, 0, row_starts=starts, out=mark).cpu().double()
+        want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, 1000, 0, d ** -0.5, dt, dt)
+        on = pr.written(rows, table, LAST, T)
+        assert on.sum() == 7 and (o[~on] == 7.0).all()
+        assert ((o - want).abs() <= bound)[on].all()
+        assert (o[3:7] == 0).all()
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+def test_attention_scores_that_move_the_maximum(lasad, dt):
+    """Scores that rise, fall and jump by hundreds from page to page, pages of zeros, scales far apart."""
+    d, Hq, Hk, n, p = 64, 4, 2, 50, 400
+    for kind in range(4):
+        pages = pr.filled_pool(lasad, 8, Hk, d, 12)
+        lift = [torch.arange(8.0), -torch.arange(8.0), torch.tensor([0, 9, -4, 3, 12, -20, 1, 0.0]), torch.zeros(8)][kind]
+        pages.k_scales.mul_((2 ** lift)[:, None].cuda())
+        pages.v_scales.mul_((2 ** -lift)[:, None].cuda())
+        if kind == 3:                                      # pages of zeros, held with scale 0, first and among others
+            for j in (0, 3):
+                for t in pages[:2]:
+                    t.view(torch.uint8)[j] = 0
+                for t in pages[2:]:
+                    t[j] = 0.0
+        for lengths, positions in (([n], [p]), ([1], [p])):
+            rows = packed(lengths, positions)
+            table = torch.arange(8, dtype=torch.int32)[None]
+            q = ref.draw((lengths[0], Hq, d), dt, 3).cuda()
+            t, pos, starts = on_gpu(table, rows, lengths == [1])
+            o = lasad.lasad_forward_pages(q, pages, t, pos, 2 ** 20, 0, row_starts=starts).cpu().double()
+            want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, 2 ** 20, 0, d ** -0.5, dt, dt)
+            assert ((o - want).abs() <= bound).all(), (kind, ((o - want).abs() / bound).max().item())
+
+
+def test_rows_that_share_pages(lasad):
+    """A common beginning lies in the tables of several rows."""
+    pages = pr.filled_pool(lasad, 8, 2, 64, 1)
+    table = torch.tensor([[0, 1, 2], [0, 1, 3], [0, 4, 5]], dtype=torch.int32)
+    rows = packed([1, 1, 1], [130, 140, 129])
+    q = ref.draw((3, 4, 64), BF, 3).cuda()
+    t, pos, _ = on_gpu(table, rows)
+    o = lasad.lasad_forward_pages(q, pages, t, pos, 1000).cpu().double()
+    want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, 1000, 0, 0.125, BF, BF)
+    assert ((o - want).abs() <= bound).all()
+
+
+# dtype, out dtype, d, Hq, Hk, positions, grid, rope, halves, weights, eps, window, sinks
+STEPS = [
+    (BF, BF, 64, 12, 12, [200], (16, 16), 2, False, "shared", EPS, 128, 1),
+    (BF, BF, 64, 6, 2, [0, 63, 64, 127, 1000, 5], (40, 40), 2, True, "heads", EPS, 96, 16),
+    (BF, F, 64, 4, 4, [63, 62, 700], (40, 40), 1, False, None, EPS, 2 ** 31 - 1, 0),
+    (F, F, 64, 4, 1, [0, 64, 321], (24, 23), 1, True, "shared", EPS, 100, 70),
+    (F, F, 32, 3, 3, [31, 500], (24, 23), 2, True, "heads", EPS, 1, 0),
+    (BF, BF, 32, 8, 2, [31, 500], (24, 23), 0, False, None, -1.0, 200, 3),
+    (BF, BF, 128, 4, 2, [65, 191], (24, 23), 2, False, "shared", EPS, 70, 0),
+    (F, F, 128, 2, 1, [128], (24, 23), 2, False, "shared", EPS, 70, 200),
+    (BF, BF, 64, 20, 1, [66, 128], (24, 23), 2, False, "shared", EPS, 90, 0),              # more query heads than a tile has columns
+    (BF, BF, 64, 2, 2, [5000, 4100], (100, 100), 2, False, "shared", EPS, 4000, 64),       # dealt out over workgroups
+    (F, F, 64, 2, 1, [5000, 4100], (100, 100), 2, False, "shared", EPS, 2 ** 30, 0),
+    (BF, BF, 128, 2, 2, [3000], (100, 100), 2, False, "shared", EPS, 4000, 64),
+]
+
+
+@pytest.mark.parametrize("case", range(len(STEPS)))
+def test_step(lasad, case):
+    """Pages as an append leaves them; o as attention over those pages of the queries of an append in fp32.  The queries are within their
+    bound of that, which moves a score by as much as the bound's share of |q| |k|."""
+    dt, odt, d, Hq, Hk, positions, grid, rope, halves, kind, eps, window, sinks = STEPS[case]
+    rows = [(b, 1, p) for b, p in enumerate(positions)]
+    B = len(rows)
+    need = sum(p // 64 + 1 for p in positions)
+    table = table_of(rows, need + 1, 8)
+    pages = pr.filled_pool(lasad, need + 1, Hk, d, 12)
+    spoil(pages, table, [(b, 1, p - 1) for b, p in enumerate(positions) if p] if all(positions) else rows)
+    before = cpu(pages)
+    q, k, v = (t.contiguous() for t in project(B, Hq, Hk, d, dt, 50 + case))
+    wq, wk = weights(Hq, Hk, d, kind)
+    t, pos, _ = on_gpu(table, rows)
+    yk, ek = expected(k, wk, rows, B, grid[1], rope, halves, eps, dt)
+    yq, eq = expected(q, wq, rows, B, grid[1], rope, halves, eps, dt)
+    for split in (True, False):
+        mine = lasad.Pages(*(x.clone().cuda() for x in before))
+        o = lasad.lasad_decode_step_pages(q, k, v, mine, t, pos, *grid, window, sinks, cuda(wq), cuda(wk), eps, rope, int(halves), BASE,
+                                          out_dtype=odt, use_workspace=split).cpu().double()
+        pr.check_append(before, cpu(mine), table, rows, grid[0] * grid[1], yk, ek, v.cpu().double())
+        want, bound = pr.attend(yq, cpu(mine), table, rows, LAST, window, sinks, d ** -0.5, dt, odt)
+        bound = bound + query_bound(yq, eq, cpu(mine), table, rows, window, sinks, d ** -0.5, dt)
+        assert ((o - want).abs() <= bound).all(), ((o - want).abs() / bound).max().item()
+
+
+def query_bound(yq, eq, pages, table, rows, window, sinks, scale, dt):
+    """What errors of the queries, `eq` and the rounding of a bf16 step's queries to 16 bits or more (2^-16 of them), add to o's error: a score is
+    off by s = scale sum (e |k|), a term by its exponential, and the sum by as much."""
+    e = eq + (2.0 ** -16 if dt == BF else 2.0 ** -24) * yq.abs()
+    kk, vv = pr.values(pages)
+    out = torch.zeros_like(yq)
+    for b, (_, _, p) in enumerate(rows):
+        j = torch.tensor([x for x in range(p + 1) if p - x < window or x < sinks])
+        page = table[b].long()[j // 64]
+        G = yq.shape[1] // kk.shape[1]
+        k, v = (x[page, :, j % 64].repeat_interleave(G, 1) for x in (kk, vv))               # [m, Hq, d]
+        off = (e[b] * k.abs()).sum(-1) * scale
+        prob = torch.softmax((yq[b] * k).sum(-1) * scale, 0)
+        worst = torch.expm1(2 * off.amax(0))
+        out[b] = (prob[..., None] * v.abs()).sum(0) * worst[:, None]
+    return out
+
+
+def test_step_inactive_rows(lasad):
+    positions = [-1, 100, 128, 127, 2 ** 31 - 1, 120]
+    B, d = 6, 64
+    table = torch.tensor([[0, 1], [2, 3], [4, 5], [6, 7], [8, 9], [10, -1]], dtype=torch.int32)
+    for grid, on in (((16, 16), [1, 3, 5]), ((11, 11), [1, 5])):
+        pages = pr.filled_pool(lasad, 12, 2, d, 12)
+        before = cpu(pages)
+        q, k, v = (t.contiguous() for t in project(B, 4, 2, d, BF, 5))
+        mark = torch.full((B, 4, d), 7.0, dtype=BF, device="cuda")
+        pos = torch.tensor(positions, dtype=torch.int32).cuda()
+        lasad.lasad_decode_step_pages(q, k, v, pages, table.cuda(), pos, *grid, 50, 3, out=mark)
+        left = [b for b in range(B) if b not in on]
+        assert (mark.cpu()[left] == 7.0).all() and not (mark.cpu()[on] == 7.0).all(-1).any()
+        rows = [(b, 1, p) for b, p in enumerate(positions)]
+        yk, ek = expected(k, None, [r if b in on else (b, 0, 0) for b, r in enumerate(rows)], B, grid[1], 2, False, EPS, BF)
+        pr.check_append(before, cpu(pages), table, rows, grid[0] * grid[1], yk, ek, v.cpu().double())
+
+
+def test_prompts_then_steps(lasad):
+    """As a server uses them: prompts of different lengths, then tokens one by one, against attention over what the cache should hold: the keys
+    and values themselves, each off by its rounding to 8 bits (2^-4; the normed keys' scores, with scale 1/8, by up to 2^-4 sum |q k| / 8)."""
+    d, Hq, Hk, W, window, sinks, steps = 64, 4, 2, 16, 60, 3, 70
+    lengths = [37, 100, 1]
+    B = 3
+    rows = packed(lengths, [0, 0, 0])
+    T = sum(lengths)
+    table = table_of([(0, n + steps, 0) for n in lengths], 12, 3)
+    pages = pr.new_pool(lasad, 12, Hk, d)
+    x = [ref.draw((n + steps, Hq + 2 * Hk, d), BF, 60 + b) for b, n in enumerate(lengths)]
+    first = torch.cat([t[:n] for t, n in zip(x, lengths)]).cuda()
+    t, pos, starts = on_gpu(table, rows)
+    q, k, v = first.split((Hq, Hk, Hk), 1)
+    q = lasad.lasad_append_pages(q, k, v, pages, t, pos, 16, W, row_starts=starts)
+    out = [[] for _ in range(B)]
+    o = lasad.lasad_forward_pages(q, pages, t, pos, window, sinks, row_starts=starts)
+    for b, (at, n, _) in enumerate(rows):
+        out[b].append(o[at:at + n].cpu())
+    for i in range(steps):
+        pos = torch.tensor([n + i for n in lengths], dtype=torch.int32).cuda()
+        q, k, v = (t.contiguous() for t in torch.stack([t[n + i] for t, n in zip(x, lengths)]).cuda().split((Hq, Hk, Hk), 1))
+        o = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, 16, W, window, sinks)
+        for b in range(B):
+            out[b].append(o[b:b + 1].cpu())
+    for b in range(B):
+        m = lengths[b] + steps
+        q, k, v = x[b].double().split((Hq, Hk, Hk), 1)
+        q, k = (ref.qk_row(y, None, torch.arange(m), W, 2, False, BASE, EPS) for y in (q, k))
+        mask = ref.seen_mask(m, m, 0, window, sinks)
+        want, lse = ref.window_forward(q[None], k[None], v[None], mask, 0.125)
+        bound, _ = ref.window_forward_bounds(q[None], k[None], v[None], mask, 0.125, BF, BF, want, lse)
+        # 8 bits: values 2^-4 each (twice below the normal codes); scores as said, and 2^-8 for the rounding of bf16 queries
+        ks = ref.shared(k[None], Hq)[0].abs()
+        score = torch.einsum("ihd,jhd->hij", q.abs(), ks) * 0.125 * (2.0 ** -4 + 2.0 ** -8)
+        score = score.masked_fill(~mask, 0.0).amax(-1).transpose(0, 1)[None, ..., None]
+        pv, _ = ref.window_forward(q[None], k[None], v[None].abs(), mask, 0.125)
+        bound = bound + pv * (torch.expm1(2 * score) * (1 + 2.0 ** -4) + 2.0 ** -4) + 2.0 ** -9
+        got = torch.cat(out[b]).double()[None]
+        assert ((got - want).abs() <= bound).all()
+        # and on the whole: e4m3 rounds a value by 2.6 % in the root mean square, a score of 64 such products with keys of 1 by
+        # 2.6 % too; together under 6 %
+        assert (got - want).norm() <= 0.06 * want.norm()
+
+
+def test_streams_and_devices(lasad):
+    """On another stream than the current one, with workspaces of the caching allocator."""
+    rows = [(0, 1, 5000), (1, 1, 4500)]
+    need = 160
+    table = table_of(rows, need, 8)
+    pages = pr.filled_pool(lasad, need, 2, 64, 12)
+    q, k, v = (t.contiguous() for t in project(2, 4, 2, 64, BF, 5))
+    t, pos, _ = on_gpu(table, rows)
+    want = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, 100, 100, 4000)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for _ in range(3):
+        a = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, 100, 100, 4000, stream=s)
+        with torch.cuda.stream(s):
+            b = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, 100, 100, 4000)
+            qr = lasad.lasad_append_pages(q, k, v, pages, t, pos, 100, 100)
+            c = lasad.lasad_forward_pages(qr, pages, t, pos, 4000)
+        s.synchronize()
+        assert torch.equal(a, want) and torch.equal(b, want)
+        assert (c.double() - want.double()).norm() <= 0.01 * want.double().norm()
+
+
+def test_graph_replays(lasad):
+    """A captured prompt and a captured step, replayed with other lengths, positions and tables than those they were captured with."""
+    d, Hq, Hk, B, T = 64, 4, 2, 3, 160
+    x = torch.zeros(T, Hq + 2 * Hk, d, dtype=BF, device="cuda")
+    y = torch.zeros(B, Hq + 2 * Hk, d, dtype=BF, device="cuda")
+    table = torch.full((B, 80), -1, dtype=torch.int32, device="cuda")
+    pos, starts = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros(B + 1, dtype=torch.int32, device="cuda")
+    pages = pr.filled_pool(lasad, 240, Hk, d, 1)
+
+    def prompt():
+        q, k, v = x.split((Hq, Hk, Hk), 1)
+        q = lasad.lasad_append_pages(q, k, v, pages, table, pos, 100, 100, row_starts=starts)
+        return lasad.lasad_forward_pages(q, pages, table, pos, 3000, 2, row_starts=starts)
+
+    def step():
+        q, k, v = (t.contiguous() for t in y.split((Hq, Hk, Hk), 1))
+        return lasad.lasad_decode_step_pages(q, k, v, pages, table, pos, 100, 100, 3000, 2)
+
+    graphs = []
+    for f in (prompt, step, step):
+        f()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            o = f()
+        graphs.append((g, o, f))
+    for seed, (lengths, positions) in enumerate((([5, 70, 1], [3, 60, 4000]), ([150, 0, 10], [0, 9, 2500]), ([1, 1, 1], [4900, 63, 64]))):
+        rows = packed(lengths, positions)
+        full = table_of(rows, 240, seed, width=80)
+        for g, o, f in graphs:
+            x.copy_(ref.draw(x.shape, BF, 70 + seed))
+            y.copy_(ref.draw(y.shape, BF, 80 + seed))
+            table.copy_(full)
+            pos.copy_(torch.tensor(positions, dtype=torch.int32))
+            starts.copy_(starts_of(rows))
+            start = [t.clone() for t in pages]
+            want = f()
+            left = [t.clone() for t in pages]
+            for _ in range(3):
+                for a, b in zip(pages, start):
+                    a.view(torch.uint8).copy_(b.view(torch.uint8))
+                o.fill_(9.0)
+                torch.cuda.synchronize()
+                g.replay()
+                torch.cuda.synchronize()
+                n = sum(lengths) if f is prompt else B
+                assert torch.equal(o[:n], want[:n]) and (f is not prompt or (o[n:] == 9.0).all())
+                for a, b in zip(pages, left):
+                    assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
