@@ -1212,6 +1212,10 @@ def lasad_append_pages(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor,
     lasad_forward_qk.  q [T, Hq, d], k, v [T, Hk, d]: views of packed tokens; row_starts: int32 [B + 1] on the device, None: one token a row;
     pos: position of the rows' first new token, an integer or an int32 tensor [B] on the device (off the grid or the table: inactive); table:
     int32 [B, pages].  Returns the normed and rotated queries (None without q); `out` may give them, q itself for in place."""
+    if q is not None and out is None and out_dtype is None and stream is None:
+        done = _fast("append_pages", q, k, v, pages, table, pos, grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base, row_starts)
+        if done is not None:
+            return done[0]
     if k.shape != v.shape or k.dtype != v.dtype:
         raise ValueError("k and v must have one shape and dtype")
     lk, lv = _packed(k, "k"), _packed(v, "v")
@@ -1256,6 +1260,10 @@ def lasad_forward_pages(q: torch.Tensor, pages: Pages, table: torch.Tensor, pos,
                         workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
     """lasad_forward_window of packed queries [T, Hq, d] (normed and rotated, their keys appended) over the rows' pages; rows, positions and
     table as in lasad_append_pages.  Queries of inactive rows and of none are left as they were in `out`."""
+    if out is None and out_dtype is None and workspace is None and use_workspace and stream is None:
+        done = _fast("forward_pages", q, pages, table, pos, window, sinks, row_starts, _scale(scale, q))
+        if done is not None:
+            return done[0]
     lq = _packed(q, "q")
     T, Hq, d = q.shape
     B, Hk = table.shape[0], pages[0].shape[1]
@@ -1293,6 +1301,11 @@ def lasad_decode_step_pages(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, p
                             workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
     """One token of every row: q [B, Hq, d], k, v [B, Hk, d] contiguous, as they leave the projection; norms, rotation, append to the
     pages and attention over them.  pos and table as in lasad_append_pages; an inactive row's output is not written."""
+    if out is None and out_dtype is None and workspace is None and use_workspace and stream is None:
+        done = _fast("decode_step_pages", q, k, v, pages, table, pos, grid_h, grid_w, q_weight, k_weight, norm_eps, rope, pairing, rope_base,
+                     window, sinks, _scale(scale, q))
+        if done is not None:
+            return done[0]
     B, Hq, d = q.shape
     _same(k, (v,), "k and v must be contiguous [B, Hk, d] of one shape and dtype")
     if not q.is_contiguous() or k.dim() != 3 or k.shape[0] != B or k.shape[2] != d or k.dtype != q.dtype:

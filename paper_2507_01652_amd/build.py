@@ -46,6 +46,7 @@ SOURCES = [
     "lasad_api_pages.hip",
     "lasad_pages_append.hip",
     "lasad_pages_attend.hip",
+    "lasad_pages_step.hip",
 ]
 
 # Packed-fp32 instruction selection is switched off for every HIP translation unit.

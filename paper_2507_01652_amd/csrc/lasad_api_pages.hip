@@ -46,10 +46,11 @@ bool known_rows(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int ta
            table_pages >= 1 && table_pages <= 1 << 24 && window >= 1 && sinks >= 0;
 }
 
-int splits(int B, int n_tokens, int n_q_heads, int n_k_heads, bool one_each, int table_pages, int window, int sinks)
+// Keys that a query sees at most.
+int64_t seen_keys(int table_pages, int window, int sinks)
 {
-    const int64_t held = (int64_t)table_pages * lasad::kPage, seen = (int64_t)window + sinks < held ? (int64_t)window + sinks : held;
-    return lasad::attend_pages_splits(B, n_tokens, n_q_heads, n_k_heads, one_each, seen);
+    const int64_t held = (int64_t)table_pages * lasad::kPage, seen = (int64_t)window + sinks;
+    return seen < held ? seen : held;
 }
 
 int check_workspace(void *workspace, size_t bytes, size_t need)
@@ -124,7 +125,7 @@ size_t lasad_forward_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, 
                                            int window, int sinks)
 {
     if (!known_rows(B, n_q_heads, n_k_heads, d, n_tokens, table_pages, window, sinks) || (one_each && n_tokens != B)) return 0;
-    return lasad::attend_pages_bytes(n_tokens, n_q_heads, d, splits(B, n_tokens, n_q_heads, n_k_heads, one_each, table_pages, window, sinks));
+    return lasad::attend_pages_bytes(n_tokens, n_q_heads, d, lasad::attend_pages_splits(B, n_tokens, n_q_heads, n_k_heads, one_each, seen_keys(table_pages, window, sinks)));
 }
 
 int lasad_forward_pages(const void *q, void *o, const lasad_layout_t *q_layout, const lasad_layout_t *o_layout, const lasad_pages_t *pages,
@@ -148,7 +149,7 @@ int lasad_forward_pages(const void *q, void *o, const lasad_layout_t *q_layout, 
     a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.Hq = n_q_heads; a.d = d;
     a.window = window; a.sinks = sinks; a.scale = scale;
     a.parts = (float *)workspace;
-    a.splits = workspace && need ? splits(B, n_tokens, n_q_heads, n_k_heads, !row_starts, pages->table_pages, window, sinks) : 1;
+    a.splits = workspace && need ? lasad::attend_pages_splits(B, n_tokens, n_q_heads, n_k_heads, !row_starts, seen_keys(pages->table_pages, window, sinks)) : 1;
     if (int rc = check_groups(lasad::attend_pages_groups(a))) return rc;
     const hipError_t e = lasad::launch_attend_pages(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_forward_pages launch", e);
@@ -157,7 +158,8 @@ int lasad_forward_pages(const void *q, void *o, const lasad_layout_t *q_layout, 
 
 size_t lasad_decode_step_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int table_pages, int window, int sinks)
 {
-    return lasad_forward_pages_workspace_bytes(B, n_q_heads, n_k_heads, d, B, 1, table_pages, window, sinks);
+    if (!known_rows(B, n_q_heads, n_k_heads, d, B, table_pages, window, sinks)) return 0;
+    return lasad::attend_pages_bytes(B, n_q_heads, d, lasad::step_pages_splits(B, n_q_heads, n_k_heads, seen_keys(table_pages, window, sinks)));
 }
 
 int lasad_decode_step_pages(const void *q, const void *k, const void *v, void *o, const lasad_pages_t *pages,
@@ -178,14 +180,13 @@ int lasad_decode_step_pages(const void *q, const void *k, const void *v, void *o
     if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
     lasad::AttendArgs a = {};
     a.pages = p.pages; a.rows = p.rows;
-    a.q = o; a.o = o; a.lq = lq; a.lo = lq;
-    a.io_dtype = out_dtype; a.out_dtype = out_dtype; a.Hq = n_q_heads; a.d = d;
+    a.o = o; a.lo = lq;
+    a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.Hq = n_q_heads; a.d = d;
     a.window = window; a.sinks = sinks; a.scale = scale;
     a.parts = (float *)workspace;
-    a.splits = workspace && need ? splits(B, B, n_q_heads, n_k_heads, true, pages->table_pages, window, sinks) : 1;
-    if (int rc = check_groups(lasad::attend_pages_groups(a))) return rc;
-    hipError_t e = lasad::launch_append_pages(p, (hipStream_t)hip_stream);
-    if (e == hipSuccess) e = lasad::launch_attend_pages(a, (hipStream_t)hip_stream);
+    a.splits = workspace && need ? lasad::step_pages_splits(B, n_q_heads, n_k_heads, seen_keys(pages->table_pages, window, sinks)) : 1;
+    if (int rc = check_groups(lasad::step_pages_groups(a))) return rc;
+    const hipError_t e = lasad::launch_step_pages(p, a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_decode_step_pages launch", e);
     return LASAD_OK;
 }

@@ -61,9 +61,15 @@ struct AttendArgs {
     int splits;
 };
 hipError_t launch_attend_pages(const AttendArgs &a, hipStream_t s);
+hipError_t launch_join_pages(const AttendArgs &a, hipStream_t s);          // of the splits
 int64_t attend_pages_groups(const AttendArgs &a);        // of a launch, splits included
 int attend_pages_splits(int64_t B, int64_t tokens, int Hq, int Hk, bool one_each, int64_t seen);
 size_t attend_pages_bytes(int64_t tokens, int Hq, int d, int splits);
+
+// One token of every row: a.k, a.v are appended, a.q are the queries; t.o, window, sinks, scale and splits of the attention.
+hipError_t launch_step_pages(const AppendArgs &a, const AttendArgs &t, hipStream_t s);
+int64_t step_pages_groups(const AttendArgs &t);
+int step_pages_splits(int64_t B, int Hq, int Hk, int64_t seen);
 
 // A row as a workgroup sees it.
 struct PageRow {

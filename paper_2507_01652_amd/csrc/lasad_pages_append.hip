@@ -9,7 +9,7 @@
 // A wavefront has one head of one page: all of its numbers are in registers (a lane has 8 channels of up to 64 / (512 / d) tokens in a row), so
 // that A is known before the first code is formed, with no wait for others.  Bound by memory: every number is read once, codes are written once.
 #include "lasad_heads.h"
-#include "lasad_pages.h"
+#include "lasad_pages_codes.h"
 
 namespace lasad {
 
@@ -23,67 +23,6 @@ __device__ inline float wave_max(float x)
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) x = fmaxf(x, __shfl_xor(x, off));
     return x;
-}
-
-__device__ inline float finite_size(float x) { return fabsf(x) < INFINITY ? fabsf(x) : 0.f; }
-
-// y / s rounded once more than exactly at most where it is halfway: a product with 1 / s and one correction.
-struct Divide {
-    float s, inv;
-    __device__ inline explicit Divide(float scale) : s(scale), inv(scale > 0.f ? 1.f / scale : 0.f) {}
-    __device__ inline float operator()(float y) const
-    {
-        const float t = y * inv;
-        return fmaf(fmaf(-t, s, y), inv, t);
-    }
-};
-
-__device__ inline uint32_t code2(float x, float y, uint32_t old, bool high)
-{
-    return high ? __builtin_amdgcn_cvt_pk_fp8_f32(x, y, old, true) : __builtin_amdgcn_cvt_pk_fp8_f32(x, y, old, false);
-}
-__device__ inline uint32_t code4(float x, float y, float z, float w) { return code2(z, w, code2(x, y, 0, false), true); }
-
-// Byte e of a word of codes divided (times `by`, a power of two), where `mask` has 0xff.
-__device__ inline uint32_t shrink(uint32_t w, float by, uint32_t mask)
-{
-    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-    const uint32_t r = code4(lo[0] * by, lo[1] * by, hi[0] * by, hi[1] * by);
-    return (r & mask) | (w & ~mask);
-}
-
-// The scale of a page whose `earlier` first positions were there before; where it grows, their codes are made smaller.  V: a page of values.
-template <int D, bool V>
-__device__ inline float page_scale(float most, int earlier, float *scale, uint8_t *codes, int lane)
-{
-    const float old = earlier > 0 ? *scale : 0.f;
-    float s;
-    if (!(old > 0.f)) {
-        s = most > 0.f ? fmaxf(most / kCodeTop, kLeastScale) : 0.f;
-    } else {
-        float by = 1.f;
-        s = old;
-        while (s * kCodeTop < most) {
-            s *= 2.f;
-            by *= 0.5f;
-        }
-        if (by < 1.f) {
-            uint32_t *words = (uint32_t *)codes;
-            for (int w = lane; w < kPage * D / 4; w += 64) {
-                uint32_t mask;
-                if (V) {
-                    const int t = 16 * (w % 4) + 4 * (w / 4 % 4);          // the word's first position
-                    mask = t + 4 <= earlier ? 0xffffffffu : t >= earlier ? 0u : (1u << 8 * (earlier - t)) - 1u;
-                } else {
-                    mask = w / (D / 4) < earlier ? 0xffffffffu : 0u;
-                }
-                if (mask) words[w] = shrink(words[w], by, mask);
-            }
-            __threadfence_block();                       // (a word of v may get one of the call's codes yet, from another lane)
-        }
-    }
-    if (lane == 0) *scale = s;
-    return s;
 }
 
 template <int BF16, int OBF16, int D>
@@ -154,6 +93,7 @@ append_pages_kernel(AppendArgs a, int groups)
             continue;
         }
         const int64_t ph = (int64_t)page * a.pages.heads + h;
+        bool grown;
         {
             float most = 0.f;
 #pragma unroll
@@ -161,7 +101,7 @@ append_pages_kernel(AppendArgs a, int groups)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size(y[u][e]));
             uint8_t *codes = a.pages.k + ph * kPage * D;
-            const Divide by(page_scale<D, false>(wave_max(most), begin, a.pages.k_scale + ph, codes, lane));
+            const Divide by(page_scale<D, false>(wave_max(most), begin, a.pages.k_scale[ph], a.pages.k_scale + ph, codes, lane, grown));
 #pragma unroll
             for (int u = 0; u < TPL; ++u)
                 if (here(u))
@@ -182,7 +122,7 @@ append_pages_kernel(AppendArgs a, int groups)
             for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size(y[u][e]));
         }
         uint8_t *codes = a.pages.v + ph * kPage * D;
-        const Divide by(page_scale<D, true>(wave_max(most), begin, a.pages.v_scale + ph, codes, lane));
+        const Divide by(page_scale<D, true>(wave_max(most), begin, a.pages.v_scale[ph], a.pages.v_scale + ph, codes, lane, grown));
 #pragma unroll
         for (int u = 0; u < TPL; u += 4) {
             const int t = slot0 + u, at = 16 * (t / 4 % 4) + 4 * (t / 16);         // place of four positions in a channel's 64

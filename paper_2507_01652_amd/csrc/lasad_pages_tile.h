@@ -1,0 +1,369 @@
+// A page's keys and values against tiles of 16 columns, as matrix operands straight from memory (lasad_pages_attend.hip has the formulas): what the
+// attention of packed queries and the step share.
+#pragma once
+
+#include "lasad_pages.h"
+
+namespace lasad {
+
+// Sum or maximum of a column's four lanes, in each of them.
+__device__ inline float quads_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return both_halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline float quads_sum(float x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return both_halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+// Four codes as bf16.
+__device__ inline uint2 codes_bf16(uint32_t w)
+{
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)));
+}
+__device__ inline Frag codes_frag(uint32_t lo, uint32_t hi)
+{
+    Frag f;
+    f.h[0] = codes_bf16(lo);
+    f.h[1] = codes_bf16(hi);
+    return f;
+}
+
+// x in N bf16 parts, each the rounding of what those before it leave.
+template <int N>
+__device__ inline void split_pair(float x, float y, uint32_t (&part)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        part[i] = pack2(x, y);
+        x -= __uint_as_float(part[i] << 16);
+        y -= __uint_as_float(part[i] & 0xffff0000u);
+    }
+}
+
+__device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }     // 0x80 where a code is NaN
+
+// A lane's share of a page: k of four blocks of 16 positions (its position of each, 16 channels of 64), v of all positions that the second
+// product has in its lane (its channel of every 16).
+template <int D>
+struct PagePart {
+    static constexpr int KW = D / 16;                    // words of k of a block
+    uint32_t k[4][KW];
+    uint4 v[D / 16];
+    float k_scale, v_scale;
+    __device__ inline void load_k(const Pages &p, int page, int h, int lane)
+    {
+        const int64_t at = (int64_t)page * p.heads + h;
+        const int col = lane & 15, quad = lane >> 4;
+        const uint8_t *kp = p.k + at * kPage * D + col * D;
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            if (D == 32) {
+                const uint2 x = *(const uint2 *)(kp + b * 16 * D + quad * 8);
+                k[b][0] = x.x; k[b][1] = x.y;
+            } else {
+#pragma unroll
+                for (int c = 0; c < D / 64; ++c) {
+                    const uint4 x = *(const uint4 *)(kp + b * 16 * D + c * 64 + quad * 16);
+                    k[b][4 * c % KW] = x.x; k[b][(4 * c + 1) % KW] = x.y; k[b][(4 * c + 2) % KW] = x.z; k[b][(4 * c + 3) % KW] = x.w;
+                }
+            }
+        }
+        k_scale = p.k_scale[at];
+    }
+    __device__ inline void load_v(const Pages &p, int page, int h, int lane)
+    {
+        const int64_t at = (int64_t)page * p.heads + h;
+        const uint8_t *vp = p.v + at * kPage * D + (lane & 15) * kPage + (lane >> 4) * 16;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) v[c] = *(const uint4 *)(vp + c * 16 * kPage);
+        v_scale = p.v_scale[at];
+    }
+};
+// first of a lane's eight channels in reduction step f of the first product
+template <int D>
+__device__ inline int page_channel(int f, int quad) { return D == 32 ? 8 * quad : 64 * (f >> 1) + 16 * quad + 8 * (f & 1); }
+
+// A wavefront's columns: NT tiles of 16, this lane's column of each.  SHARE > 1, for fewer queries than a tile has columns: 16 / SHARE queries
+// lie in it SHARE times, and copy i keeps those scores alone whose block of 16 positions is i modulo SHARE.  Its sums are over those, as if it
+// were another wavefront's, and a lane has 16 / SHARE scores of a page to raise to a power instead of 16.
+template <int D, int NQ, int NP, int NT, int SHARE = 1>
+struct Columns {
+    static constexpr int NF = D / 32, NC = D / 16, NB = 4 / SHARE;        // NB: blocks of a lane
+    static_assert(SHARE == 1 || NT == 1, "copies of one tile");
+    Frag q[NT][NF][NQ];
+    int p[NT];                                           // position (-1: no column)
+    int p0, p1;                                          // first and last position of the wavefront's columns
+    float m[NT], l[NT];
+    f32x4v acc[NT][NC];
+
+    // Page number j of the row, in `t`: what its keys add.  Once its keys are used, and its values, next_k and next_v load those of the next page
+    // in their place, so that loads are in flight all the time with one set of registers.
+    template <typename K, typename V>
+    __device__ inline void take(PagePart<D> &t, int j, float scale2, int window, int sinks, int lane, K next_k, V next_v)
+    {
+        const int quad = lane >> 4, j0 = j * kPage;
+        const bool edge = j0 + kPage - 1 > p0 || (j0 <= p1 - window && j0 + kPage > sinks);
+        const float sc = fmaxf(t.k_scale * scale2, 0x1p-126f);       // (a page of zeros has scale 0, and 0 times -infinity is none)
+        const int copy = SHARE > 1 ? (lane & 15) / (16 / SHARE) : 0, own = 4 * quad + 16 * copy;      // (a lane's block r is number SHARE r + copy)
+        f32x4v s[NT][NB];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            Frag k[NF];
+#pragma unroll
+            for (int f = 0; f < NF; ++f) k[f] = codes_frag(t.k[b][2 * f], t.k[b][2 * f + 1]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4v x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = NQ - 1; i >= 0; --i)
+#pragma unroll
+                    for (int f = 0; f < NF; ++f) x = mfma16(k[f], q[n][f][i], x);
+                if (b % SHARE == 0) {
+                    s[n][b / SHARE] = x;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[n][b / SHARE][i] = copy == b % SHARE ? x[i] : s[n][b / SHARE][i];
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);               // (loads moved up over the products, or conversions over the exponentials, would need registers)
+        next_k();
+        if (edge) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int hi = p[n] - j0 - own, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
+#pragma unroll
+                for (int r = 0; r < NB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = 16 * SHARE * r + i;
+                        if (at > hi || (at < lo && at >= first)) s[n][r][i] = -INFINITY;
+                    }
+            }
+        }
+        float top[NT];
+        bool grows = false;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            top[n] = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < NB; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top[n] = fmaxf(top[n], s[n][r][i]);
+            top[n] = quads_max(top[n]) * sc;
+            grows |= top[n] > m[n] + kSlack;
+        }
+        if (__any(grows)) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const float m1 = top[n] > m[n] + kSlack ? top[n] : m[n];
+                const float fade = m[n] == m1 ? 1.f : __builtin_amdgcn_exp2f(m[n] - m1);
+                m[n] = m1;
+                l[n] *= fade;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][c][i] *= fade;
+            }
+        }
+        Frag pf[NT][2][NP];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float use = m[n] == -INFINITY ? 0.f : m[n];        // (nothing seen yet: every term is 2^-inf)
+            float sum = 0.f;
+            uint32_t part[NB][2][NP];
+#pragma unroll
+            for (int r = 0; r < NB; ++r) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float e = __builtin_amdgcn_exp2f(fmaf(s[n][r][i], sc, -use));
+                    sum += e;
+                    s[n][r][i] = e * t.v_scale;
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) split_pair<NP>(s[n][r][2 * i], s[n][r][2 * i + 1], part[r][i]);
+            }
+            l[n] += sum;
+#pragma unroll
+            for (int x = 0; x < NP; ++x) {
+                uint2 w[NB];
+#pragma unroll
+                for (int r = 0; r < NB; ++r) w[r] = make_uint2(part[r][0][x], part[r][1][x]);
+                spread(w, copy, pf[n][0][x], pf[n][1][x]);
+            }
+        }
+        // A code that not every column sees may be NaN (what is not yet written is anything), and 0 * NaN would reach the sums: such codes
+        // are 0 in the product, and the columns that do see one get their NaN from a product of flags.
+        if (edge) {
+            uint32_t bad = 0;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) bad |= nan_bytes(t.v[c].x) | nan_bytes(t.v[c].y) | nan_bytes(t.v[c].z) | nan_bytes(t.v[c].w);
+            if (__any(bad != 0)) take_nan_out(t, j0, window, sinks, copy, own);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const Frag v = half ? codes_frag(t.v[c].z, t.v[c].w) : codes_frag(t.v[c].x, t.v[c].y);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int x = NP - 1; x >= 0; --x) acc[n][c] = mfma16(v, pf[n][half][x], acc[n][c]);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        next_v();
+    }
+
+    // A lane's blocks, four bf16 of each, as the operands of the second product: 0 where a block is another copy's.
+    static __device__ inline void spread(const uint2 (&w)[NB], int copy, Frag &low, Frag &high)
+    {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const bool mine = SHARE == 1 || copy == b % SHARE;
+            (b < 2 ? low : high).h[b & 1] = make_uint2(mine ? w[b / SHARE].x : 0u, mine ? w[b / SHARE].y : 0u);
+        }
+    }
+
+    __device__ inline void take_nan_out(PagePart<D> &t, int j0, int window, int sinks, int copy, int own)
+    {
+        Frag seen[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int hi = p[n] - j0 - own, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
+            uint2 w[NB];
+#pragma unroll
+            for (int r = 0; r < NB; ++r) {
+                uint32_t on[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = 16 * SHARE * r + i;
+                    on[i] = at > hi || (at < lo && at >= first) ? 0u : 0x3f80u;
+                }
+                w[r] = make_uint2(on[0] | on[1] << 16, on[2] | on[3] << 16);
+            }
+            spread(w, copy, seen[n][0], seen[n][1]);
+        }
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            uint32_t w[4] = {t.v[c].x, t.v[c].y, t.v[c].z, t.v[c].w}, flag[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t nan = nan_bytes(w[i]) >> 7;
+                w[i] &= ~(nan * 0xffu);
+                flag[i] = nan * 0x38u;                               // (the code of 1)
+            }
+            t.v[c] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                f32x4v count = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) count = mfma16(codes_frag(flag[2 * half], flag[2 * half + 1]), seen[n][half], count);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (count[i] > 0.f) acc[n][c][i] = __builtin_nanf("");
+            }
+        }
+    }
+};
+
+// Eight channels of a query as the parts of a fragment.
+template <typename T, int NQ>
+__device__ inline void query_parts(const T *p, Frag (&f)[NQ])
+{
+    if constexpr (sizeof(T) == 2) {
+        f[0].u = *(const uint4 *)p;
+    } else {
+        const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+        uint32_t part[4][NQ];
+        split_pair<NQ>(a.x, a.y, part[0]);
+        split_pair<NQ>(a.z, a.w, part[1]);
+        split_pair<NQ>(b.x, b.y, part[2]);
+        split_pair<NQ>(b.z, b.w, part[3]);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) f[i].u = make_uint4(part[0][i], part[1][i], part[2][i], part[3][i]);
+    }
+}
+
+// The pages that positions p0 .. p1 see: those of the sinks before the window's, then the window's.
+struct PageList {
+    int sink_pages, first, count;
+    __device__ inline PageList(int p0, int p1, int window, int sinks)
+    {
+        first = max(0, p0 - window + 1) / kPage;
+        sink_pages = min((int)(((int64_t)sinks + kPage - 1) / kPage), first);
+        count = p1 < 0 ? 0 : sink_pages + p1 / kPage - first + 1;
+    }
+    __device__ inline int number(int i) const { return i < sink_pages ? i : first + i - sink_pages; }
+};
+
+// The pages that a wavefront takes, every `step`th from `begin` on: their numbers in the pool are loaded 64 at a time.
+struct Walk {
+    int ids, base;
+    __device__ inline void fill(const Pages &p, const PageList &list, int b, int i, int step)
+    {
+        const int at = i + (int)(threadIdx.x & 63) * step;
+        base = i;
+        ids = at < list.count ? page_of(p, b, list.number(at)) : -1;
+    }
+    __device__ inline int page(const Pages &p, const PageList &list, int b, int i, int step)
+    {
+        const int n = (i - base) / step;
+        if (n < 64) return __builtin_amdgcn_readlane(ids, n);
+        fill(p, list, b, i, step);
+        return __builtin_amdgcn_readlane(ids, 0);
+    }
+};
+
+// The sums of KW wavefronts (and of SHARE copies in each) that share columns, joined in `red` and put out: results (of splits: parts) of
+// `columns` of them, to where `to` says.
+template <typename O>
+struct Result {
+    float *parts;                                        // of the column's splits
+    O *o;                                                // its channels from `ch` on
+};
+template <typename O, int D, int KW, int SHARE, typename To>
+__device__ inline void join_waves(float (&red)[KW][16][D + 4], const f32x4v (&acc)[D / 16], float m, float l, int kw, int lane, int columns, int splits,
+                                  int split, To to)
+{
+    const int quad = lane >> 4;
+    float *mine = red[kw][lane & 15];
+#pragma unroll
+    for (int b = 0; b < D / 16; ++b) *(float4 *)(mine + 16 * b + 4 * quad) = make_float4(acc[b][0], acc[b][1], acc[b][2], acc[b][3]);
+    if (quad == 0) { mine[D] = m; mine[D + 1] = l; }
+    __syncthreads();
+    constexpr int EACH = 16 / SHARE;
+    for (int i = threadIdx.x; i < EACH * D / 4; i += KW * 64) {
+        const int c = i / (D / 4), ch = i % (D / 4) * 4;
+        if (c >= columns) continue;
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < KW * SHARE; ++w) top = fmaxf(top, red[w / SHARE][c + w % SHARE * EACH][D]);
+        const float use = top == -INFINITY ? 0.f : top;
+        float sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < KW * SHARE; ++w) {
+            const float *x = red[w / SHARE][c + w % SHARE * EACH];
+            const float f = __builtin_amdgcn_exp2f(x[D] - use);
+            const float4 r = *(const float4 *)(x + ch);
+            sum = fmaf(x[D + 1], f, sum);
+            o.x = fmaf(r.x, f, o.x); o.y = fmaf(r.y, f, o.y); o.z = fmaf(r.z, f, o.z); o.w = fmaf(r.w, f, o.w);
+        }
+        const Result<O> r = to(c, ch);
+        if (splits > 1) {
+            float *p = r.parts + split * (D + 4);
+            *(float4 *)(p + ch) = o;
+            if (ch == 0) { p[D] = top; p[D + 1] = sum; }
+        } else {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            store4(r.o, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        }
+    }
+}
+
+}  // namespace lasad

@@ -458,7 +458,8 @@ struct QkOptions {                                 // grid_h, grid_w, q_weight, 
     int gh, gw, shared = -1, rope, pairing;
     const float *wq, *wk;
     float eps, base;
-    QkOptions(const Pair &p, PyObject *const *a)
+    template <typename P>
+    QkOptions(const P &p, PyObject *const *a)
     {
         gh = integer(a[0]); gw = integer(a[1]);
         wq = head_weight(a[2], p.Hq, p.d, shared); wk = head_weight(a[3], p.Hk, p.d, shared);
@@ -637,6 +638,126 @@ PyObject *decode_step_window(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- a cache in pages ----
+
+lasad_layout_t packed(const at::Tensor &t)
+{
+    if (t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1)) throw NotHandled();
+    return {0, t.size(0) > 1 ? t.stride(0) : 0, t.size(1) > 1 ? t.stride(1) : 0};
+}
+
+// (k, v, k_scales, v_scales) of a pool and the rows' table [B, pages]
+lasad_pages_t pool(PyObject *o, PyObject *ot, int Hk, int d, int &B)
+{
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) throw NotHandled();
+    const at::Tensor &k = tensor(PyTuple_GET_ITEM(o, 0)), &v = tensor(PyTuple_GET_ITEM(o, 1));
+    const at::Tensor &ks = tensor(PyTuple_GET_ITEM(o, 2)), &vs = tensor(PyTuple_GET_ITEM(o, 3)), &t = any_strides(ot);
+    if (k.dim() != 4 || v.dim() != 4 || k.scalar_type() != at::kFloat8_e4m3fn || v.scalar_type() != at::kFloat8_e4m3fn) throw NotHandled();
+    const int64_t n = k.size(0);
+    if (k.size(1) != Hk || k.size(2) != 64 || k.size(3) != d || v.size(0) != n || v.size(1) != Hk || v.size(2) != d || v.size(3) != 64) throw NotHandled();
+    for (const at::Tensor *x : {&ks, &vs})
+        if (x->scalar_type() != at::kFloat || x->dim() != 2 || x->size(0) != n || x->size(1) != Hk) throw NotHandled();
+    if (t.scalar_type() != at::kInt || t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) throw NotHandled();
+    B = narrow(t.size(0));
+    return {(uint8_t *)k.data_ptr(), (uint8_t *)v.data_ptr(), (float *)ks.data_ptr(), (float *)vs.data_ptr(), narrow(n), narrow(t.size(1)),
+            (const int32_t *)t.data_ptr(), B > 1 ? t.stride(0) : 0};
+}
+
+const int32_t *row_starts(PyObject *o, int B)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = tensor(o);
+    if (t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) != (int64_t)B + 1) throw NotHandled();
+    return (const int32_t *)t.data_ptr();
+}
+
+struct Packed {                                    // q and k of packed tokens: everything alike but the heads
+    const at::Tensor &q, &k;
+    int T, Hq, Hk, d, io;
+    Packed(PyObject *oq, PyObject *ok) : q(any_strides(oq)), k(any_strides(ok))
+    {
+        if (q.dim() != 3 || k.dim() != 3 || q.scalar_type() != k.scalar_type() || q.size(0) != k.size(0) || q.size(2) != k.size(2)) throw NotHandled();
+        T = narrow(q.size(0)); Hq = narrow(q.size(1)); Hk = narrow(k.size(1)); d = narrow(q.size(2));
+        io = code(q);
+    }
+};
+
+// q, k, v, pages, table, pos, [8 options], row_starts
+PyObject *append_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 15, [&](at::Tensor (&g)[4], int &count) {
+        const Packed p(a[0], a[1]);
+        const at::Tensor &v = any_strides(a[2]);
+        if (v.sizes() != p.k.sizes() || v.scalar_type() != p.k.scalar_type()) throw NotHandled();
+        int B, pos;
+        const lasad_pages_t pages = pool(a[3], a[4], p.Hk, p.d, B);
+        const int32_t *pos_rows = row_positions(a[5], B, pos);
+        const QkOptions o(p, a + 6);
+        const int32_t *starts = row_starts(a[14], B);
+        const lasad_layout_t lq = packed(p.q), lk = packed(p.k), lv = packed(v);
+        count = 1;
+        g[0] = dense(p.q);
+        const lasad_layout_t lo = packed(g[0]);
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_append_pages(p.q.data_ptr(), p.k.data_ptr(), v.data_ptr(), g[0].data_ptr(), &lq, &lk, &lv, &lo, &pages, p.io, p.io, B, p.Hq,
+                                              p.Hk, p.d, o.gh, o.gw, p.T, starts, pos, pos_rows, o.wq, o.wk, o.shared, o.eps, o.rope, o.pairing, o.base, st));
+    });
+}
+
+// q, pages, table, pos, window, sinks, row_starts, scale
+PyObject *forward_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 8, [&](at::Tensor (&g)[4], int &count) {
+        const at::Tensor &q = any_strides(a[0]);
+        const lasad_layout_t lq = packed(q);
+        if (!PyTuple_Check(a[1]) || PyTuple_GET_SIZE(a[1]) != 4) throw NotHandled();
+        const at::Tensor &k = tensor(PyTuple_GET_ITEM(a[1], 0));
+        if (k.dim() != 4) throw NotHandled();
+        const int T = narrow(q.size(0)), Hq = narrow(q.size(1)), d = narrow(q.size(2)), Hk = narrow(k.size(1)), io = code(q);
+        int B, pos;
+        const lasad_pages_t pages = pool(a[1], a[2], Hk, d, B);
+        const int32_t *pos_rows = row_positions(a[3], B, pos);
+        const int window = integer(a[4]), sinks = integer(a[5]);
+        const int32_t *starts = row_starts(a[6], B);
+        const float scale = real(a[7]);
+        count = 1;
+        g[0] = dense(q);
+        const lasad_layout_t lo = packed(g[0]);
+        const size_t need = lasad_forward_pages_workspace_bytes(B, Hq, Hk, d, T, !starts, pages.table_pages, window, sinks);
+        at::Tensor ws;
+        if (need) ws = at::empty({(int64_t)need}, q.options().dtype(at::kByte));
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_forward_pages(q.data_ptr(), g[0].data_ptr(), &lq, &lo, &pages, io, io, B, Hq, Hk, d, T, starts, pos, pos_rows, window, sinks,
+                                               scale, need ? ws.data_ptr() : nullptr, need, st));
+    });
+}
+
+// q, k, v, pages, table, pos, [8 options], window, sinks, scale
+PyObject *decode_step_pages(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return gradients(n, 17, [&](at::Tensor (&g)[4], int &count) {
+        const Packed p(a[0], a[1]);
+        const at::Tensor &v = tensor(a[2]);
+        if (!p.q.is_contiguous() || !p.k.is_contiguous() || v.sizes() != p.k.sizes() || v.scalar_type() != p.k.scalar_type()) throw NotHandled();
+        int B, pos;
+        const lasad_pages_t pages = pool(a[3], a[4], p.Hk, p.d, B);
+        if (B != p.T) throw NotHandled();
+        const int32_t *pos_rows = row_positions(a[5], B, pos);
+        const QkOptions o(p, a + 6);
+        const int window = integer(a[14]), sinks = integer(a[15]);
+        const float scale = real(a[16]);
+        count = 1;
+        g[0] = dense(p.q);
+        const size_t need = lasad_decode_step_pages_workspace_bytes(B, p.Hq, p.Hk, p.d, pages.table_pages, window, sinks);
+        at::Tensor ws;
+        if (need) ws = at::empty({(int64_t)need}, p.q.options().dtype(at::kByte));
+        void *st = stream(Py_None);
+        return WITHOUT_GIL(lasad_decode_step_pages(p.q.data_ptr(), p.k.data_ptr(), v.data_ptr(), g[0].data_ptr(), &pages, p.io, p.io, B, p.Hq, p.Hk, p.d, o.gh,
+                                                   o.gw, pos, pos_rows, o.wq, o.wk, o.shared, o.eps, o.rope, o.pairing, o.base, window, sinks, scale,
+                                                   need ? ws.data_ptr() : nullptr, need, st));
+    });
+}
+
 PyMethodDef methods[] = {
     {"decode_step", (PyCFunction)(void (*)(void))decode_step, METH_FASTCALL, nullptr},
     {"decode_step_gated", (PyCFunction)(void (*)(void))decode_step_gated, METH_FASTCALL, nullptr},
@@ -654,6 +775,9 @@ PyMethodDef methods[] = {
     {"forward_window", (PyCFunction)(void (*)(void))forward_window, METH_FASTCALL, nullptr},
     {"backward_window", (PyCFunction)(void (*)(void))backward_window, METH_FASTCALL, nullptr},
     {"decode_step_window", (PyCFunction)(void (*)(void))decode_step_window, METH_FASTCALL, nullptr},
+    {"append_pages", (PyCFunction)(void (*)(void))append_pages, METH_FASTCALL, nullptr},
+    {"forward_pages", (PyCFunction)(void (*)(void))forward_pages, METH_FASTCALL, nullptr},
+    {"decode_step_pages", (PyCFunction)(void (*)(void))decode_step_pages, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_steps", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
