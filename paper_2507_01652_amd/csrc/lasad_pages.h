@@ -109,6 +109,11 @@ __device__ inline bool find_row(const PageRows &r, const Pages &pages, int slot,
         row.n = 1;
     }
     row.pos = r.pos_rows ? r.pos_rows[row.b] : r.pos;
+    row.b = __builtin_amdgcn_readfirstlane(row.b);       // (the same in all lanes; so that the compiler knows)
+    row.first = __builtin_amdgcn_readfirstlane(row.first);
+    row.n = __builtin_amdgcn_readfirstlane(row.n);
+    row.pos = __builtin_amdgcn_readfirstlane(row.pos);
+    row.unit = __builtin_amdgcn_readfirstlane(row.unit);
     return row.n > 0 && row.pos >= 0 && (int64_t)row.pos + row.n <= min((int64_t)r.last_pos, (int64_t)pages.table_pages * kPage);
 }
 inline int64_t row_slots(const PageRows &r, int num, int den, int extra)

@@ -9,13 +9,16 @@
 // applied to the scores and to P in fp32.  fp32 queries and P are three bf16 parts each.
 #include "lasad_pages_tile.h"
 
+#ifndef LASAD_NT
+#define LASAD_NT 2
+#endif
 namespace lasad {
 
 namespace {
 
 // Workgroup: WAVES wavefronts, CW of them beside each other over CW * NT * 16 columns of a row's key head, WAVES / CW over the pages.
 template <typename T, typename O, int D, int NQ, int NP, int NT, int CW, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, NT > 1 || D == 128 ? 1 : 2)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 && sizeof(T) == 4 ? 1 : 2)
 attend_pages_kernel(AttendArgs a)
 {
     constexpr int KW = WAVES / CW, COLS = CW * NT * 16, NC = D / 16, NF = D / 32;
@@ -30,8 +33,8 @@ attend_pages_kernel(AttendArgs a)
     const int cw = wave % CW, kw = wave / CW, c0 = group0 + cw * NT * 16;
 
     Columns<D, NQ, NP, NT> x;
-    x.p0 = row.pos + c0 / G;
-    x.p1 = c0 < columns ? row.pos + (min(c0 + NT * 16, columns) - 1) / G : -1;
+    x.p0 = __builtin_amdgcn_readfirstlane(row.pos + c0 / G);
+    x.p1 = __builtin_amdgcn_readfirstlane(c0 < columns ? row.pos + (min(c0 + NT * 16, columns) - 1) / G : -1);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int c = c0 + 16 * n + col, token = c / G, h = hk * G + c - token * G;
@@ -51,26 +54,19 @@ attend_pages_kernel(AttendArgs a)
     int i = split * KW + kw;
     Walk walk;
     walk.fill(a.pages, list, row.b, i, step);
-    int page = walk.page(a.pages, list, row.b, i, step);
+    int page = walk.next(a.pages, list, row.b, i, step);
     PagePart<D> t;
     const auto load_k = [&] { t.load_k(a.pages, max(page, 0), hk, lane); };
     const auto load_v = [&] { t.load_v(a.pages, max(page, 0), hk, lane); };
     load_k();
     load_v();
     while (i < list.count) {
-        const int j = list.number(i);
+        const int j = __builtin_amdgcn_readfirstlane(list.number(i));
         const bool there = page >= 0;
         i += step;
-        if (i < list.count) page = walk.page(a.pages, list, row.b, i, step);               // (behind the last page that one again)
-        if (there) {
-            x.take(t, j, scale2, a.window, a.sinks, lane, load_k, load_v);
-        } else {
-            load_k();
-            load_v();
-        }
+        if (i < list.count) page = walk.next(a.pages, list, row.b, i, step);               // (behind the last page that one again)
+        x.take(t, j, there, scale2, a.window, a.sinks, lane, load_k, load_v);
     }
-#pragma unroll
-    for (int n = 0; n < NT; ++n) x.l[n] = quads_sum(x.l[n]);
 
     if constexpr (KW == 1) {
 #pragma unroll
@@ -170,7 +166,7 @@ Shape choose(const AttendArgs &a)
 {
     const int64_t columns = (int64_t)a.rows.tokens * (a.Hq / a.pages.heads);
     if (columns <= 32 * (int64_t)a.rows.B) return {1, 1, 4};
-    return {a.io_dtype == LASAD_BF16 && a.d <= 64 ? 2 : 1, 4, 4};
+    return {a.io_dtype == LASAD_BF16 && a.d <= 64 ? LASAD_NT : 1, 4, 4};
 }
 int64_t groups_of(const AttendArgs &a, const Shape &s) { return row_slots(a.rows, a.Hq / a.pages.heads, s.columns(), 1) * a.pages.heads; }
 
@@ -185,7 +181,7 @@ hipError_t launch(const AttendArgs &a, hipStream_t s)
 {
     const Shape shape = choose(a);
     const dim3 grid((unsigned)groups_of(a, shape), (unsigned)a.splits);
-    constexpr int WIDE = sizeof(T) == 2 && D <= 64 ? 2 : 1;
+    constexpr int WIDE = sizeof(T) == 2 && D <= 64 ? LASAD_NT : 1;
     if (shape.cw == 1) attend_pages_kernel<T, O, D, NP, NP, 1, 1, 4><<<grid, dim3(256), 0, s>>>(a);
     else attend_pages_kernel<T, O, D, NP, NP, WIDE, 4, 4><<<grid, dim3(256), 0, s>>>(a);
     hipError_t e = hipGetLastError();

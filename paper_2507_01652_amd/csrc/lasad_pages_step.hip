@@ -211,7 +211,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
     }
     if (a.rope != LASAD_ROPE_NONE && threadIdx.x < P)
         cs[threadIdx.x] = pair_angle<D>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
-    int page = walk.page(a.pages, list, b, begin, step);
+    int page = walk.next(a.pages, list, b, begin, step);
     PagePart<D> t;
     const auto load_k = [&] { t.load_k(a.pages, max(page, 0), hk, lane); };
     const auto load_v = [&] { t.load_v(a.pages, max(page, 0), hk, lane); };
@@ -227,7 +227,8 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         if (g0 > 0) {
             __syncthreads();                             // (the sums of the heads before are out of LDS)
             rq.load(queries + min(g0 + col % EACH, G - 1) * D, quad);
-            page = walk.page(a.pages, list, b, begin, step);
+            walk.fill(a.pages, list, b, begin, step);
+            page = walk.next(a.pages, list, b, begin, step);
             load_k();
             load_v();
         }
@@ -252,7 +253,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         for (int c = 0; c < NC; ++c) x.acc[0][c] = f32x4v{0.f, 0.f, 0.f, 0.f};
         int i = begin;
         while (i < list.count) {
-            const int j = list.number(i);
+            const int j = __builtin_amdgcn_readfirstlane(list.number(i));
             const bool there = page >= 0;
             if (i == list.count - 1 && there) {
                 if (fresh.grown) {
@@ -262,15 +263,10 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
                 fresh.put(t, pos % kPage, lane);
             }
             i += step;
-            if (i < list.count) page = walk.page(a.pages, list, b, i, step);               // (behind the last page that one again)
-            if (there) {
-                x.take(t, j, g.scale * kLog2e, g.window, g.sinks, lane, load_k, load_v);
-            } else {
-                load_k();
-                load_v();
-            }
+            if (i < list.count) page = walk.next(a.pages, list, b, i, step);               // (behind the last page that one again)
+            x.take(t, j, there, g.scale * kLog2e, g.window, g.sinks, lane, load_k, load_v);
         }
-        join_waves<O, D, WAVES, SHARE>(red, x.acc[0], x.m[0], quads_sum(x.l[0]), wave, lane, min(EACH, G - g0), g.splits, split, [&](int c, int ch) {
+        join_waves<O, D, WAVES, SHARE>(red, x.acc[0], x.m[0], x.total(0), wave, lane, min(EACH, G - g0), g.splits, split, [&](int c, int ch) {
             const int64_t at = (int64_t)b * a.Hq + hk * G + g0 + c;
             return Result<O>{g.parts + at * g.splits * (D + 4), (O *)g.o + at * D + ch};
         });

@@ -18,17 +18,17 @@ __device__ inline float quads_sum(float x)
     return both_halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-// Four codes as bf16.
-__device__ inline uint2 codes_bf16(uint32_t w)
+// Four codes as bf16, times a power of two.
+__device__ inline uint2 codes_bf16(uint32_t w, float scale)
 {
-    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)));
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
 }
-__device__ inline Frag codes_frag(uint32_t lo, uint32_t hi)
+__device__ inline Frag codes_frag(uint32_t lo, uint32_t hi, float scale = 1.f)
 {
     Frag f;
-    f.h[0] = codes_bf16(lo);
-    f.h[1] = codes_bf16(hi);
+    f.h[0] = codes_bf16(lo, scale);
+    f.h[1] = codes_bf16(hi, scale);
     return f;
 }
 
@@ -100,14 +100,19 @@ struct Columns {
     float m[NT], l[NT];
     f32x4v acc[NT][NC];
 
-    // Page number j of the row, in `t`: what its keys add.  Once its keys are used, and its values, next_k and next_v load those of the next page
-    // in their place, so that loads are in flight all the time with one set of registers.
+    // Page number j of the row, in `t` (there: whether it is one of the pool's; none of another's keys are seen): what its keys add.  Once its
+    // keys are used, and its values, next_k and next_v load those of the next page in their place, so that loads are in flight all the time
+    // with one set of registers.
     template <typename K, typename V>
-    __device__ inline void take(PagePart<D> &t, int j, float scale2, int window, int sinks, int lane, K next_k, V next_v)
+    __device__ inline void take(PagePart<D> &t, int j, bool there, float scale2, int window, int sinks, int lane, K next_k, V next_v)
     {
         const int quad = lane >> 4, j0 = j * kPage;
-        const bool edge = j0 + kPage - 1 > p0 || (j0 <= p1 - window && j0 + kPage > sinks);
+        const bool edge = !there || j0 + kPage - 1 > p0 || (j0 <= p1 - window && j0 + kPage > sinks);
         const float sc = fmaxf(t.k_scale * scale2, 0x1p-126f);       // (a page of zeros has scale 0, and 0 times -infinity is none)
+        // The values' scale is 2^e f, 1 <= f < 2: codes become bf16 with the power of two, and P is raised to P f by its exponent.
+        const uint32_t vbits = there && t.v_scale > 0.f ? __float_as_uint(t.v_scale) : 0x3f800000u;
+        const float power = __uint_as_float(vbits & 0x7f800000u), f = __uint_as_float((vbits & 0x007fffffu) | 0x3f800000u);
+        const float log2f_ = __builtin_amdgcn_logf(f), per_f = __builtin_amdgcn_rcpf(f);
         const int copy = SHARE > 1 ? (lane & 15) / (16 / SHARE) : 0, own = 4 * quad + 16 * copy;      // (a lane's block r is number SHARE r + copy)
         f32x4v s[NT][NB];
 #pragma unroll
@@ -135,13 +140,13 @@ struct Columns {
         if (edge) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const int hi = p[n] - j0 - own, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
+                const int hi = there ? p[n] - j0 - own : -1, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
 #pragma unroll
                 for (int r = 0; r < NB; ++r)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int at = 16 * SHARE * r + i;
-                        if (at > hi || (at < lo && at >= first)) s[n][r][i] = -INFINITY;
+                        s[n][r][i] = (at <= hi) & ((at >= lo) | (at < first)) ? s[n][r][i] : -INFINITY;
                     }
             }
         }
@@ -173,21 +178,15 @@ struct Columns {
         Frag pf[NT][2][NP];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float use = m[n] == -INFINITY ? 0.f : m[n];        // (nothing seen yet: every term is 2^-inf)
-            float sum = 0.f;
+            const float use = (m[n] == -INFINITY ? 0.f : m[n]) - log2f_;           // (nothing seen yet: every term is 2^-inf)
             uint32_t part[NB][2][NP];
 #pragma unroll
             for (int r = 0; r < NB; ++r) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float e = __builtin_amdgcn_exp2f(fmaf(s[n][r][i], sc, -use));
-                    sum += e;
-                    s[n][r][i] = e * t.v_scale;
-                }
+                for (int i = 0; i < 4; ++i) s[n][r][i] = __builtin_amdgcn_exp2f(fmaf(s[n][r][i], sc, -use));
 #pragma unroll
                 for (int i = 0; i < 2; ++i) split_pair<NP>(s[n][r][2 * i], s[n][r][2 * i + 1], part[r][i]);
             }
-            l[n] += sum;
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
                 uint2 w[NB];
@@ -196,28 +195,55 @@ struct Columns {
                 spread(w, copy, pf[n][0][x], pf[n][1][x]);
             }
         }
+        // Sums of P.  Of a whole tile as it enters the product, by a product with ones, which the matrix cores have more room for than the vector
+        // units; of copies, which have fewer terms a lane, by additions.
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if constexpr (SHARE == 1) {
+                Frag ones;
+                ones.u = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+                f32x4v sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int x = NP - 1; x >= 0; --x)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) sum = mfma16(ones, pf[n][half][x], sum);
+                l[n] = fmaf(sum[0], per_f, l[n]);
+            } else {
+                float sum = 0.f;
+#pragma unroll
+                for (int r = 0; r < NB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum += s[n][r][i];
+                l[n] = fmaf(sum, per_f, l[n]);
+            }
+        }
         // A code that not every column sees may be NaN (what is not yet written is anything), and 0 * NaN would reach the sums: such codes
         // are 0 in the product, and the columns that do see one get their NaN from a product of flags.
         if (edge) {
             uint32_t bad = 0;
 #pragma unroll
             for (int c = 0; c < NC; ++c) bad |= nan_bytes(t.v[c].x) | nan_bytes(t.v[c].y) | nan_bytes(t.v[c].z) | nan_bytes(t.v[c].w);
-            if (__any(bad != 0)) take_nan_out(t, j0, window, sinks, copy, own);
+            if (__any(bad != 0)) take_nan_out(t, j0, there, window, sinks, copy, own);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const Frag v = half ? codes_frag(t.v[c].z, t.v[c].w) : codes_frag(t.v[c].x, t.v[c].y);
+                const Frag v = half ? codes_frag(t.v[c].z, t.v[c].w, power) : codes_frag(t.v[c].x, t.v[c].y, power);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
                     for (int x = NP - 1; x >= 0; --x) acc[n][c] = mfma16(v, pf[n][half][x], acc[n][c]);
             }
         __builtin_amdgcn_sched_barrier(0);
+        // The compiler has counted too few wait states from a loop's last product to moves of its result at the loop's head (seen with d = 32,
+        // where the sums' second half was stale): these are enough.
+        asm volatile("s_nop 7");
         next_v();
     }
+
+    __device__ inline float total(int n) const { return SHARE == 1 ? l[n] : quads_sum(l[n]); }
 
     // A lane's blocks, four bf16 of each, as the operands of the second product: 0 where a block is another copy's.
     static __device__ inline void spread(const uint2 (&w)[NB], int copy, Frag &low, Frag &high)
@@ -229,12 +255,12 @@ struct Columns {
         }
     }
 
-    __device__ inline void take_nan_out(PagePart<D> &t, int j0, int window, int sinks, int copy, int own)
+    __device__ inline void take_nan_out(PagePart<D> &t, int j0, bool there, int window, int sinks, int copy, int own)
     {
         Frag seen[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const int hi = p[n] - j0 - own, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
+            const int hi = there ? p[n] - j0 - own : -1, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
             uint2 w[NB];
 #pragma unroll
             for (int r = 0; r < NB; ++r) {
@@ -242,7 +268,7 @@ struct Columns {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int at = 16 * SHARE * r + i;
-                    on[i] = at > hi || (at < lo && at >= first) ? 0u : 0x3f80u;
+                    on[i] = (at <= hi) & ((at >= lo) | (at < first)) ? 0x3f80u : 0u;
                 }
                 w[r] = make_uint2(on[0] | on[1] << 16, on[2] | on[3] << 16);
             }
@@ -303,19 +329,18 @@ struct PageList {
 
 // The pages that a wavefront takes, every `step`th from `begin` on: their numbers in the pool are loaded 64 at a time.
 struct Walk {
-    int ids, base;
+    int ids, used;
     __device__ inline void fill(const Pages &p, const PageList &list, int b, int i, int step)
     {
         const int at = i + (int)(threadIdx.x & 63) * step;
-        base = i;
         ids = at < list.count ? page_of(p, b, list.number(at)) : -1;
+        used = 0;
     }
-    __device__ inline int page(const Pages &p, const PageList &list, int b, int i, int step)
+    // of item i: begin, then the ones that follow in turn
+    __device__ inline int next(const Pages &p, const PageList &list, int b, int i, int step)
     {
-        const int n = (i - base) / step;
-        if (n < 64) return __builtin_amdgcn_readlane(ids, n);
-        fill(p, list, b, i, step);
-        return __builtin_amdgcn_readlane(ids, 0);
+        if (used == 64) fill(p, list, b, i, step);
+        return __builtin_amdgcn_readlane(ids, used++);
     }
 };
 
