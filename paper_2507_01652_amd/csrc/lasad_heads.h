@@ -37,9 +37,14 @@ __device__ inline void store8(char *p, const float (&f)[8])
 }
 
 template <int CTRL>
+__device__ inline float dpp_move(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+}
+template <int CTRL>
 __device__ inline float dpp_add(float x)
 {
-    return x + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true));
+    return x + dpp_move<CTRL>(x);
 }
 
 // Sum over the LPR lanes (4, 8 or 16, aligned) of a row, in every one of them.

@@ -32,41 +32,39 @@ __device__ inline uint32_t shrink(uint32_t w, float by, uint32_t mask)
     return (r & mask) | (w & ~mask);
 }
 
-// The scale of a page whose `earlier` first positions were there before, with scale `old`; where it grows, their codes are made smaller.  By
-// a wavefront; V: a page of values.
-template <int D, bool V>
-__device__ inline float page_scale(float most, int earlier, float old, float *scale, uint8_t *codes, int lane, bool &grown)
+// The bytes of a word before the first `n`, 0xff each.
+__device__ inline uint32_t first_bytes(int n) { return n <= 0 ? 0u : n >= 4 ? 0xffffffffu : (1u << 8 * n) - 1u; }
+
+// The scale of a page whose `earlier` first positions were there before, with scale `old`; their codes are then to be multiplied by `by`.
+__device__ inline float page_scale(float most, int earlier, float old, float &by)
 {
-    float s;
-    grown = false;
-    if (earlier == 0) old = 0.f;
-    if (!(old > 0.f)) {
-        s = most > 0.f ? fmaxf(most / kCodeTop, kLeastScale) : 0.f;
-    } else {
-        float by = 1.f;
-        s = old;
-        while (s * kCodeTop < most) {
-            s *= 2.f;
-            by *= 0.5f;
-        }
-        grown = by < 1.f;
-        if (grown) {
-            uint32_t *words = (uint32_t *)codes;
-            for (int w = lane; w < kPage * D / 4; w += 64) {
-                uint32_t mask;
-                if (V) {
-                    const int t = 16 * (w % 4) + 4 * (w / 4 % 4);          // the word's first position
-                    mask = t + 4 <= earlier ? 0xffffffffu : t >= earlier ? 0u : (1u << 8 * (earlier - t)) - 1u;
-                } else {
-                    mask = w / (D / 4) < earlier ? 0xffffffffu : 0u;
-                }
-                if (mask) words[w] = shrink(words[w], by, mask);
-            }
-            __threadfence_block();                       // (a word of v may get one of the call's codes yet, from another lane)
-        }
+    by = 1.f;
+    if (earlier == 0 || !(old > 0.f)) return most > 0.f ? fmaxf(most / kCodeTop, kLeastScale) : 0.f;
+    while (old * kCodeTop < most) {
+        old *= 2.f;
+        by *= 0.5f;
     }
-    if (lane == 0) *scale = s;
-    return s;
+    return old;
+}
+
+// The codes of the `earlier` first positions of a page made smaller, by a wavefront; V: a page of values.
+template <int D, bool V>
+__device__ inline void shrink_page(uint8_t *codes, int earlier, float by, int lane)
+{
+    uint4 w[D / 16];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) w[i] = ((const uint4 *)codes)[i * 64 + lane];
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        const int at = i * 64 + lane, g = at % 4;                              // v: positions 16 b + 4 g ..
+        const uint32_t whole = at / (D / 16) < earlier ? 0xffffffffu : 0u;      // k: a position's channels
+        w[i].x = shrink(w[i].x, by, V ? first_bytes(earlier - 4 * g) : whole);
+        w[i].y = shrink(w[i].y, by, V ? first_bytes(earlier - 4 * g - 16) : whole);
+        w[i].z = shrink(w[i].z, by, V ? first_bytes(earlier - 4 * g - 32) : whole);
+        w[i].w = shrink(w[i].w, by, V ? first_bytes(earlier - 4 * g - 48) : whole);
+        ((uint4 *)codes)[at] = w[i];
+    }
+    __threadfence_block();                               // (one of the call's codes may go there yet, from another lane)
 }
 
 }  // namespace lasad

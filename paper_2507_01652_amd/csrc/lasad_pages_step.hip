@@ -137,10 +137,16 @@ struct NewKey {
 #pragma unroll
         for (int off = 1; off < 16; off <<= 1) v_most = fmaxf(v_most, __shfl_xor(v_most, off));
         uint8_t *kp = a.pages.k + ph * kPage * D, *vp = a.pages.v + ph * kPage * D;
-        bool k_grown, v_grown;
-        k_scale = page_scale<D, false>(quads_max(k_most), slot, k_old, a.pages.k_scale + ph, kp, lane, k_grown);
-        v_scale = page_scale<D, true>(v_most, slot, v_old, a.pages.v_scale + ph, vp, lane, v_grown);
-        grown = k_grown || v_grown;
+        float k_less, v_less;
+        k_scale = page_scale(quads_max(k_most), slot, k_old, k_less);
+        v_scale = page_scale(v_most, slot, v_old, v_less);
+        if (k_less < 1.f) shrink_page<D, false>(kp, slot, k_less, lane);
+        if (v_less < 1.f) shrink_page<D, true>(vp, slot, v_less, lane);
+        if (lane == 0) {
+            a.pages.k_scale[ph] = k_scale;
+            a.pages.v_scale[ph] = v_scale;
+        }
+        grown = k_less < 1.f || v_less < 1.f;
         const Divide k_by(k_scale), v_by(v_scale);
 #pragma unroll
         for (int f = 0; f < NF; ++f)
