@@ -6,10 +6,11 @@
 // A power of two keeps the earlier codes exact but for the smallest binades, so that a page filled token by token is not rounded again and
 // again; and the first scale as it comes leaves no border at which a rounding of A would change a page by a factor of two.
 //
-// A wavefront has one head of one page, queries, keys or values: all of its numbers are in registers, so that A is known before the first code is
-// formed, with no wait for others.  Of queries and keys a lane has 8 channels of up to 64 / (512 / d) tokens in a row, of values d / 16 channels
-// of the 16 tokens whose codes are 16 bytes in a row of a channel.  Bound by memory: every number is read once, codes are written once.  What the
-// next head needs is on its way while one is worked on, and the first one's before the table of angles is formed.
+// A wavefront has 2048 numbers of one head of one page (queries, keys or values), in registers, so that A is known before the first code is formed:
+// of queries and keys 2048 / d tokens, a lane 8 channels of four of them in a row; of values 32 channels, a lane two of the 16 tokens whose
+// codes are 16 bytes in a row of a channel.  d / 32 wavefronts share a head and tell each other their maxima.  Twice as many numbers a lane
+// (no sharing at d = 64) took registers and code for two wavefronts a SIMD instead of five.  Bound by memory: every number is read once, codes
+// are written once.  What the next head needs is on its way while one is worked on, and the first one's before the table of angles is formed.
 #include "lasad_heads.h"
 #include "lasad_pages_codes.h"
 
@@ -17,7 +18,7 @@ namespace lasad {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 512, kWaves = 8;
 
 // the largest of a wavefront's lanes, in every one of them
 __device__ inline float wave_max(float x)
@@ -57,14 +58,13 @@ __device__ inline float word_float(const uint32_t *w, int e)
 enum { kNone, kAdjacent, kHalves };
 
 template <int BF16, int OBF16, int D, int TURN>
-__global__ void __launch_bounds__(kThreads, D == 128 ? 2 : 3)
+__global__ void __launch_bounds__(kThreads, 4)
 append_pages_kernel(AppendArgs a, int groups)
 {
-    constexpr int LPR = D / 8, P = D / 2, TPL = kPage * LPR / 64;          // lanes of a token, pairs, tokens of a lane
-    constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4;
-    constexpr int CH = D / 16, VW = CH * ELT / 4;                          // values: channels and words of a lane and token
-    constexpr bool AHEAD = BF16 || D < 128;                                // (fp32 of 128 channels would not fit in registers twice)
-    __shared__ __align__(16) float2 cs[kPage * P];
+    constexpr int LPR = D / 8, P = D / 2, PARTS = D / 32, ABREAST = kWaves / PARTS;      // lanes of a token, pairs, wavefronts of a head, heads at once
+    constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4, RW = 2 * ELT, VW = ELT / 2;  // words of 8 channels, of 2
+    __shared__ __align__(16) float2 cs[TURN == kNone ? 1 : kPage * P];
+    __shared__ float tops[2][kWaves];
     const int group = blockIdx.x % groups;
     PageRow row;
     if (!find_row(a.rows, a.pages, blockIdx.x / groups, 1, kPage, 2, row)) return;
@@ -72,96 +72,121 @@ append_pages_kernel(AppendArgs a, int groups)
     if (j * kPage >= row.pos + row.n) return;
     const int begin = max(row.pos - j * kPage, 0), end = min(row.pos + row.n - j * kPage, kPage);      // the call's positions in the page
     const int64_t token0 = (int64_t)row.first + j * kPage - row.pos;                                  // token of the page's position 0
-    const int page = __builtin_amdgcn_readfirstlane(page_of(a.pages, row.b, j));
+    const int entry = page_of(a.pages, row.b, j);
 
     // A lane's place is formed anew for each head: kept, all the offsets that follow from it would fill the registers.
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave % PARTS;
     struct Place {
-        int lane, piece, slot0;                          // queries and keys: 8 channels from 8 piece on, TPL positions from slot0 on
-        int quad, ch0;                                   // values: CH channels from ch0 on, positions 16 b + 4 quad + i
-        __device__ inline Place()
+        int lane, piece, slot;                           // queries and keys: 8 channels from 8 piece on, four positions from slot on
+        int quad, ch;                                    // values: two channels from ch on, positions 16 b + 4 quad + i
+        __device__ inline explicit Place(int part)
         {
             lane = threadIdx.x & 63;
             asm volatile("" : "+v"(lane));
-            piece = lane % LPR; slot0 = lane / LPR * TPL;
-            quad = lane % 4; ch0 = lane / 4 * CH;
+            piece = lane % LPR; slot = part * (kPage / PARTS) + lane / LPR * 4;
+            quad = lane % 4; ch = part * 32 + lane / 4 * 2;
         }
     };
     const auto here = [&](int t) { return t >= begin && t < end; };
     const auto near = [&](int t) -> int64_t { return min(max(t, begin), end - 1); };          // (other positions: one of the call's once more)
 
-    const int q_heads = a.q ? a.Hq : 0, heads = a.pages.heads, units = q_heads + (page < 0 ? 0 : 2 * heads), step = groups * kWaves;
-    uint32_t raw[D * ELT / 4];
-    float w[8], old = 0.f;
+    const int q_heads = a.q ? a.Hq : 0, heads = a.pages.heads, step = groups * ABREAST;
+    uint32_t raw[16 * VW];
+    float w[8];
     const auto load = [&](int unit) {
-        const Place at;
+        const Place at(part);
         if (unit < q_heads + heads) {
             const bool key = unit >= q_heads;
             const int h = key ? unit - q_heads : unit;
             const lasad_layout_t &l = key ? a.lk : a.lq;
-            const int64_t stride = l.stride_n;
-            const char *in = (const char *)(key ? a.k : a.q) + (token0 * stride + h * l.stride_h + at.piece * 8) * ELT;
+            const char *in = (const char *)(key ? a.k : a.q) + (token0 * l.stride_n + h * l.stride_h + at.piece * 8) * ELT;
 #pragma unroll
-            for (int u = 0; u < TPL; ++u)
-                load_words<2 * ELT>(in + near(at.slot0 + u) * stride * ELT, raw + u * 2 * ELT);
+            for (int u = 0; u < 4; ++u) load_words<RW>(in + near(at.slot + u) * l.stride_n * ELT, raw + u * RW);
             if (a.w[key]) load8<0>((const char *)(a.w[key] + (a.shared ? 0 : (int64_t)h * D) + at.piece * 8), w);
-            if (key) old = a.pages.k_scale[(int64_t)page * heads + h];
         } else {
             const int h = unit - q_heads - heads;
-            const int64_t stride = a.lv.stride_n;
-            const char *in = (const char *)a.v + (token0 * stride + h * a.lv.stride_h + at.ch0) * ELT;
+            const char *in = (const char *)a.v + (token0 * a.lv.stride_n + h * a.lv.stride_h + at.ch) * ELT;
 #pragma unroll
-            for (int u = 0; u < 16; ++u) {
-                load_words<VW>(in + near(u / 4 * 16 + 4 * at.quad + u % 4) * stride * ELT, raw + u * VW);
-                if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);           // (addresses of a few at a time)
-            }
-            old = a.pages.v_scale[(int64_t)page * heads + h];
+            for (int u = 0; u < 16; ++u) load_words<VW>(in + near(u / 4 * 16 + 4 * at.quad + u % 4) * a.lv.stride_n * ELT, raw + u * VW);
         }
     };
-    int unit = group * kWaves + wave;
-    if (AHEAD && unit < units) load(unit);
-    if (TURN != kNone) {
+    int unit = group * ABREAST + wave / PARTS;
+    if (unit < q_heads + 2 * heads) load(unit);
+    if constexpr (TURN != kNone) {
         const int pair = tid % P;
         const double f = pair_turns<D>(a.rope, pair, a.log2_base);
         for (int t = begin + tid / P; t < end; t += kThreads / P) cs[t * P + pair] = pair_angle<D>(a.rope, pair, j * kPage + t, a.grid_w, f);
+        __syncthreads();
     }
-    __syncthreads();
+    const int page = __builtin_amdgcn_readfirstlane(entry), units = q_heads + (page < 0 ? 0 : 2 * heads);
 
-    for (; unit < units; unit += step) {
-        if (!AHEAD) load(unit);
-        const Place at;
-        const bool value = unit >= q_heads + heads, key = !value && unit >= q_heads;
+    for (int first = group * ABREAST, turn_of = 0; first < units; first += step, unit += step, turn_of ^= 1) {        // (as often in all wavefronts)
+        const Place at(part);
+        const bool on = unit < units, value = unit >= q_heads + heads, key = !value && unit >= q_heads;
         const int h = value ? unit - q_heads - heads : key ? unit - q_heads : unit;
         const int64_t ph = (int64_t)page * heads + h;
-        const float was = old;
+        uint8_t *codes = value ? a.pages.v + ph * kPage * D + at.ch * kPage + 16 * at.quad : a.pages.k + ph * kPage * D + at.slot * D + at.piece * 8;
+        float *scale = (value ? a.pages.v_scale : a.pages.k_scale) + ph;
+        float y[32], old = 0.f;
+        if (on && (value || key)) old = *scale;
+        // (a value's old bytes beside the call's in a lane's 16)
+        uint4 before[2] = {};
+        bool all = true;
         if (value) {
-            uint8_t *codes = a.pages.v + ph * kPage * D;
-            uint4 before[CH] = {};
-            bool all = true;
 #pragma unroll
             for (int b = 0; b < 4; ++b) all &= here(16 * b + 4 * at.quad) && here(16 * b + 4 * at.quad + 3);
-            if (!all) {
-#pragma unroll
-                for (int e = 0; e < CH; ++e) before[e] = *(const uint4 *)(codes + (at.ch0 + e) * kPage + 16 * at.quad);
+            if (on && !all) {
+                before[0] = *(const uint4 *)codes;
+                before[1] = *(const uint4 *)(codes + kPage);
             }
-            float y[16][CH], most = 0.f;
+        }
 #pragma unroll
-            for (int u = 0; u < 16; ++u)
+        for (int i = 0; i < 32; ++i) y[i] = word_float<BF16>(raw + i / 2 * VW, i % 2);          // (four tokens' 8 channels, or 16 tokens' two)
+        float x[8];
 #pragma unroll
-                for (int e = 0; e < CH; ++e) {
-                    y[u][e] = word_float<BF16>(raw + u * VW, e);
-                    most = fmaxf(most, finite_size(y[u][e]));
-                }
-            if (AHEAD && unit + step < units) load(unit + step);
-            float less;
-            const float s = page_scale(wave_max(most), begin, was, less);
-            if (at.lane == 0) a.pages.v_scale[ph] = s;
-            const Divide by(s);
+        for (int e = 0; e < 8; ++e) x[e] = a.w[key] ? w[e] : 1.f;
+        if (unit + step < units) load(unit + step);
+        if (!value) {
+            const Turn turn = lane_turn<D>(a.rope, TURN == kHalves ? LASAD_PAIR_HALVES : LASAD_PAIR_ADJACENT, at.piece);
 #pragma unroll
-            for (int e = 0; e < CH; ++e) {
+            for (int u = 0; u < 4; ++u) {
+                float (&z)[8] = *(float (*)[8])(y + 8 * u);
+                float ss = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ss = fmaf(z[e], z[e], ss);
+                const float r = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + a.eps), rstd = a.norm ? r : 1.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = z[e] * rstd * x[e];
+                if constexpr (TURN != kNone) turn8(cs + near(at.slot + u) * P, turn, false, z);
+            }
+            if (!key && on) {
+                char *out = (char *)a.q_out + ((token0 + at.slot) * a.lo.stride_n + h * a.lo.stride_h + at.piece * 8) * OELT;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (here(at.slot + u)) store8<OBF16>(out + u * a.lo.stride_n * OELT, *(const float (*)[8])(y + 8 * u));
+            }
+        }
+        float most = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) most = fmaxf(most, finite_size(y[i]));
+        most = wave_max(most);
+        if constexpr (PARTS > 1) {
+            if (at.lane == 0) tops[turn_of][wave] = most;
+            __syncthreads();                             // (the other half of `tops` is read by then)
+#pragma unroll
+            for (int i = 0; i < PARTS; ++i) most = fmaxf(most, tops[turn_of][wave - part + i]);
+        }
+        if (!on || !(value || key)) continue;
+        float less;
+        const float s = page_scale(most, begin, old, less);
+        if (part == 0 && at.lane == 0) *scale = s;
+        const Divide by(s);
+        if (value) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
                 uint32_t c[4];
 #pragma unroll
-                for (int b = 0; b < 4; ++b) c[b] = code4(by(y[4 * b][e]), by(y[4 * b + 1][e]), by(y[4 * b + 2][e]), by(y[4 * b + 3][e]));
+                for (int b = 0; b < 4; ++b) c[b] = code4(by(y[8 * b + e]), by(y[8 * b + 2 + e]), by(y[8 * b + 4 + e]), by(y[8 * b + 6 + e]));
                 if (!all) {
                     const uint32_t o[4] = {before[e].x, before[e].y, before[e].z, before[e].w};
 #pragma unroll
@@ -171,62 +196,21 @@ append_pages_kernel(AppendArgs a, int groups)
                         c[b] = (c[b] & mine) | ((less < 1.f ? shrink(o[b], less, earlier) : o[b]) & ~mine);
                     }
                 }
-                *(uint4 *)(codes + (at.ch0 + e) * kPage + 16 * at.quad) = make_uint4(c[0], c[1], c[2], c[3]);
+                *(uint4 *)(codes + e * kPage) = make_uint4(c[0], c[1], c[2], c[3]);
             }
-            continue;
+        } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                uint2 c = make_uint2(code4(by(y[8 * u]), by(y[8 * u + 1]), by(y[8 * u + 2]), by(y[8 * u + 3])),
+                                     code4(by(y[8 * u + 4]), by(y[8 * u + 5]), by(y[8 * u + 6]), by(y[8 * u + 7])));
+                const bool earlier = less < 1.f && at.slot + u < begin;
+                if (earlier) {
+                    c = *(const uint2 *)(codes + u * D);
+                    c = make_uint2(shrink(c.x, less, 0xffffffffu), shrink(c.y, less, 0xffffffffu));
+                }
+                if (earlier || here(at.slot + u)) *(uint2 *)(codes + u * D) = c;
+            }
         }
-        const Turn turn = lane_turn<D>(a.rope, TURN == kHalves ? LASAD_PAIR_HALVES : LASAD_PAIR_ADJACENT, at.piece);
-        float y[TPL][8], x[8];
-#pragma unroll
-        for (int u = 0; u < TPL; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[u][e] = word_float<BF16>(raw + u * 2 * ELT, e);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = a.w[key] ? w[e] : 1.f;
-        if (AHEAD && unit + step < units) load(unit + step);
-        // (one run of code with no branches: values that branches change would be held twice)
-#pragma unroll
-        for (int u = 0; u < TPL; ++u) {
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) ss = fmaf(y[u][e], y[u][e], ss);
-            const float r = rsqrtf(row_sum<LPR>(ss) * (1.0f / D) + a.eps), rstd = a.norm ? r : 1.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[u][e] = y[u][e] * rstd * x[e];
-            if constexpr (TURN != kNone) turn8(cs + near(at.slot0 + u) * P, turn, false, y[u]);
-            if (u % 2) __builtin_amdgcn_sched_barrier(0);               // (all tokens' angles at once would need registers)
-        }
-        if (!key) {
-            const int64_t stride = a.lo.stride_n;
-            char *out = (char *)a.q_out + ((token0 + at.slot0) * stride + h * a.lo.stride_h + at.piece * 8) * OELT;
-#pragma unroll
-            for (int u = 0; u < TPL; ++u)
-                if (here(at.slot0 + u)) store8<OBF16>(out + u * stride * OELT, y[u]);
-            continue;
-        }
-        float most = 0.f, less;
-#pragma unroll
-        for (int u = 0; u < TPL; ++u)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) most = fmaxf(most, finite_size(y[u][e]));
-        const float s = page_scale(wave_max(most), begin, was, less);
-        if (at.lane == 0) a.pages.k_scale[ph] = s;
-        const Divide by(s);
-        uint8_t *codes = a.pages.k + ph * kPage * D + at.slot0 * D + at.piece * 8;
-        if (less < 1.f) {
-            uint2 o[TPL] = {};
-#pragma unroll
-            for (int u = 0; u < TPL; ++u)
-                if (at.slot0 + u < begin) o[u] = *(const uint2 *)(codes + u * D);
-#pragma unroll
-            for (int u = 0; u < TPL; ++u)
-                if (at.slot0 + u < begin) *(uint2 *)(codes + u * D) = make_uint2(shrink(o[u].x, less, 0xffffffffu), shrink(o[u].y, less, 0xffffffffu));
-        }
-#pragma unroll
-        for (int u = 0; u < TPL; ++u)
-            if (here(at.slot0 + u))
-                *(uint2 *)(codes + u * D) =
-                    make_uint2(code4(by(y[u][0]), by(y[u][1]), by(y[u][2]), by(y[u][3])), code4(by(y[u][4]), by(y[u][5]), by(y[u][6]), by(y[u][7])));
     }
 }
 
@@ -236,8 +220,8 @@ int64_t slots_of(const AppendArgs &a) { return row_slots(a.rows, 1, kPage, 2); }
 
 int head_groups(const AppendArgs &a)
 {
-    const int units = (a.q ? a.Hq : 0) + 2 * a.pages.heads, most = (units + kWaves - 1) / kWaves;
-    const int64_t want = (1024 + slots_of(a) - 1) / slots_of(a);
+    const int units = (a.q ? a.Hq : 0) + 2 * a.pages.heads, abreast = kWaves * 32 / a.d, most = (units + abreast - 1) / abreast;
+    const int64_t want = (512 + slots_of(a) - 1) / slots_of(a);
     return (int)(want < 1 ? 1 : want > most ? most : want);
 }
 
