@@ -84,21 +84,23 @@ __device__ inline bool find_row(const PageRows &r, const Pages &pages, int slot,
     if (r.starts) {
         const int lane = threadIdx.x & 63;
         int lo = 0, span = r.B;
-        const auto first_slot = [&](int b) {
-            const int64_t s = min(max(r.starts[b], 0), r.tokens);
-            return s * num / den + (int64_t)b * extra;
-        };
-        while (span > 1) {
+        const auto clamped = [&](int s) { return min(max(s, 0), r.tokens); };
+        const auto first_slot = [&](int b, int s) { return (int64_t)s * num / den + (int64_t)b * extra; };
+        while (span > 64) {
             const int step = (span + 63) / 64, b = lo + lane * step;
-            const bool before = lane * step < span && first_slot(b) <= slot;
+            const bool before = lane * step < span && first_slot(b, clamped(r.starts[b])) <= slot;
             const int found = max(1, __popcll(__ballot(before))) - 1;
             lo += found * step;
             span = min(step, span - found * step);
         }
-        row.b = __builtin_amdgcn_readfirstlane(lo);
-        row.first = min(max(r.starts[row.b], 0), r.tokens);
-        row.n = min(max(r.starts[row.b + 1], row.first), r.tokens) - row.first;
-        const int64_t unit = slot - first_slot(row.b);
+        // the rest at once, with what is needed of the one that it will be
+        const int start = clamped(r.starts[min(lo + lane, r.B)]), pos = r.pos_rows ? r.pos_rows[min(lo + lane, r.B - 1)] : r.pos;
+        const int found = max(1, __popcll(__ballot(lane < span && first_slot(lo + lane, start) <= slot))) - 1;
+        row.b = __builtin_amdgcn_readfirstlane(lo + found);
+        row.first = __builtin_amdgcn_readlane(start, found);
+        row.n = max(found < 63 ? __builtin_amdgcn_readlane(start, found + 1) : clamped(r.starts[row.b + 1]), row.first) - row.first;
+        row.pos = __builtin_amdgcn_readlane(pos, found);
+        const int64_t unit = slot - first_slot(row.b, row.first);
         if (unit < 0) return false;
         row.unit = (int)unit;
     } else {
@@ -107,8 +109,8 @@ __device__ inline bool find_row(const PageRows &r, const Pages &pages, int slot,
         row.unit = slot - row.b * each;
         row.first = row.b;
         row.n = 1;
+        row.pos = r.pos_rows ? r.pos_rows[row.b] : r.pos;
     }
-    row.pos = r.pos_rows ? r.pos_rows[row.b] : r.pos;
     row.b = __builtin_amdgcn_readfirstlane(row.b);       // (the same in all lanes; so that the compiler knows)
     row.first = __builtin_amdgcn_readfirstlane(row.first);
     row.n = __builtin_amdgcn_readfirstlane(row.n);

@@ -11,6 +11,8 @@
 // codes are 16 bytes in a row of a channel.  d / 32 wavefronts share a head and tell each other their maxima.  Twice as many numbers a lane
 // (no sharing at d = 64) took registers and code for two wavefronts a SIMD instead of five.  Bound by memory: every number is read once, codes
 // are written once.  What the next head needs is on its way while one is worked on, and the first one's before the table of angles is formed.
+#include <type_traits>
+
 #include "lasad_heads.h"
 #include "lasad_pages_codes.h"
 
@@ -21,14 +23,16 @@ namespace {
 constexpr int kThreads = 512, kWaves = 8;
 
 // the largest of a wavefront's lanes, in every one of them
-__device__ inline float wave_max(float x)
+__device__ inline uint32_t wave_max(uint32_t x)
 {
-    x = fmaxf(x, dpp_move<0xB1>(x));
-    x = fmaxf(x, dpp_move<0x4E>(x));
-    x = fmaxf(x, dpp_move<0x141>(x));
-    x = fmaxf(x, dpp_move<0x140>(x));
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return both_halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    x = max(x, __float_as_uint(dpp_move<0xB1>(__uint_as_float(x))));
+    x = max(x, __float_as_uint(dpp_move<0x4E>(__uint_as_float(x))));
+    x = max(x, __float_as_uint(dpp_move<0x141>(__uint_as_float(x))));
+    x = max(x, __float_as_uint(dpp_move<0x140>(__uint_as_float(x))));
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    x = max(r[0], r[1]);
+    const auto t = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return max(t[0], t[1]);
 }
 
 // n words from p on.
@@ -55,6 +59,9 @@ __device__ inline float word_float(const uint32_t *w, int e)
     return __uint_as_float(w[e]);
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 enum { kNone, kAdjacent, kHalves };
 
 template <int BF16, int OBF16, int D, int TURN>
@@ -64,7 +71,7 @@ append_pages_kernel(AppendArgs a, int groups)
     constexpr int LPR = D / 8, P = D / 2, PARTS = D / 32, ABREAST = kWaves / PARTS;      // lanes of a token, pairs, wavefronts of a head, heads at once
     constexpr int ELT = BF16 ? 2 : 4, OELT = OBF16 ? 2 : 4, RW = 2 * ELT, VW = ELT / 2;  // words of 8 channels, of 2
     __shared__ __align__(16) float2 cs[TURN == kNone ? 1 : kPage * P];
-    __shared__ float tops[2][kWaves];
+    __shared__ uint32_t tops[2][kWaves];
     const int group = blockIdx.x % groups;
     PageRow row;
     if (!find_row(a.rows, a.pages, blockIdx.x / groups, 1, kPage, 2, row)) return;
@@ -88,7 +95,27 @@ append_pages_kernel(AppendArgs a, int groups)
         }
     };
     const auto here = [&](int t) { return t >= begin && t < end; };
-    const auto near = [&](int t) -> int64_t { return min(max(t, begin), end - 1); };          // (other positions: one of the call's once more)
+    const auto near = [&](int t) { return min(max(t, begin), end - 1); };          // (other positions: one of the call's once more)
+    // words of N positions' numbers, from the token of position 0 on: offsets in 32 bits where the stride allows it (16 MB a token)
+    const auto load_tokens = [&](auto words, auto count, const char *in, uint32_t lane_bytes, int64_t stride, uint32_t *to, auto position) {
+        constexpr int W = decltype(words)::value, N = decltype(count)::value;
+        if (stride < 1 << 24) {
+            if (begin == 0 && end == kPage) {
+                const uint32_t at = (uint32_t)position(0) * (uint32_t)stride + lane_bytes;
+#pragma unroll
+                for (int u = 0; u < N; ++u) load_words<W>(in + (position(u) - position(0)) * stride + at, to + u * W);
+            } else {
+#pragma unroll
+                for (int u = 0; u < N; ++u) load_words<W>(in + (__umul24(near(position(u)), (uint32_t)stride) + lane_bytes), to + u * W);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                load_words<W>(in + near(position(u)) * stride + lane_bytes, to + u * W);
+                __builtin_amdgcn_sched_barrier(0);                             // (one address at a time)
+            }
+        }
+    };
 
     const int q_heads = a.q ? a.Hq : 0, heads = a.pages.heads, step = groups * ABREAST;
     uint32_t raw[16 * VW];
@@ -99,15 +126,13 @@ append_pages_kernel(AppendArgs a, int groups)
             const bool key = unit >= q_heads;
             const int h = key ? unit - q_heads : unit;
             const lasad_layout_t &l = key ? a.lk : a.lq;
-            const char *in = (const char *)(key ? a.k : a.q) + (token0 * l.stride_n + h * l.stride_h + at.piece * 8) * ELT;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) load_words<RW>(in + near(at.slot + u) * l.stride_n * ELT, raw + u * RW);
+            const char *in = (const char *)(key ? a.k : a.q) + (token0 * l.stride_n + h * l.stride_h) * ELT;
+            load_tokens(Int<RW>(), Int<4>(), in, at.piece * 8 * ELT, l.stride_n * ELT, raw, [&](int u) { return at.slot + u; });
             if (a.w[key]) load8<0>((const char *)(a.w[key] + (a.shared ? 0 : (int64_t)h * D) + at.piece * 8), w);
         } else {
             const int h = unit - q_heads - heads;
-            const char *in = (const char *)a.v + (token0 * a.lv.stride_n + h * a.lv.stride_h + at.ch) * ELT;
-#pragma unroll
-            for (int u = 0; u < 16; ++u) load_words<VW>(in + near(u / 4 * 16 + 4 * at.quad + u % 4) * a.lv.stride_n * ELT, raw + u * VW);
+            const char *in = (const char *)a.v + (token0 * a.lv.stride_n + h * a.lv.stride_h) * ELT;
+            load_tokens(Int<VW>(), Int<16>(), in, at.ch * ELT, a.lv.stride_n * ELT, raw, [&](int u) { return u / 4 * 16 + 4 * at.quad + u % 4; });
         }
     };
     int unit = group * ABREAST + wave / PARTS;
@@ -122,6 +147,7 @@ append_pages_kernel(AppendArgs a, int groups)
 
     for (int first = group * ABREAST, turn_of = 0; first < units; first += step, unit += step, turn_of ^= 1) {        // (as often in all wavefronts)
         const Place at(part);
+        if (!BF16 && first != group * ABREAST && unit < units) load(unit);                   // (a second set would not fit in registers)
         const bool on = unit < units, value = unit >= q_heads + heads, key = !value && unit >= q_heads;
         const int h = value ? unit - q_heads - heads : key ? unit - q_heads : unit;
         const int64_t ph = (int64_t)page * heads + h;
@@ -145,7 +171,7 @@ append_pages_kernel(AppendArgs a, int groups)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = a.w[key] ? w[e] : 1.f;
-        if (unit + step < units) load(unit + step);
+        if (BF16 && unit + step < units) load(unit + step);
         if (!value) {
             const Turn turn = lane_turn<D>(a.rope, TURN == kHalves ? LASAD_PAIR_HALVES : LASAD_PAIR_ADJACENT, at.piece);
 #pragma unroll
@@ -158,6 +184,7 @@ append_pages_kernel(AppendArgs a, int groups)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) z[e] = z[e] * rstd * x[e];
                 if constexpr (TURN != kNone) turn8(cs + near(at.slot + u) * P, turn, false, z);
+                if (!BF16) __builtin_amdgcn_sched_barrier(0);
             }
             if (!key && on) {
                 char *out = (char *)a.q_out + ((token0 + at.slot) * a.lo.stride_n + h * a.lo.stride_h + at.piece * 8) * OELT;
@@ -166,19 +193,26 @@ append_pages_kernel(AppendArgs a, int groups)
                     if (here(at.slot + u)) store8<OBF16>(out + u * a.lo.stride_n * OELT, *(const float (*)[8])(y + 8 * u));
             }
         }
-        float most = 0.f;
+        // The bits of magnitudes are in their order, what is not finite behind: a second look where there is any.
+        uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) most = fmaxf(most, finite_size(y[i]));
+        for (int i = 0; i < 32; ++i) most = max(most, __float_as_uint(y[i]) & 0x7fffffffu);
         most = wave_max(most);
+        if (most >= 0x7f800000u) {
+            most = 0;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) most = max(most, __float_as_uint(finite_size(y[i])));
+            most = wave_max(most);
+        }
         if constexpr (PARTS > 1) {
             if (at.lane == 0) tops[turn_of][wave] = most;
             __syncthreads();                             // (the other half of `tops` is read by then)
 #pragma unroll
-            for (int i = 0; i < PARTS; ++i) most = fmaxf(most, tops[turn_of][wave - part + i]);
+            for (int i = 0; i < PARTS; ++i) most = max(most, tops[turn_of][wave - part + i]);
         }
         if (!on || !(value || key)) continue;
         float less;
-        const float s = page_scale(most, begin, old, less);
+        const float s = page_scale(__uint_as_float(most), begin, old, less);
         if (part == 0 && at.lane == 0) *scale = s;
         const Divide by(s);
         if (value) {
