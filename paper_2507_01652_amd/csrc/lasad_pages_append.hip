@@ -9,7 +9,7 @@
 // A wavefront has 2048 numbers of one head of one page (queries, keys or values), in registers, so that A is known before the first code is formed:
 // of queries and keys 2048 / d tokens, a lane 8 channels of four of them in a row; of values 32 channels, a lane two of the 16 tokens whose
 // codes are 16 bytes in a row of a channel.  d / 32 wavefronts share a head and tell each other their maxima.  Twice as many numbers a lane
-// (no sharing at d = 64) took registers and code for two wavefronts a SIMD instead of five.  Bound by memory: every number is read once, codes
+// (no sharing at d = 64) took registers for two or three wavefronts a SIMD instead of four.  Bound by memory: every number is read once, codes
 // are written once.  What the next head needs is on its way while one is worked on, and the first one's before the table of angles is formed.
 #include <type_traits>
 
@@ -145,33 +145,45 @@ append_pages_kernel(AppendArgs a, int groups)
     }
     const int page = __builtin_amdgcn_readfirstlane(entry), units = q_heads + (page < 0 ? 0 : 2 * heads);
 
+    // What the pages held: the scale, and the old bytes beside the call's in a lane's 16 of a value.
+    float next_old = 0.f;
+    uint4 next_before[2] = {};
+    const auto load_old = [&](int unit) {
+        if (unit < q_heads || unit >= units) return;
+        const Place at(part);
+        const bool value = unit >= q_heads + heads;
+        const int64_t ph = (int64_t)page * heads + (value ? unit - q_heads - heads : unit - q_heads);
+        next_old = (value ? a.pages.v_scale : a.pages.k_scale)[ph];
+        if (value && (begin > 0 || end < kPage)) {
+            const uint8_t *codes = a.pages.v + ph * kPage * D + at.ch * kPage + 16 * at.quad;
+            next_before[0] = *(const uint4 *)codes;
+            next_before[1] = *(const uint4 *)(codes + kPage);
+        }
+    };
+    load_old(unit);
     for (int first = group * ABREAST, turn_of = 0; first < units; first += step, unit += step, turn_of ^= 1) {        // (as often in all wavefronts)
         const Place at(part);
-        if (!BF16 && first != group * ABREAST && unit < units) load(unit);                   // (a second set would not fit in registers)
+        if (!BF16 && first != group * ABREAST) {         // (a second set would not fit in registers)
+            if (unit < units) load(unit);
+            load_old(unit);
+        }
         const bool on = unit < units, value = unit >= q_heads + heads, key = !value && unit >= q_heads;
         const int h = value ? unit - q_heads - heads : key ? unit - q_heads : unit;
         const int64_t ph = (int64_t)page * heads + h;
         uint8_t *codes = value ? a.pages.v + ph * kPage * D + at.ch * kPage + 16 * at.quad : a.pages.k + ph * kPage * D + at.slot * D + at.piece * 8;
         float *scale = (value ? a.pages.v_scale : a.pages.k_scale) + ph;
-        float y[32], old = 0.f;
-        if (on && (value || key)) old = *scale;
-        // (a value's old bytes beside the call's in a lane's 16)
-        uint4 before[2] = {};
-        bool all = true;
-        if (value) {
-#pragma unroll
-            for (int b = 0; b < 4; ++b) all &= here(16 * b + 4 * at.quad) && here(16 * b + 4 * at.quad + 3);
-            if (on && !all) {
-                before[0] = *(const uint4 *)codes;
-                before[1] = *(const uint4 *)(codes + kPage);
-            }
-        }
+        const float old = next_old;
+        const uint4 before[2] = {next_before[0], next_before[1]};
+        float y[32];
 #pragma unroll
         for (int i = 0; i < 32; ++i) y[i] = word_float<BF16>(raw + i / 2 * VW, i % 2);          // (four tokens' 8 channels, or 16 tokens' two)
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = a.w[key] ? w[e] : 1.f;
-        if (BF16 && unit + step < units) load(unit + step);
+        if constexpr (BF16) {
+            if (unit + step < units) load(unit + step);
+            load_old(unit + step);
+        }
         if (!value) {
             const Turn turn = lane_turn<D>(a.rope, TURN == kHalves ? LASAD_PAIR_HALVES : LASAD_PAIR_ADJACENT, at.piece);
 #pragma unroll
@@ -221,7 +233,7 @@ append_pages_kernel(AppendArgs a, int groups)
                 uint32_t c[4];
 #pragma unroll
                 for (int b = 0; b < 4; ++b) c[b] = code4(by(y[8 * b + e]), by(y[8 * b + 2 + e]), by(y[8 * b + 4 + e]), by(y[8 * b + 6 + e]));
-                if (!all) {
+                if (begin > 0 || end < kPage) {
                     const uint32_t o[4] = {before[e].x, before[e].y, before[e].z, before[e].w};
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
