@@ -51,7 +51,7 @@ attend_pages_kernel(AttendArgs a)
     const float scale2 = a.scale * kLog2e;
     const PageList list(x.p0, x.p1, a.window, a.sinks);
     const int step = a.splits * KW;
-    int i = split * KW + kw;
+    const int i = split * KW + kw;
     Walk walk;
     walk.fill(a.pages, list, row.b, i, step);
     int page = walk.next(a.pages, list, row.b, i, step);
@@ -60,13 +60,7 @@ attend_pages_kernel(AttendArgs a)
     const auto load_v = [&] { t.load_v(a.pages, max(page, 0), hk, lane); };
     load_k();
     load_v();
-    while (i < list.count) {
-        const int j = __builtin_amdgcn_readfirstlane(list.number(i));
-        const bool there = page >= 0;
-        i += step;
-        if (i < list.count) page = walk.next(a.pages, list, row.b, i, step);               // (behind the last page that one again)
-        x.take(t, j, there, scale2, a.window, a.sinks, lane, load_k, load_v);
-    }
+    x.run(t, list, i, step, scale2, a.window, a.sinks, lane, [&](int) { return page >= 0; }, [&](int i) { page = walk.next(a.pages, list, row.b, i, step); }, load_k, load_v);
 
     if constexpr (KW == 1) {
 #pragma unroll

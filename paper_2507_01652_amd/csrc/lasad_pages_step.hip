@@ -170,16 +170,16 @@ struct NewKey {
     {
         const int quad = lane >> 4, col = lane & 15;
         const uint32_t shift = 8 * (slot % 4), keep = quad == slot / 4 % 4 ? ~(0xffu << shift) : ~0u;
+        const int block = slot / 16;
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (slot / 16 != b) continue;
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int w = 0; w < D / 16; ++w) t.k[b][w] = col == slot % 16 ? k[w] : t.k[b][w];
+            for (int w = 0; w < D / 16; ++w) t.k[b][w] = b == block && col == slot % 16 ? k[w] : t.k[b][w];
 #pragma unroll
-            for (int c = 0; c < D / 16; ++c) {
-                uint32_t &w = b == 0 ? t.v[c].x : b == 1 ? t.v[c].y : b == 2 ? t.v[c].z : t.v[c].w;
-                w = (w & keep) | (v[c] << shift & ~keep);
-            }
+        for (int c = 0; c < D / 16; ++c) {
+            const uint4 w = t.v[c];
+            const auto with = [&](uint32_t x, int b) { return b == block ? (x & keep) | (v[c] << shift & ~keep) : x; };
+            t.v[c] = make_uint4(with(w.x, 0), with(w.y, 1), with(w.z, 2), with(w.w, 3));
         }
         t.k_scale = k_scale;
         t.v_scale = v_scale;
@@ -257,9 +257,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         x.l[0] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) x.acc[0][c] = f32x4v{0.f, 0.f, 0.f, 0.f};
-        int i = begin;
-        while (i < list.count) {
-            const int j = __builtin_amdgcn_readfirstlane(list.number(i));
+        const auto take_up = [&](int i) __attribute__((always_inline)) {
             const bool there = page >= 0;
             if (i == list.count - 1 && there) {
                 if (fresh.grown) {
@@ -268,10 +266,9 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
                 }
                 fresh.put(t, pos % kPage, lane);
             }
-            i += step;
-            if (i < list.count) page = walk.next(a.pages, list, b, i, step);               // (behind the last page that one again)
-            x.take(t, j, there, g.scale * kLog2e, g.window, g.sinks, lane, load_k, load_v);
-        }
+            return there;
+        };
+        x.run(t, list, begin, step, g.scale * kLog2e, g.window, g.sinks, lane, take_up, [&](int i) { page = walk.next(a.pages, list, b, i, step); }, load_k, load_v);
         join_waves<O, D, WAVES, SHARE>(red, x.acc[0], x.m[0], x.total(0), wave, lane, min(EACH, G - g0), g.splits, split, [&](int c, int ch) {
             const int64_t at = (int64_t)b * a.Hq + hk * G + g0 + c;
             return Result<O>{g.parts + at * g.splits * (D + 4), (O *)g.o + at * D + ch};

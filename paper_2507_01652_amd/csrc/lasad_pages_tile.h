@@ -87,6 +87,35 @@ struct PagePart {
 template <int D>
 __device__ inline int page_channel(int f, int quad) { return D == 32 ? 8 * quad : 64 * (f >> 1) + 16 * quad + 8 * (f & 1); }
 
+// The pages that positions p0 .. p1 see: those of the sinks before the window's, then the window's.
+struct PageList {
+    int sink_pages, first, count;
+    __device__ inline PageList(int p0, int p1, int window, int sinks)
+    {
+        first = max(0, p0 - window + 1) / kPage;
+        sink_pages = min((int)(((int64_t)sinks + kPage - 1) / kPage), first);
+        count = p1 < 0 ? 0 : sink_pages + p1 / kPage - first + 1;
+    }
+    __device__ inline int number(int i) const { return i < sink_pages ? i : first + i - sink_pages; }
+};
+
+// The pages that a wavefront takes, every `step`th from `begin` on: their numbers in the pool are loaded 64 at a time.
+struct Walk {
+    int ids, used;
+    __device__ inline void fill(const Pages &p, const PageList &list, int b, int i, int step)
+    {
+        const int at = i + (int)(threadIdx.x & 63) * step;
+        ids = at < list.count ? page_of(p, b, list.number(at)) : -1;
+        used = 0;
+    }
+    // of item i: begin, then the ones that follow in turn
+    __device__ inline int next(const Pages &p, const PageList &list, int b, int i, int step)
+    {
+        if (used == 64) fill(p, list, b, i, step);
+        return __builtin_amdgcn_readlane(ids, used++);
+    }
+};
+
 // A wavefront's columns: NT tiles of 16, this lane's column of each.  SHARE > 1, for fewer queries than a tile has columns: 16 / SHARE queries
 // lie in it SHARE times, and copy i keeps those scores alone whose block of 16 positions is i modulo SHARE.  Its sums are over those, as if it
 // were another wavefront's, and a lane has 16 / SHARE scores of a page to raise to a power instead of 16.
@@ -100,21 +129,17 @@ struct Columns {
     float m[NT], l[NT];
     f32x4v acc[NT][NC];
 
-    // Page number j of the row, in `t` (there: whether it is one of the pool's; none of another's keys are seen): what its keys add.  Once its
-    // keys are used, and its values, next_k and next_v load those of the next page in their place, so that loads are in flight all the time
-    // with one set of registers.
-    template <typename K, typename V>
-    __device__ inline void take(PagePart<D> &t, int j, bool there, float scale2, int window, int sinks, int lane, K next_k, V next_v)
+    // The compiler counts too few wait states from a block's last product to moves of its result in the next one (seen at a loop's head with d = 32,
+    // where the second half of the sums was stale): these are enough.
+    static __device__ inline void wait_for_products()
     {
-        const int quad = lane >> 4, j0 = j * kPage;
-        const bool edge = !there || j0 + kPage - 1 > p0 || (j0 <= p1 - window && j0 + kPage > sinks);
-        const float sc = fmaxf(t.k_scale * scale2, 0x1p-126f);       // (a page of zeros has scale 0, and 0 times -infinity is none)
-        // The values' scale is 2^e f, 1 <= f < 2: codes become bf16 with the power of two, and P is raised to P f by its exponent.
-        const uint32_t vbits = there && t.v_scale > 0.f ? __float_as_uint(t.v_scale) : 0x3f800000u;
-        const float power = __uint_as_float(vbits & 0x7f800000u), f = __uint_as_float((vbits & 0x007fffffu) | 0x3f800000u);
-        const float log2f_ = __builtin_amdgcn_logf(f), per_f = __builtin_amdgcn_rcpf(f);
-        const int copy = SHARE > 1 ? (lane & 15) / (16 / SHARE) : 0, own = 4 * quad + 16 * copy;      // (a lane's block r is number SHARE r + copy)
-        f32x4v s[NT][NB];
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_nop 7");
+    }
+
+    // Scores of a page, 16 positions x 16 columns a product.
+    __device__ inline void scores(const PagePart<D> &t, int copy, f32x4v (&s)[NT][NB]) const
+    {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             Frag k[NF];
@@ -135,57 +160,24 @@ struct Columns {
                 }
             }
         }
-        __builtin_amdgcn_sched_barrier(0);               // (loads moved up over the products, or conversions over the exponentials, would need registers)
-        next_k();
-        if (edge) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int hi = there ? p[n] - j0 - own : -1, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
-#pragma unroll
-                for (int r = 0; r < NB; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at = 16 * SHARE * r + i;
-                        s[n][r][i] = (at <= hi) & ((at >= lo) | (at < first)) ? s[n][r][i] : -INFINITY;
-                    }
-            }
-        }
-        float top[NT];
-        bool grows = false;
+        wait_for_products();
+    }
+
+    // P = 2^(s sc - m + log2_more) as the second product's operand, and its sums.  Of a whole tile as it enters the product, by a product with ones,
+    // which the matrix cores have more room for than the vector units; of copies, which have fewer terms a lane, by additions (a lane's own).
+    __device__ inline void powers(const f32x4v (&s)[NT][NB], float sc, float log2_more, int copy, Frag (&pf)[NT][2][NP], float (&sum)[NT]) const
+    {
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            top[n] = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < NB; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top[n] = fmaxf(top[n], s[n][r][i]);
-            top[n] = quads_max(top[n]) * sc;
-            grows |= top[n] > m[n] + kSlack;
-        }
-        if (__any(grows)) {
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float m1 = top[n] > m[n] + kSlack ? top[n] : m[n];
-                const float fade = m[n] == m1 ? 1.f : __builtin_amdgcn_exp2f(m[n] - m1);
-                m[n] = m1;
-                l[n] *= fade;
-#pragma unroll
-                for (int c = 0; c < NC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][c][i] *= fade;
-            }
-        }
-        Frag pf[NT][2][NP];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const float use = (m[n] == -INFINITY ? 0.f : m[n]) - log2f_;           // (nothing seen yet: every term is 2^-inf)
+            const float use = (m[n] == -INFINITY ? 0.f : m[n]) - log2_more;        // (nothing seen yet: every term is 2^-inf)
+            float e[NB][4];
             uint32_t part[NB][2][NP];
 #pragma unroll
             for (int r = 0; r < NB; ++r) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[n][r][i] = __builtin_amdgcn_exp2f(fmaf(s[n][r][i], sc, -use));
+                for (int i = 0; i < 4; ++i) e[r][i] = __builtin_amdgcn_exp2f(fmaf(s[n][r][i], sc, -use));
 #pragma unroll
-                for (int i = 0; i < 2; ++i) split_pair<NP>(s[n][r][2 * i], s[n][r][2 * i + 1], part[r][i]);
+                for (int i = 0; i < 2; ++i) split_pair<NP>(e[r][2 * i], e[r][2 * i + 1], part[r][i]);
             }
 #pragma unroll
             for (int x = 0; x < NP; ++x) {
@@ -194,37 +186,31 @@ struct Columns {
                 for (int r = 0; r < NB; ++r) w[r] = make_uint2(part[r][0][x], part[r][1][x]);
                 spread(w, copy, pf[n][0][x], pf[n][1][x]);
             }
-        }
-        // Sums of P.  Of a whole tile as it enters the product, by a product with ones, which the matrix cores have more room for than the vector
-        // units; of copies, which have fewer terms a lane, by additions.
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            if constexpr (SHARE == 1) {
-                Frag ones;
-                ones.u = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-                f32x4v sum = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int x = NP - 1; x >= 0; --x)
-#pragma unroll
-                    for (int half = 0; half < 2; ++half) sum = mfma16(ones, pf[n][half][x], sum);
-                l[n] = fmaf(sum[0], per_f, l[n]);
-            } else {
-                float sum = 0.f;
+            if constexpr (SHARE > 1) {
+                sum[n] = 0.f;
 #pragma unroll
                 for (int r = 0; r < NB; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum += s[n][r][i];
-                l[n] = fmaf(sum, per_f, l[n]);
+                    for (int i = 0; i < 4; ++i) sum[n] += e[r][i];
             }
         }
-        // A code that not every column sees may be NaN (what is not yet written is anything), and 0 * NaN would reach the sums: such codes
-        // are 0 in the product, and the columns that do see one get their NaN from a product of flags.
-        if (edge) {
-            uint32_t bad = 0;
+        if constexpr (SHARE == 1) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c) bad |= nan_bytes(t.v[c].x) | nan_bytes(t.v[c].y) | nan_bytes(t.v[c].z) | nan_bytes(t.v[c].w);
-            if (__any(bad != 0)) take_nan_out(t, j0, there, window, sinks, copy, own);
+            for (int n = 0; n < NT; ++n) {
+                Frag ones;
+                ones.u = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+                f32x4v x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = NP - 1; i >= 0; --i)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) x = mfma16(ones, pf[n][half][i], x);
+                sum[n] = x[0];
+            }
         }
+    }
+
+    __device__ inline void add_values(const PagePart<D> &t, const Frag (&pf)[NT][2][NP], float power)
+    {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
@@ -236,11 +222,110 @@ struct Columns {
 #pragma unroll
                     for (int x = NP - 1; x >= 0; --x) acc[n][c] = mfma16(v, pf[n][half][x], acc[n][c]);
             }
-        __builtin_amdgcn_sched_barrier(0);
-        // The compiler has counted too few wait states from a loop's last product to moves of its result at the loop's head (seen with d = 32,
-        // where the sums' second half was stale): these are enough.
-        asm volatile("s_nop 7");
-        next_v();
+        wait_for_products();
+    }
+
+    // Items i, i + step, .. of the list, the first in `t`: what their keys add.  begin(i): whether the item's page is one of the pool's (none of
+    // another's keys are seen); next(i) goes on to it, load_k and load_v load it: once a page's keys are used, and its values, in their place,
+    // so that loads are in flight all the time with one set of registers.
+    //
+    // Most pages are seen whole and raise no maximum by much: their P is formed with the maximum at hand, and the sums, which are needed
+    // anyway, tell if a score was beyond 2^kLimit of it.  That one, and pages that are seen in part, take the long way, which looks for the
+    // maximum first.  (A loop of its own for the short way keeps the accumulators where they are: joined by one path, every page moved them twice.)
+    template <typename Begin, typename Next, typename LoadK, typename LoadV>
+    __device__ __forceinline__ void run(PagePart<D> &t, const PageList &list, int i, int step, float scale2, int window, int sinks, int lane, Begin begin, Next next, LoadK load_k,
+                               LoadV load_v)
+    {
+        constexpr float kLimit = 65536.f;                // (64 keys at 2^kSlack have 2^14)
+        const int quad = lane >> 4;
+        const int copy = SHARE > 1 ? (lane & 15) / (16 / SHARE) : 0, own = 4 * quad + 16 * copy;      // (a lane's block r is number SHARE r + copy)
+        bool ready = false;                              // every column has a maximum
+        while (i < list.count) {
+            f32x4v s[NT][NB];
+            Frag pf[NT][2][NP];
+            float sum[NT], sc, power, log2_more, less;
+            bool there, whole, done;
+            int j0;
+            do {
+                j0 = __builtin_amdgcn_readfirstlane(list.number(i)) * kPage;
+                there = begin(i);
+                scores(t, copy, s);
+                sc = fmaxf(t.k_scale * scale2, 0x1p-126f);           // (a page of zeros has scale 0, and 0 times -infinity is none)
+                i += step;
+                if (i < list.count) next(i);                         // (behind the last page that one again)
+                __builtin_amdgcn_sched_barrier(0);                   // (loads moved up over the products, or conversions over the exponentials, would need registers)
+                load_k();
+                // The values' scale is 2^e f, 1 <= f < 2: codes become bf16 with the power of two, and P is raised to P f by its exponent.
+                const uint32_t vbits = there && t.v_scale > 0.f ? __float_as_uint(t.v_scale) : 0x3f800000u;
+                const float f = __uint_as_float((vbits & 0x007fffffu) | 0x3f800000u);
+                power = __uint_as_float(vbits & 0x7f800000u);
+                log2_more = __builtin_amdgcn_logf(f);
+                less = __builtin_amdgcn_rcpf(f);
+                whole = there && j0 + kPage - 1 <= p0 && !(j0 <= p1 - window && j0 + kPage > sinks);
+                done = whole && ready;
+                if (done) {
+                    powers(s, sc, log2_more, copy, pf, sum);
+                    bool fine = true;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) fine &= sum[n] <= kLimit;
+                    done = __all(fine);
+                    if (done) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) l[n] = fmaf(sum[n], less, l[n]);
+                        add_values(t, pf, power);
+                        load_v();
+                    }
+                }
+            } while (done && i < list.count);
+            if (done) break;
+
+            if (!whole) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int hi = there ? p[n] - j0 - own : -1, lo = max(0, p[n] - window + 1) - j0 - own, first = sinks - j0 - own;
+#pragma unroll
+                    for (int r = 0; r < NB; ++r)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int at = 16 * SHARE * r + i;
+                            s[n][r][i] = (at <= hi) & ((at >= lo) | (at < first)) ? s[n][r][i] : -INFINITY;
+                        }
+                }
+            }
+            ready = true;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float top = -INFINITY;
+#pragma unroll
+                for (int r = 0; r < NB; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, s[n][r][i]);
+                top = quads_max(top) * sc;
+                const float m1 = top > m[n] + kSlack ? top : m[n];
+                const float fade = m[n] == m1 ? 1.f : __builtin_amdgcn_exp2f(m[n] - m1);
+                m[n] = m1;
+                ready &= p[n] < 0 || m1 != -INFINITY;
+                l[n] *= fade;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[n][c][i] *= fade;
+            }
+            ready = __all(ready);
+            powers(s, sc, log2_more, copy, pf, sum);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) l[n] = fmaf(sum[n], less, l[n]);
+            // A code that not every column sees may be NaN (what is not yet written is anything), and 0 * NaN would reach the sums: such codes
+            // are 0 in the product, and the columns that do see one get their NaN from a product of flags.
+            if (!whole) {
+                uint32_t bad = 0;
+#pragma unroll
+                for (int c = 0; c < NC; ++c) bad |= nan_bytes(t.v[c].x) | nan_bytes(t.v[c].y) | nan_bytes(t.v[c].z) | nan_bytes(t.v[c].w);
+                if (__any(bad != 0)) take_nan_out(t, j0, there, window, sinks, copy, own);
+            }
+            add_values(t, pf, power);
+            load_v();
+        }
     }
 
     __device__ inline float total(int n) const { return SHARE == 1 ? l[n] : quads_sum(l[n]); }
@@ -314,35 +399,6 @@ __device__ inline void query_parts(const T *p, Frag (&f)[NQ])
         for (int i = 0; i < NQ; ++i) f[i].u = make_uint4(part[0][i], part[1][i], part[2][i], part[3][i]);
     }
 }
-
-// The pages that positions p0 .. p1 see: those of the sinks before the window's, then the window's.
-struct PageList {
-    int sink_pages, first, count;
-    __device__ inline PageList(int p0, int p1, int window, int sinks)
-    {
-        first = max(0, p0 - window + 1) / kPage;
-        sink_pages = min((int)(((int64_t)sinks + kPage - 1) / kPage), first);
-        count = p1 < 0 ? 0 : sink_pages + p1 / kPage - first + 1;
-    }
-    __device__ inline int number(int i) const { return i < sink_pages ? i : first + i - sink_pages; }
-};
-
-// The pages that a wavefront takes, every `step`th from `begin` on: their numbers in the pool are loaded 64 at a time.
-struct Walk {
-    int ids, used;
-    __device__ inline void fill(const Pages &p, const PageList &list, int b, int i, int step)
-    {
-        const int at = i + (int)(threadIdx.x & 63) * step;
-        ids = at < list.count ? page_of(p, b, list.number(at)) : -1;
-        used = 0;
-    }
-    // of item i: begin, then the ones that follow in turn
-    __device__ inline int next(const Pages &p, const PageList &list, int b, int i, int step)
-    {
-        if (used == 64) fill(p, list, b, i, step);
-        return __builtin_amdgcn_readlane(ids, used++);
-    }
-};
 
 // The sums of KW wavefronts (and of SHARE copies in each) that share columns, joined in `red` and put out: results (of splits: parts) of
 // `columns` of them, to where `to` says.
