@@ -18,7 +18,7 @@ namespace {
 
 // Workgroup: WAVES wavefronts, CW of them beside each other over CW * NT * 16 columns of a row's key head, WAVES / CW over the pages.
 template <typename T, typename O, int D, int NQ, int NP, int NT, int CW, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D == 128 && sizeof(T) == 4 ? 1 : 2)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (sizeof(T) == 4 ? 1 : 2) : 3)
 attend_pages_kernel(AttendArgs a)
 {
     constexpr int KW = WAVES / CW, COLS = CW * NT * 16, NC = D / 16, NF = D / 32;
@@ -54,13 +54,15 @@ attend_pages_kernel(AttendArgs a)
     const int i = split * KW + kw;
     Walk walk;
     walk.fill(a.pages, list, row.b, i, step);
-    int page = walk.next(a.pages, list, row.b, i, step);
+    const int page = walk.next(a.pages, list, row.b, i, step);
     PagePart<D> t;
-    const auto load_k = [&] { t.load_k(a.pages, max(page, 0), hk, lane); };
-    const auto load_v = [&] { t.load_v(a.pages, max(page, 0), hk, lane); };
-    load_k();
-    load_v();
-    x.run(t, list, i, step, scale2, a.window, a.sinks, lane, [&](int) { return page >= 0; }, [&](int i) { page = walk.next(a.pages, list, row.b, i, step); }, load_k, load_v);
+    const auto load_k = [&](int page) { t.load_k(a.pages, max(page, 0), hk, lane); };
+    const auto load_v = [&](int page) { t.load_v(a.pages, max(page, 0), hk, lane); };
+    load_k(page);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(page);
+    x.template run<false>(t, list, i, step, page, scale2, a.window, a.sinks, lane, [&](int i) { return walk.next(a.pages, list, row.b, i, step); },
+                          load_k, load_v, [] {});
 
     if constexpr (KW == 1) {
 #pragma unroll

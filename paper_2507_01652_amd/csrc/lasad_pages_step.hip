@@ -174,13 +174,14 @@ struct NewKey {
 #pragma unroll
         for (int b = 0; b < 4; ++b)
 #pragma unroll
-            for (int w = 0; w < D / 16; ++w) t.k[b][w] = b == block && col == slot % 16 ? k[w] : t.k[b][w];
+            for (int w = 0; w < D / 16; ++w) {
+                constexpr int EACH = D == 32 ? 2 : 4;
+                t.k[b][w / EACH][w % EACH] = b == block && col == slot % 16 ? k[w] : t.k[b][w / EACH][w % EACH];
+            }
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-            const uint4 w = t.v[c];
-            const auto with = [&](uint32_t x, int b) { return b == block ? (x & keep) | (v[c] << shift & ~keep) : x; };
-            t.v[c] = make_uint4(with(w.x, 0), with(w.y, 1), with(w.z, 2), with(w.w, 3));
-        }
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+            for (int b = 0; b < 4; ++b) t.v[c][b] = b == block ? (t.v[c][b] & keep) | (v[c] << shift & ~keep) : t.v[c][b];
         t.k_scale = k_scale;
         t.v_scale = v_scale;
     }
@@ -188,7 +189,7 @@ struct NewKey {
 
 // T: type of q, k and v.  NQ, NP: bf16 parts of a query and of P.  SHARE: copies of the query heads in a tile of 16 columns.
 template <typename T, typename O, int D, int NQ, int NP, int SHARE, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (SHARE == 4 ? 2 : 1) : D == 64 && SHARE == 1 ? 2 : 3)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 ? 1 : D == 64 && (SHARE < 4 || sizeof(T) == 4) ? 2 : 3)
 step_pages_kernel(AppendArgs a, AttendArgs g)
 {
     constexpr int NF = D / 32, NC = D / 16, P = D / 2, EACH = 16 / SHARE;
@@ -219,14 +220,16 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         cs[threadIdx.x] = pair_angle<D>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
     int page = walk.next(a.pages, list, b, begin, step);
     PagePart<D> t;
-    const auto load_k = [&] { t.load_k(a.pages, max(page, 0), hk, lane); };
-    const auto load_v = [&] { t.load_v(a.pages, max(page, 0), hk, lane); };
-    load_k();
-    load_v();
+    const auto load_k = [&](int page) { t.load_k(a.pages, max(page, 0), hk, lane); };
+    const auto load_v = [&](int page) { t.load_v(a.pages, max(page, 0), hk, lane); };
+    load_k(page);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(page);
     __syncthreads();
     NewKey<D> fresh;
+    int last = -1;
     if (owner) {
-        const int last = list.count - 1 == begin ? page : page_of(a.pages, b, list.number(list.count - 1));
+        last = list.count - 1 == begin ? page : page_of(a.pages, b, list.number(list.count - 1));
         if (last >= 0) fresh.template append<T>(a, cs, rk, rv, hk, pos, last, lane);
     }
     for (int g0 = 0; g0 < G; g0 += EACH) {
@@ -235,8 +238,9 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
             rq.load(queries + min(g0 + col % EACH, G - 1) * D, quad);
             walk.fill(a.pages, list, b, begin, step);
             page = walk.next(a.pages, list, b, begin, step);
-            load_k();
-            load_v();
+            load_k(page);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v(page);
         }
         Columns<D, NQ, NP, 1, SHARE> x;
         {
@@ -257,18 +261,15 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         x.l[0] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) x.acc[0][c] = f32x4v{0.f, 0.f, 0.f, 0.f};
-        const auto take_up = [&](int i) __attribute__((always_inline)) {
-            const bool there = page >= 0;
-            if (i == list.count - 1 && there) {
-                if (fresh.grown) {
-                    load_k();
-                    load_v();
-                }
-                fresh.put(t, pos % kPage, lane);
+        const auto put_new = [&]() __attribute__((always_inline)) {
+            if (fresh.grown) {
+                load_k(last);
+                load_v(last);
             }
-            return there;
+            fresh.put(t, pos % kPage, lane);
         };
-        x.run(t, list, begin, step, g.scale * kLog2e, g.window, g.sinks, lane, take_up, [&](int i) { page = walk.next(a.pages, list, b, i, step); }, load_k, load_v);
+        x.template run<true>(t, list, begin, step, page, g.scale * kLog2e, g.window, g.sinks, lane, [&](int i) { return walk.next(a.pages, list, b, i, step); },
+                             load_k, load_v, put_new);
         join_waves<O, D, WAVES, SHARE>(red, x.acc[0], x.m[0], x.total(0), wave, lane, min(EACH, G - g0), g.splits, split, [&](int c, int ch) {
             const int64_t at = (int64_t)b * a.Hq + hk * G + g0 + c;
             return Result<O>{g.parts + at * g.splits * (D + 4), (O *)g.o + at * D + ch};

@@ -2,6 +2,8 @@
 // attention of packed queries and the step share.
 #pragma once
 
+#include <type_traits>
+
 #include "lasad_pages.h"
 
 namespace lasad {
@@ -46,41 +48,46 @@ __device__ inline void split_pair(float x, float y, uint32_t (&part)[N])
 
 __device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }     // 0x80 where a code is NaN
 
+// A number at an address that is the same in all lanes, through the scalar cache: one more vector load between those of the pages would have
+// the next page's keys wait for the values behind it.  (No kernel reads a scale like this that it has written.)
+__device__ inline float scalar_load(const float *p) { return *(const __attribute__((address_space(4))) float *)(uintptr_t)p; }
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 // A lane's share of a page: k of four blocks of 16 positions (its position of each, 16 channels of 64), v of all positions that the second
 // product has in its lane (its channel of every 16).
 template <int D>
 struct PagePart {
-    static constexpr int KW = D / 16;                    // words of k of a block
-    uint32_t k[4][KW];
-    uint4 v[D / 16];
+    static constexpr int KL = D == 32 ? 1 : D / 64;      // loads of k of a block
+    typedef typename std::conditional<D == 32, u32x2, u32x4>::type K;
+    K k[4][KL];
+    u32x4 v[D / 16];
     float k_scale, v_scale;
     __device__ inline void load_k(const Pages &p, int page, int h, int lane)
     {
         const int64_t at = (int64_t)page * p.heads + h;
         const int col = lane & 15, quad = lane >> 4;
-        const uint8_t *kp = p.k + at * kPage * D + col * D;
+        const uint8_t *kp = p.k + at * kPage * D + col * D + quad * sizeof(K);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            if (D == 32) {
-                const uint2 x = *(const uint2 *)(kp + b * 16 * D + quad * 8);
-                k[b][0] = x.x; k[b][1] = x.y;
-            } else {
+        for (int b = 0; b < 4; ++b)
 #pragma unroll
-                for (int c = 0; c < D / 64; ++c) {
-                    const uint4 x = *(const uint4 *)(kp + b * 16 * D + c * 64 + quad * 16);
-                    k[b][4 * c % KW] = x.x; k[b][(4 * c + 1) % KW] = x.y; k[b][(4 * c + 2) % KW] = x.z; k[b][(4 * c + 3) % KW] = x.w;
-                }
-            }
-        }
-        k_scale = p.k_scale[at];
+            for (int c = 0; c < KL; ++c) k[b][c] = *(const K *)(kp + b * 16 * D + c * 64);
+        k_scale = scalar_load(p.k_scale + at);
     }
     __device__ inline void load_v(const Pages &p, int page, int h, int lane)
     {
         const int64_t at = (int64_t)page * p.heads + h;
         const uint8_t *vp = p.v + at * kPage * D + (lane & 15) * kPage + (lane >> 4) * 16;
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) v[c] = *(const uint4 *)(vp + c * 16 * kPage);
-        v_scale = p.v_scale[at];
+        for (int c = 0; c < D / 16; ++c) v[c] = *(const u32x4 *)(vp + c * 16 * kPage);
+        v_scale = scalar_load(p.v_scale + at);
+    }
+    // words 2 f and 2 f + 1 of a block's k: the codes of reduction step f
+    __device__ inline uint32_t k_word(int b, int f, int i) const
+    {
+        if constexpr (D == 32) return k[b][0][i];
+        else return k[b][f >> 1][2 * (f & 1) + i];
     }
 };
 // first of a lane's eight channels in reduction step f of the first product
@@ -144,7 +151,7 @@ struct Columns {
         for (int b = 0; b < 4; ++b) {
             Frag k[NF];
 #pragma unroll
-            for (int f = 0; f < NF; ++f) k[f] = codes_frag(t.k[b][2 * f], t.k[b][2 * f + 1]);
+            for (int f = 0; f < NF; ++f) k[f] = codes_frag(t.k_word(b, f, 0), t.k_word(b, f, 1));
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 f32x4v x = {0.f, 0.f, 0.f, 0.f};
@@ -209,14 +216,14 @@ struct Columns {
         }
     }
 
-    __device__ inline void add_values(const PagePart<D> &t, const Frag (&pf)[NT][2][NP], float power)
+    __device__ inline void add_values(const u32x4 (&values)[NC], const Frag (&pf)[NT][2][NP], float power)
     {
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const Frag v = half ? codes_frag(t.v[c].z, t.v[c].w, power) : codes_frag(t.v[c].x, t.v[c].y, power);
+                const Frag v = half ? codes_frag(values[c].z, values[c].w, power) : codes_frag(values[c].x, values[c].y, power);
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -225,59 +232,87 @@ struct Columns {
         wait_for_products();
     }
 
-    // Items i, i + step, .. of the list, the first in `t`: what their keys add.  begin(i): whether the item's page is one of the pool's (none of
-    // another's keys are seen); next(i) goes on to it, load_k and load_v load it: once a page's keys are used, and its values, in their place,
-    // so that loads are in flight all the time with one set of registers.
+    // Items i, i + step, .. of the list, the first (in `page`) in `t`: what their keys add.  next(i): page of the next item, i (-1: none of the
+    // pool's; none of another's keys are seen); load_k(page), load_v(page) load it: once a page's keys are used, and its values, in their
+    // place, so that loads are in flight all the time with one set of registers.  finish() puts into the list's last page what is new in it.
     //
     // Most pages are seen whole and raise no maximum by much: their P is formed with the maximum at hand, and the sums, which are needed
-    // anyway, tell if a score was beyond 2^kLimit of it.  That one, and pages that are seen in part, take the long way, which looks for the
-    // maximum first.  (A loop of its own for the short way keeps the accumulators where they are: joined by one path, every page moved them twice.)
-    template <typename Begin, typename Next, typename LoadK, typename LoadV>
-    __device__ __forceinline__ void run(PagePart<D> &t, const PageList &list, int i, int step, float scale2, int window, int sinks, int lane, Begin begin, Next next, LoadK load_k,
-                               LoadV load_v)
+    // anyway, tell if a score was beyond 2^kLimit of it.  Then that page, and those that are seen in part, take the long way, which looks for
+    // the maximum first.  The short way has a loop of its own, and leaves it with the loads of a next page under way, as it goes round:
+    // joined with the long one, every page moved the accumulators twice; left with others, the compiler lets the next keys wait for the values
+    // behind them.
+    template <bool FINISH, typename Next, typename LoadK, typename LoadV, typename Finish>
+    __device__ __forceinline__ void run(PagePart<D> &t, const PageList &list, int i, int step, int page, float scale2, int window, int sinks, int lane, Next next,
+                                        LoadK load_k, LoadV load_v, Finish finish)
     {
         constexpr float kLimit = 65536.f;                // (64 keys at 2^kSlack have 2^14)
         const int quad = lane >> 4;
         const int copy = SHARE > 1 ? (lane & 15) / (16 / SHARE) : 0, own = 4 * quad + 16 * copy;      // (a lane's block r is number SHARE r + copy)
         bool ready = false;                              // every column has a maximum
-        while (i < list.count) {
-            f32x4v s[NT][NB];
-            Frag pf[NT][2][NP];
-            float sum[NT], sc, power, log2_more, less;
-            bool there, whole, done;
-            int j0;
-            do {
+        f32x4v s[NT][NB];
+        Frag pf[NT][2][NP];
+        float sum[NT], sc, power, log2_more, less;
+        bool there, whole;
+        int j0, taken = page;
+        const auto go_on = [&]() __attribute__((always_inline)) {
+            taken = page;
+            i += step;
+            if (i < list.count) page = next(i);                      // (behind the last page that one again)
+        };
+        const auto start = [&]() __attribute__((always_inline)) {
+            scores(t, copy, s);
+            sc = fmaxf(t.k_scale * scale2, 0x1p-126f);               // (a page of zeros has scale 0, and 0 times -infinity is none)
+        };
+        const auto load_next_k = [&]() __attribute__((always_inline)) {
+            __builtin_amdgcn_sched_barrier(0);                       // (loads moved up over the products, or conversions over the exponentials, would need registers)
+            load_k(page);
+            // The values' scale is 2^e f, 1 <= f < 2: codes become bf16 with the power of two, and P is raised to P f by its exponent.
+            const uint32_t vbits = there && t.v_scale > 0.f ? __float_as_uint(t.v_scale) : 0x3f800000u;
+            const float f = __uint_as_float((vbits & 0x007fffffu) | 0x3f800000u);
+            power = __uint_as_float(vbits & 0x7f800000u);
+            log2_more = __builtin_amdgcn_logf(f);
+            less = __builtin_amdgcn_rcpf(f);
+        };
+        enum { kDone, kLong, kAgain };
+        int left = i < list.count ? kLong : kDone;
+        while (left != kDone) {
+            for (;;) {
                 j0 = __builtin_amdgcn_readfirstlane(list.number(i)) * kPage;
-                there = begin(i);
-                scores(t, copy, s);
-                sc = fmaxf(t.k_scale * scale2, 0x1p-126f);           // (a page of zeros has scale 0, and 0 times -infinity is none)
-                i += step;
-                if (i < list.count) next(i);                         // (behind the last page that one again)
-                __builtin_amdgcn_sched_barrier(0);                   // (loads moved up over the products, or conversions over the exponentials, would need registers)
-                load_k();
-                // The values' scale is 2^e f, 1 <= f < 2: codes become bf16 with the power of two, and P is raised to P f by its exponent.
-                const uint32_t vbits = there && t.v_scale > 0.f ? __float_as_uint(t.v_scale) : 0x3f800000u;
-                const float f = __uint_as_float((vbits & 0x007fffffu) | 0x3f800000u);
-                power = __uint_as_float(vbits & 0x7f800000u);
-                log2_more = __builtin_amdgcn_logf(f);
-                less = __builtin_amdgcn_rcpf(f);
-                whole = there && j0 + kPage - 1 <= p0 && !(j0 <= p1 - window && j0 + kPage > sinks);
-                done = whole && ready;
-                if (done) {
-                    powers(s, sc, log2_more, copy, pf, sum);
-                    bool fine = true;
+                there = page >= 0;
+                whole = there && j0 + kPage - 1 <= p0 && !(j0 <= p1 - window && j0 + kPage > sinks) && !(FINISH && i == list.count - 1);
+                if (!whole || !ready) break;
+                start();
+                go_on();
+                load_next_k();
+                powers(s, sc, log2_more, copy, pf, sum);
+                bool fine = true;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) fine &= sum[n] <= kLimit;
-                    done = __all(fine);
-                    if (done) {
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) l[n] = fmaf(sum[n], less, l[n]);
-                        add_values(t, pf, power);
-                        load_v();
-                    }
+                for (int n = 0; n < NT; ++n) fine &= sum[n] <= kLimit;
+                if (!__all(fine)) {
+                    load_v(page);
+                    left = kAgain;
+                    break;
                 }
-            } while (done && i < list.count);
-            if (done) break;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) l[n] = fmaf(sum[n], less, l[n]);
+                add_values(t.v, pf, power);
+                load_v(page);
+                if (i >= list.count) {
+                    left = kDone;
+                    break;
+                }
+            }
+            if (left == kDone) break;
+            if (left == kAgain) {
+                load_k(taken);
+                load_v(taken);
+                start();
+            } else {
+                if (FINISH && there && i == list.count - 1) finish();
+                start();
+                go_on();
+            }
+            load_next_k();
 
             if (!whole) {
 #pragma unroll
@@ -317,14 +352,18 @@ struct Columns {
             for (int n = 0; n < NT; ++n) l[n] = fmaf(sum[n], less, l[n]);
             // A code that not every column sees may be NaN (what is not yet written is anything), and 0 * NaN would reach the sums: such codes
             // are 0 in the product, and the columns that do see one get their NaN from a product of flags.
+            u32x4 v[NC];
+#pragma unroll
+            for (int c = 0; c < NC; ++c) v[c] = t.v[c];
             if (!whole) {
                 uint32_t bad = 0;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) bad |= nan_bytes(t.v[c].x) | nan_bytes(t.v[c].y) | nan_bytes(t.v[c].z) | nan_bytes(t.v[c].w);
-                if (__any(bad != 0)) take_nan_out(t, j0, there, window, sinks, copy, own);
+                for (int c = 0; c < NC; ++c) bad |= nan_bytes(v[c].x) | nan_bytes(v[c].y) | nan_bytes(v[c].z) | nan_bytes(v[c].w);
+                if (__any(bad != 0)) take_nan_out(v, j0, there, window, sinks, copy, own);
             }
-            add_values(t, pf, power);
-            load_v();
+            add_values(v, pf, power);
+            load_v(page);
+            left = i < list.count ? kLong : kDone;
         }
     }
 
@@ -340,7 +379,7 @@ struct Columns {
         }
     }
 
-    __device__ inline void take_nan_out(PagePart<D> &t, int j0, bool there, int window, int sinks, int copy, int own)
+    __device__ inline void take_nan_out(u32x4 (&v)[NC], int j0, bool there, int window, int sinks, int copy, int own)
     {
         Frag seen[NT][2];
 #pragma unroll
@@ -361,14 +400,14 @@ struct Columns {
         }
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-            uint32_t w[4] = {t.v[c].x, t.v[c].y, t.v[c].z, t.v[c].w}, flag[4];
+            uint32_t w[4] = {v[c].x, v[c].y, v[c].z, v[c].w}, flag[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint32_t nan = nan_bytes(w[i]) >> 7;
                 w[i] &= ~(nan * 0xffu);
                 flag[i] = nan * 0x38u;                               // (the code of 1)
             }
-            t.v[c] = make_uint4(w[0], w[1], w[2], w[3]);
+            v[c] = u32x4{w[0], w[1], w[2], w[3]};
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 f32x4v count = {0.f, 0.f, 0.f, 0.f};
