@@ -9,9 +9,6 @@
 // applied to the scores and to P in fp32.  fp32 queries and P are three bf16 parts each.
 #include "lasad_pages_tile.h"
 
-#ifndef LASAD_NT
-#define LASAD_NT 2
-#endif
 namespace lasad {
 
 namespace {
@@ -153,16 +150,24 @@ join_pages_kernel(AttendArgs a)
     store4((O *)a.o + token * a.lo.stride_n + h * a.lo.stride_h + ch, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
+// Workgroups of 128 columns from which on they are taken instead of 64 (bf16, d up to 64; a page's codes are then turned into bf16 once for 32 columns,
+// not 16, by three wavefronts a SIMD instead of four).  12 heads, window 512: 288 workgroups 11.8 us, with 64 columns 9.0; 480 17.2 and 18.3; 1632
+// 53.6 and 65.3.
+constexpr int64_t kFull = 384;
+
 // How a launch divides its columns.
 struct Shape {
-    int nt, cw, waves;
+    int nt, cw;
     int columns() const { return 16 * nt * cw; }
 };
 Shape choose(const AttendArgs &a)
 {
-    const int64_t columns = (int64_t)a.rows.tokens * (a.Hq / a.pages.heads);
-    if (columns <= 32 * (int64_t)a.rows.B) return {1, 1, 4};
-    return {a.io_dtype == LASAD_BF16 && a.d <= 64 ? LASAD_NT : 1, 4, 4};
+    const int G = a.Hq / a.pages.heads;
+    const int64_t columns = (int64_t)a.rows.tokens * G;
+    if (columns <= 32 * (int64_t)a.rows.B) return {1, 1};
+    const Shape wide = {2, 4};
+    const bool full = row_slots(a.rows, G, wide.columns(), 1) * a.pages.heads >= kFull;
+    return {a.io_dtype == LASAD_BF16 && a.d <= 64 && full ? 2 : 1, 4};
 }
 int64_t groups_of(const AttendArgs &a, const Shape &s) { return row_slots(a.rows, a.Hq / a.pages.heads, s.columns(), 1) * a.pages.heads; }
 
@@ -177,8 +182,9 @@ hipError_t launch(const AttendArgs &a, hipStream_t s)
 {
     const Shape shape = choose(a);
     const dim3 grid((unsigned)groups_of(a, shape), (unsigned)a.splits);
-    constexpr int WIDE = sizeof(T) == 2 && D <= 64 ? LASAD_NT : 1;
+    constexpr int WIDE = sizeof(T) == 2 && D <= 64 ? 2 : 1;
     if (shape.cw == 1) attend_pages_kernel<T, O, D, NP, NP, 1, 1, 4><<<grid, dim3(256), 0, s>>>(a);
+    else if (shape.nt == 1) attend_pages_kernel<T, O, D, NP, NP, 1, 4, 4><<<grid, dim3(256), 0, s>>>(a);
     else attend_pages_kernel<T, O, D, NP, NP, WIDE, 4, 4><<<grid, dim3(256), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
