@@ -75,8 +75,8 @@ append_pages_kernel(AppendArgs a, int groups)
     const int group = blockIdx.x % groups;
     PageRow row;
     if (!find_row(a.rows, a.pages, blockIdx.x / groups, 1, kPage, 2, row)) return;
+    if (row.unit > (row.pos % kPage + row.n - 1) / kPage) return;
     const int j = row.pos / kPage + row.unit;
-    if (j * kPage >= row.pos + row.n) return;
     const int begin = max(row.pos - j * kPage, 0), end = min(row.pos + row.n - j * kPage, kPage);      // the call's positions in the page
     const int64_t token0 = (int64_t)row.first + j * kPage - row.pos;                                  // token of the page's position 0
     const int entry = page_of(a.pages, row.b, j);

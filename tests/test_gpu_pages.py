@@ -247,6 +247,25 @@ def test_append_in_place_and_broadcast(lasad):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+def test_append_strides_of_16_mb(lasad):
+    """Tokens further apart than offsets of 24 bits reach."""
+    d, Hq, Hk, far = 64, 2, 1, 2 ** 23 + 8
+    rows = packed([3, 2], [62, 5])
+    table = table_of(rows, 4, 3)
+    for dt in (BF, F):
+        base = ref.draw((5, Hq + 2 * Hk, d), dt, 9).cuda()
+        wide = torch.zeros(4 * far + (Hq + 2 * Hk) * d, dtype=dt, device="cuda").as_strided((5, Hq + 2 * Hk, d), (far, d, 1))
+        wide.copy_(base)
+        out = []
+        for x in (base, wide):
+            pages = pr.filled_pool(lasad, 4, Hk, d, 11)
+            t, pos, starts = on_gpu(table, rows)
+            q = lasad.lasad_append_pages(*x.split((Hq, Hk, Hk), 1), pages, t, pos, 16, 16, row_starts=starts)
+            out.append([q.clone()] + [p.view(torch.uint8) for p in pages])
+        for a, b in zip(*out):
+            assert torch.equal(a, b)
+
+
 # dtype, out dtype, d, Hq, Hk, lengths, positions, window, sinks
 ATTENDS = [
     (BF, BF, 64, 2, 2, [130], [0], 50, 0),
@@ -391,6 +410,59 @@ def test_attention_scores_that_move_the_maximum(lasad, dt):
             assert ((o - want).abs() <= bound).all(), (kind, ((o - want).abs() / bound).max().item())
 
 
+@pytest.mark.parametrize("dt, d, Hq, Hk", [(BF, 64, 24, 24), (BF, 32, 26, 26), (BF, 128, 8, 4), (F, 64, 8, 4)])
+@pytest.mark.parametrize("kind", range(3))
+def test_attention_of_many_columns(lasad, dt, d, Hq, Hk, kind):
+    """A launch that fills the chip, where a wavefront has two tiles of columns (bf16, d up to 64): pages seen whole and in part, the last ones
+    with NaN behind the rows' ends; scales alike (0), rising by 4 from page to page (1), and a jump that no exponential of the maximum before
+    holds in fp32 (2)."""
+    lengths, positions, window, sinks = [1000, 920], [30, 0], 500, 70
+    rows = packed(lengths, positions)
+    T = sum(lengths)
+    table = table_of(rows, 34, 8)
+    pages = pr.filled_pool(lasad, 34, Hk, d, 12)
+    if kind:
+        lift = torch.zeros(34)
+        for b in range(2):
+            for j in range(table.shape[1]):
+                if table[b, j] >= 0:
+                    lift[table[b, j]] = 0.25 * j if kind == 1 else 9.0 if j in (3, 9) else 0.0
+        pages.k_scales.mul_((2 ** lift)[:, None].cuda())
+    spoil(pages, table, rows)
+    q = ref.draw((T, Hq, d), dt, 3).cuda()
+    t, pos, starts = on_gpu(table, rows)
+    o = lasad.lasad_forward_pages(q, pages, t, pos, window, sinks, row_starts=starts).cpu().double()
+    want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, window, sinks, d ** -0.5, dt, dt)
+    # (fp64 has exponentials that fp32 has not: those below 2^-126 of the largest are 0 there; 2^10 of them times values below 2^4)
+    assert ((o - want).abs() <= bound + 2.0 ** -112).all(), ((o - want).abs() / bound).max().item()
+
+
+def test_pools_beyond_2_gib(lasad):
+    """Pages whose codes lie beyond 2^31 bytes from the pool's first."""
+    d, Hq, Hk, n = 64, 4, 2, 2 ** 18 + 9                   # 2 GiB and 72 KiB of keys, as much of values
+    small = pr.filled_pool(lasad, 9, Hk, d, 12)
+    pages = lasad.new_pages(n, Hk, d)
+    far = torch.arange(n - 9, n)
+    for big, few in zip(pages, small):
+        big[n - 9:].view(torch.uint8).copy_(few.view(torch.uint8))
+    rows = packed([70, 100], [100, 40])
+    near_table = table_of(rows, 9, 8)
+    table = torch.where(near_table >= 0, near_table + (n - 9), near_table)
+    assert int(table.max()) * Hk * 64 * d > 2 ** 31 - 2 ** 20
+    q, k, v = project(170, Hq, Hk, d, BF, 3)
+    out = []
+    for tb, pool in ((table, pages), (near_table, small)):
+        t, pos, starts = on_gpu(tb, rows)
+        qr = lasad.lasad_append_pages(q, k, v, pool, t, pos, 16, 16, row_starts=starts)
+        o = lasad.lasad_forward_pages(qr, pool, t, pos, 90, 3, row_starts=starts)
+        step = [x[:2].contiguous() for x in (q, k, v)]
+        end = torch.tensor([170, 140], dtype=torch.int32).cuda()
+        z = lasad.lasad_decode_step_pages(*step, pool, t, end, 16, 16, 90, 3)
+        out.append([qr, o, z] + [x[-9:].view(torch.uint8) for x in pool])
+    for a, b in zip(*out):
+        assert torch.equal(a, b)
+
+
 def test_rows_that_share_pages(lasad):
     """A common beginning lies in the tables of several rows."""
     pages = pr.filled_pool(lasad, 8, 2, 64, 1)
@@ -463,6 +535,40 @@ def query_bound(yq, eq, pages, table, rows, window, sinks, scale, dt):
         worst = torch.expm1(2 * off.amax(0))
         out[b] = (prob[..., None] * v.abs()).sum(0) * worst[:, None]
     return out
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("Hq", [2, 12, 40])
+def test_step_scores_that_move_the_maximum(lasad, Hq, dt):
+    """One, six and twenty query heads a key head; scores that rise and jump from page to page, pages of zeros, one that is not there."""
+    d, Hk, B, grid, window = 64, 2, 2, (40, 40), 2 ** 20
+    positions = [1100, 700]
+    rows = [(b, 1, p) for b, p in enumerate(positions)]
+    for kind in range(3):
+        table = table_of(rows, 30, 8)
+        pages = pr.filled_pool(lasad, 30, Hk, d, 12)
+        lift = torch.zeros(30)
+        for b in range(B):
+            for j in range(table.shape[1]):
+                if table[b, j] >= 0:
+                    lift[table[b, j]] = (0.25 * j, 9.0 if j in (5, 9) else 0.0, 0.0)[kind]
+        pages.k_scales.mul_((2 ** lift)[:, None].cuda())
+        if kind == 2:
+            zero = int(table[0, 4])
+            for t in pages:
+                t.view(torch.uint8)[zero] = 0
+            table[1, 2] = -1
+        before = cpu(pages)
+        q, k, v = (t.contiguous() for t in project(B, Hq, Hk, d, dt, 50 + kind))
+        t, pos, _ = on_gpu(table, rows)
+        yk, ek = expected(k, None, rows, B, grid[1], 2, False, EPS, dt)
+        yq, eq = expected(q, None, rows, B, grid[1], 2, False, EPS, dt)
+        o = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, *grid, window).cpu().double()
+        pr.check_append(before, cpu(pages), table, rows, grid[0] * grid[1], yk, ek, v.cpu().double())
+        want, bound = pr.attend(yq, cpu(pages), table, rows, LAST, window, 0, d ** -0.5, dt, dt)
+        bound = bound + query_bound(yq, eq, cpu(pages), torch.where(table < 0, table[0, 0], table), rows, window, 0, d ** -0.5, dt)
+        # (2^10 terms below 2^-126 of the largest, which fp32 does not hold, values below 2^4)
+        assert ((o - want).abs() <= bound + 2.0 ** -112).all(), (kind, ((o - want).abs() / bound).max().item())
 
 
 def test_step_inactive_rows(lasad):
