@@ -140,7 +140,7 @@ append_pages_kernel(AppendArgs a, int groups)
     if constexpr (TURN != kNone) {
         const int pair = tid % P;
         const double f = pair_turns<D>(a.rope, pair, a.log2_base);
-        for (int t = begin + tid / P; t < end; t += kThreads / P) cs[t * P + pair] = pair_angle<D>(a.rope, pair, j * kPage + t, a.grid_w, f);
+        for (int t = begin + tid / P; t < end; t += kThreads / P) cs[t * P + pair] = pair_angle<D, true>(a.rope, pair, j * kPage + t, a.grid_w, f);
         __syncthreads();
     }
     const int page = __builtin_amdgcn_readfirstlane(entry), units = q_heads + (page < 0 ? 0 : 2 * heads);

@@ -217,7 +217,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         for (int c = 0; c < NC; ++c) rv[c] = ((const T *)a.v)[at + 16 * c + col];
     }
     if (a.rope != LASAD_ROPE_NONE && threadIdx.x < P)
-        cs[threadIdx.x] = pair_angle<D>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
+        cs[threadIdx.x] = pair_angle<D, true>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
     int page = walk.next(a.pages, list, b, begin, step);
     PagePart<D> t;
     const auto load_k = [&](int page) { t.load_k(a.pages, max(page, 0), hk, lane); };
