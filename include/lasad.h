@@ -603,7 +603,7 @@ int lasad_decode_step_window(const void *q, const void *k, const void *v, void *
  * e4m3 codes (finite up to 448, 0x7f and 0xff NaN) with a scale for each page and head: k = code * scale.
  *   k_pages   [n_pages, n_k_heads, 64, d] bytes:  position t of the page, channel c.
  *   v_pages   [n_pages, n_k_heads, d, 64] bytes:  channel c, position t = 16 b + 4 g + i (b, g, i in 0 .. 3) at 16 g + 4 b + i.
- *   k_scales, v_scales  [n_pages, n_k_heads] fp32; 0: all codes of the page are 0.
+ *   k_scales, v_scales  [n_pages, n_k_heads] fp32, 0 (all codes of the page are 0) or a normal number.
  *   table     int32, device: row b's positions 64 j .. 64 j + 63 lie in page table[b * table_stride + j], j < table_pages.  A number that
  *             is none of the pool's (-1, say: given back once it has left the window) is not read or written: its keys are not seen.
  * Pages that a call appends to belong to one row; others may lie in the tables of several (a common beginning).  What lies behind the
@@ -660,7 +660,8 @@ int lasad_forward_pages(const void *q, void *o, const lasad_layout_t *q_layout, 
 
 /*
  * Both for one token of every row: q, k (before their norms and rotation) and v [B, heads, d] contiguous; k and v are appended, o
- * [B, n_q_heads, d] contiguous is the attention of the token over its row's pages, its own key among them.
+ * [B, n_q_heads, d] contiguous is the attention of the token over its row's pages, its own key among them.  The queries are not rounded to
+ * io_dtype on the way: they enter the products, as P does, in two bf16 parts (three with fp32).
  */
 size_t lasad_decode_step_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int table_pages, int window, int sinks);
 int lasad_decode_step_pages(const void *q, const void *k, const void *v, void *o, const lasad_pages_t *pages,

@@ -5,8 +5,17 @@
 // A wavefront takes a page at a time for tiles of 16 columns; the columns of a row are its (token, query head of the key head's group) pairs in
 // order, so that heads that share keys read them once.  Scores are formed transposed, 16 positions x 16 columns: a column's numbers are then four
 // registers of each of four lanes, and as they lie there they are the second operand of the product with v, whose first operand is 16 bytes of a
-// page a lane (lasad_pages.h).  Nothing passes through LDS but the join of wavefronts that share columns.  Codes become bf16 exactly, scales are
-// applied to the scores and to P in fp32.  fp32 queries and P are three bf16 parts each.
+// page a lane (lasad_pages.h).  Nothing passes through LDS but the join of wavefronts that share columns.  Codes become bf16 exactly; a page's
+// scale of k is applied to the scores in fp32, that of v as a power of two with the conversion and the rest in P's exponent.  fp32 queries and P
+// are three bf16 parts each; of bf16 queries P is one, rounded to 2^-9, which is what o's own rounding costs: more parts would
+// double the second product.  Its sums are those of the rounded P.
+//
+// 4 x 24 heads over 8, 4096 tokens, window 1024, d = 64: 137 us a pass in a stream, 91 GFLOP, 668 TFLOP/s where a product of 8192^3 reaches 1199.
+// The matrix cores are busy for 0.29 of the time, the vector units for 0.55 (exponentials, conversions of codes and of P, 150 instructions a page
+// of 64 keys and 32 columns), and three wavefronts a SIMD do not always have one of each.  On the way: sums of P by additions and both
+// scales by products 343; with the search for a maximum in every page 197; with the accumulators moved twice a page by it 167; with keys that
+// waited for the values behind them 154; 48 columns a wavefront 151 then, 64 176, 16 200.  Rows of 128 to 256 tokens (12 heads, window 128): 8.5 us, a
+// launch and four to six pages one behind the other.
 #include "lasad_pages_tile.h"
 
 namespace lasad {
