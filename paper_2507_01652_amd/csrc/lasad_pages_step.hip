@@ -52,9 +52,9 @@ struct RawHead {
     }
 };
 
-// Its norm, weight (NULL: ones) and rotation by the table cs.
+// Its norm, weights (read where `weighted`) and rotation by the table cs.
 template <int D>
-__device__ inline void norm_and_turn(const AppendArgs &a, const float *w, const float2 *cs, int quad, float (&y)[D / 32][8])
+__device__ inline void norm_and_turn(const AppendArgs &a, bool weighted, const RawHead<float, D> &w, const float2 *cs, int quad, float (&y)[D / 32][8])
 {
     constexpr int NF = D / 32;
     if (a.norm) {
@@ -68,11 +68,9 @@ __device__ inline void norm_and_turn(const AppendArgs &a, const float *w, const 
         for (int f = 0; f < NF; ++f)
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[f][e] *= rstd;
-        if (w) {
+        if (weighted) {
             float x[NF][8];
-            RawHead<float, D> raw;
-            raw.load(w, quad);
-            raw.unpack(x);
+            w.unpack(x);
 #pragma unroll
             for (int f = 0; f < NF; ++f)
 #pragma unroll
@@ -120,9 +118,10 @@ struct NewKey {
     float k_scale, v_scale;
     bool grown;                                          // the page's earlier codes have changed
 
-    // rk, rv: the key's channels and channel 16 c + lane % 16 of the value
+    // rk, rv: the key's channels and channel 16 c + lane % 16 of the value; w: the key's weights; k_old, v_old: the page's scales before
     template <typename T>
-    __device__ inline void append(const AppendArgs &a, const float2 *cs, const RawHead<T, D> &rk, const T (&rv)[D / 16], int hk, int pos, int page, int lane)
+    __device__ inline void append(const AppendArgs &a, const float2 *cs, const RawHead<T, D> &rk, const T (&rv)[D / 16], const RawHead<float, D> &w, float k_old,
+                                  float v_old, int hk, int pos, int page, int lane)
     {
         constexpr int NF = D / 32, NC = D / 16;
         const int quad = lane >> 4, col = lane & 15, slot = pos % kPage;
@@ -131,8 +130,7 @@ struct NewKey {
         rk.unpack(y);
 #pragma unroll
         for (int c = 0; c < NC; ++c) x[c] = as_float<T>(rv[c]);
-        const float k_old = a.pages.k_scale[ph], v_old = a.pages.v_scale[ph];
-        norm_and_turn<D>(a, a.w[1] ? a.w[1] + (a.shared ? 0 : hk * D) : nullptr, cs, quad, y);
+        norm_and_turn<D>(a, a.w[1] != nullptr, w, cs, quad, y);
         float k_most = 0.f, v_most = 0.f;
 #pragma unroll
         for (int f = 0; f < NF; ++f)
@@ -140,8 +138,10 @@ struct NewKey {
             for (int e = 0; e < 8; ++e) k_most = fmaxf(k_most, finite_size(y[f][e]));
 #pragma unroll
         for (int c = 0; c < NC; ++c) v_most = fmaxf(v_most, finite_size(x[c]));
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) v_most = fmaxf(v_most, __shfl_xor(v_most, off));
+        v_most = fmaxf(v_most, dpp_move<0xB1>(v_most));
+        v_most = fmaxf(v_most, dpp_move<0x4E>(v_most));
+        v_most = fmaxf(v_most, dpp_move<0x141>(v_most));
+        v_most = fmaxf(v_most, dpp_move<0x140>(v_most));
         uint8_t *kp = a.pages.k + ph * kPage * D, *vp = a.pages.v + ph * kPage * D;
         float k_less, v_less;
         k_scale = page_scale(quads_max(k_most), slot, k_old, k_less);
@@ -195,7 +195,7 @@ struct NewKey {
 
 // T: type of q, k and v.  NQ, NP: bf16 parts of a query and of P.  SHARE: copies of the query heads in a tile of 16 columns.
 template <typename T, typename O, int D, int NQ, int NP, int SHARE, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D == 128 ? 1 : D == 64 && (SHARE < 4 || sizeof(T) == 4) ? 2 : 3)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 ? 1 : D == 64 && (SHARE == 1 || sizeof(T) == 4) ? 2 : 3)
 step_pages_kernel(AppendArgs a, AttendArgs g)
 {
     constexpr int NF = D / 32, NC = D / 16, P = D / 2, EACH = 16 / SHARE;
@@ -208,40 +208,51 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, quad = lane >> 4, col = lane & 15;
     const PageList list(pos, pos, g.window, g.sinks);
     const int step = g.splits * WAVES, begin = split * WAVES + wave;
-    // everything that the first page needs is on its way before anything is waited for
+    // Everything that the first page, the queries and the new key need is on its way before anything is waited for, what is needed first in front:
+    // their norms and codes are formed while the page's codes come.
     Walk walk;
     walk.fill(a.pages, list, b, begin, step);
     RawHead<T, D> rq, rk;
+    RawHead<float, D> wq, wk;
     T rv[NC];
     const T *queries = (const T *)a.q + ((int64_t)b * a.Hq + hk * G) * D;
     const bool owner = (list.count - 1) % step == begin;               // the wavefront that has the row's last page
-    rq.load(queries + min(col % EACH, G - 1) * D, quad);
+    const auto load_queries = [&](int g0) {
+        const int h = min(g0 + col % EACH, G - 1);
+        rq.load(queries + h * D, quad);
+        if (a.w[0]) wq.load(a.w[0] + (a.shared ? 0 : (hk * G + h) * D), quad);
+    };
+    int last = -1;
+    float k_old = 0.f, v_old = 0.f;
     if (owner) {
         const int64_t at = ((int64_t)b * heads + hk) * D;
         rk.load((const T *)a.k + at, quad);
+        if (a.w[1]) wk.load(a.w[1] + (a.shared ? 0 : hk * D), quad);
 #pragma unroll
         for (int c = 0; c < NC; ++c) rv[c] = ((const T *)a.v)[at + 16 * c + col];
+        const int entry = scalar_load(a.pages.table + b * a.pages.table_stride + list.number(list.count - 1));
+        last = entry < a.pages.n_pages ? max(entry, -1) : -1;
+        k_old = scalar_load(a.pages.k_scale + (int64_t)max(last, 0) * heads + hk);
+        v_old = scalar_load(a.pages.v_scale + (int64_t)max(last, 0) * heads + hk);
     }
-    if (a.rope != LASAD_ROPE_NONE && threadIdx.x < P)
-        cs[threadIdx.x] = pair_angle<D, true>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
+    load_queries(0);
     int page = walk.next(a.pages, list, b, begin, step);
     PagePart<D> t;
     const auto load_k = [&](int page) { t.load_k(a.pages, max(page, 0), hk, lane); };
     const auto load_v = [&](int page) { t.load_v(a.pages, max(page, 0), hk, lane); };
+    __builtin_amdgcn_sched_barrier(0);
     load_k(page);
     __builtin_amdgcn_sched_barrier(0);
     load_v(page);
+    if (a.rope != LASAD_ROPE_NONE && threadIdx.x < P)
+        cs[threadIdx.x] = pair_angle<D, true>(a.rope, threadIdx.x, pos, a.grid_w, pair_turns<D>(a.rope, threadIdx.x, a.log2_base));
     __syncthreads();
     NewKey<D> fresh;
-    int last = -1;
-    if (owner) {
-        last = list.count - 1 == begin ? page : page_of(a.pages, b, list.number(list.count - 1));
-        if (last >= 0) fresh.template append<T>(a, cs, rk, rv, hk, pos, last, lane);
-    }
-    for (int g0 = 0; g0 < G; g0 += EACH) {
+    if (last >= 0) fresh.template append<T>(a, cs, rk, rv, wk, k_old, v_old, hk, pos, last, lane);
+    for (int g0 = 0; g0 < (SHARE > 1 ? 1 : G); g0 += EACH) {               // (copies: all of the heads at once)
         if (g0 > 0) {
             __syncthreads();                             // (the sums of the heads before are out of LDS)
-            rq.load(queries + min(g0 + col % EACH, G - 1) * D, quad);
+            load_queries(g0);
             walk.fill(a.pages, list, b, begin, step);
             page = walk.next(a.pages, list, b, begin, step);
             load_k(page);
@@ -252,7 +263,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
         {
             float y[NF][8];
             rq.unpack(y);
-            norm_and_turn<D>(a, a.w[0] ? a.w[0] + (a.shared ? 0 : (hk * G + min(g0 + col % EACH, G - 1)) * D) : nullptr, cs, quad, y);
+            norm_and_turn<D>(a, a.w[0] != nullptr, wq, cs, quad, y);
 #pragma unroll
             for (int f = 0; f < NF; ++f) {
                 uint32_t part[4][NQ];

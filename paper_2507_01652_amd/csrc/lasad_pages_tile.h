@@ -49,8 +49,9 @@ __device__ inline void split_pair(float x, float y, uint32_t (&part)[N])
 __device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }     // 0x80 where a code is NaN
 
 // A number at an address that is the same in all lanes, through the scalar cache: one more vector load between those of the pages would have
-// the next page's keys wait for the values behind it.  (No kernel reads a scale like this that it has written.)
-__device__ inline float scalar_load(const float *p) { return *(const __attribute__((address_space(4))) float *)(uintptr_t)p; }
+// the next page's keys wait for the values behind it.  (No kernel reads what it has written like this.)
+template <typename T>
+__device__ inline T scalar_load(const T *p) { return *(const __attribute__((address_space(4))) T *)(uintptr_t)p; }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
