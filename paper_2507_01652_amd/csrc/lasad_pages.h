@@ -57,7 +57,7 @@ struct AttendArgs {
     float scale;
     Pages pages;
     PageRows rows;
-    float *parts;                                        // workspace of splits: [tokens * Hq][splits][d + 2]
+    float *parts;                                        // workspace of splits: [tokens * Hq][splits][d + 4]: sums, maximum, sum of P
     int splits;
 };
 hipError_t launch_attend_pages(const AttendArgs &a, hipStream_t s);

@@ -8,8 +8,8 @@
 // again, unless the page's scale had to grow.
 //
 // bf16 queries are two bf16 parts and so is P: what a step adds to o's error is far below o's own rounding.  Bound by memory where there is enough:
-// 128 rows of 20 heads that see 24 to 4001 keys (767 MB) 152 us, 5.0 TB/s; 64 rows of 24 heads over 8, 1040 keys (58 MB) 16 us, 3.6; two rows of
-// 16 heads, 16448 keys (67 MB) 15.6 in 16 parts and 4 for their join; one row of 12 heads 7.5, the chain position, page, codes, norms, products,
+// 128 rows of 20 heads that see 24 to 4001 keys (767 MB) 151 us, 5.1 TB/s; 64 rows of 24 heads over 8, 1040 keys (58 MB) 15.1 us, 3.9; two rows of
+// 16 heads, 16448 keys (67 MB) 14 in 16 parts and 4 for their join; one row of 12 heads 6.7, of which the launch, position and table take 2.3: the chain position, page, codes, norms, products,
 // join.  With up to eight query heads a key head a tile holds copies of them (Columns): 16 columns for 3 heads would
 // raise four times as many scores to powers.
 #include "lasad_heads.h"
@@ -209,7 +209,7 @@ step_pages_kernel(AppendArgs a, AttendArgs g)
     const PageList list(pos, pos, g.window, g.sinks);
     const int step = g.splits * WAVES, begin = split * WAVES + wave;
     // Everything that the first page, the queries and the new key need is on its way before anything is waited for, what is needed first in front:
-    // their norms and codes are formed while the page's codes come.
+    // their norms and codes are formed while the page's codes come (weights and old scales loaded where they are used: 15.8 us for 64 rows, 15.2 so).
     Walk walk;
     walk.fill(a.pages, list, b, begin, step);
     RawHead<T, D> rq, rk;
@@ -317,7 +317,7 @@ hipError_t launch(const AppendArgs &a, const AttendArgs &t, hipStream_t s)
 
 int64_t step_pages_groups(const AttendArgs &t) { return (int64_t)t.rows.B * t.pages.heads * t.splits; }
 
-// Splits of a step whose rows see up to `seen` keys: for 512 workgroups in all (two rows of 16 heads, 16448 keys: 19.6 us; for 256 20.7, 1024 21.5).
+// Splits of a step whose rows see up to `seen` keys: for 512 workgroups in all (two rows of 16 heads, 16448 keys: 19.6 us; for 256 20.7, 1024 21.5, each a little less since).
 int step_pages_splits(int64_t B, int Hq, int Hk, int64_t seen)
 {
     int64_t n = 512 / (B * Hk);
