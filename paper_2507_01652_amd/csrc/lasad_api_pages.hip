@@ -97,7 +97,7 @@ int append_args(const void *q, const void *k, const void *v, void *q_out,
     a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.Hq = n_q_heads; a.d = d;
     a.w[0] = q_weight; a.w[1] = k_weight; a.shared = shared_weight != 0; a.norm = o.norm; a.eps = o.eps;
     a.rope = rope; a.pairing = pairing; a.grid_w = grid_w; a.log2_base = o.log2_base;
-    return check_groups(lasad::append_pages_groups(a));
+    return LASAD_OK;
 }
 
 }  // namespace
@@ -116,6 +116,7 @@ int lasad_append_pages(const void *q, const void *k, const void *v, void *q_out,
     if (int rc = append_args(q, k, v, q_out, q_layout, k_layout, v_layout, q_out_layout, pages, io_dtype, out_dtype, B, n_q_heads, n_k_heads, d, grid_h, grid_w,
                              n_tokens, row_starts, pos, pos_rows, q_weight, k_weight, shared_weight, norm_eps, rope, pairing, rope_base, a)) return rc;
     if (n_tokens == 0) return LASAD_OK;
+    if (int rc = check_groups(lasad::append_pages_groups(a))) return rc;
     const hipError_t e = lasad::launch_append_pages(a, (hipStream_t)hip_stream);
     if (e != hipSuccess) return hip_fail("lasad_append_pages launch", e);
     return LASAD_OK;

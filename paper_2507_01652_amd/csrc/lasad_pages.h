@@ -46,7 +46,7 @@ struct AppendArgs {
     PageRows rows;
 };
 hipError_t launch_append_pages(const AppendArgs &a, hipStream_t s);
-int64_t append_pages_groups(const AppendArgs &a);
+int64_t append_pages_groups(const AppendArgs &a);         // of a launch, in workgroups of 256 threads
 
 struct AttendArgs {
     const void *q;

@@ -278,12 +278,12 @@ int head_groups(const AppendArgs &a)
 
 }  // namespace
 
-int64_t append_pages_groups(const AppendArgs &a) { return slots_of(a) * head_groups(a); }
+int64_t append_pages_groups(const AppendArgs &a) { return slots_of(a) * head_groups(a) * (kThreads / 256); }
 
 hipError_t launch_append_pages(const AppendArgs &a, hipStream_t s)
 {
     const int groups = head_groups(a);
-    const dim3 grid((unsigned)append_pages_groups(a)), block(kThreads);
+    const dim3 grid((unsigned)(slots_of(a) * groups)), block(kThreads);
     const int turn = a.rope == LASAD_ROPE_NONE ? kNone : a.pairing == LASAD_PAIR_ADJACENT ? kAdjacent : kHalves;
 #define LASAD_AP_T(I, O, D, T) append_pages_kernel<I, O, D, T><<<grid, block, 0, s>>>(a, groups)
 #define LASAD_AP(I, O, D) (turn == kNone ? (void)(LASAD_AP_T(I, O, D, kNone)) : turn == kAdjacent ? (void)(LASAD_AP_T(I, O, D, kAdjacent)) : (void)(LASAD_AP_T(I, O, D, kHalves)))
