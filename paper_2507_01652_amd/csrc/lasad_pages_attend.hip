@@ -23,8 +23,9 @@ namespace lasad {
 namespace {
 
 // Workgroup: WAVES wavefronts, CW of them beside each other over CW * NT * 16 columns of a row's key head, WAVES / CW over the pages.
+// (At d = 32 the wide shape's 128 registers are four wavefronts a SIMD's; without the bound it takes two more.)
 template <typename T, typename O, int D, int NQ, int NP, int NT, int CW, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (sizeof(T) == 4 ? 1 : 2) : 3)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (sizeof(T) == 4 ? 1 : 2) : D == 32 ? 4 : 3)
 attend_pages_kernel(AttendArgs a)
 {
     constexpr int KW = WAVES / CW, COLS = CW * NT * 16, NC = D / 16, NF = D / 32;
