@@ -269,7 +269,7 @@ struct Columns {
         };
         const auto start = [&]() __attribute__((always_inline)) {
             scores(t, copy, s);
-            sc = fmaxf(t.k_scale * scale2, 0x1p-126f);               // (a page of zeros has scale 0, and 0 times -infinity is none)
+            sc = fmaxf(t.k_scale * scale2, 0x1p-149f);               // (a page of zeros has scale 0, and 0 times -infinity is none)
         };
         const auto load_next_k = [&]() __attribute__((always_inline)) {
             __builtin_amdgcn_sched_barrier(0);                       // (loads moved up over the products, or conversions over the exponentials, would need registers)

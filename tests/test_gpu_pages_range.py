@@ -1,4 +1,5 @@
-"""Attention over the paged 8-bit cache where values are far from 1: sums of P v that would pass fp32 although the average does not."""
+"""Attention over the paged 8-bit cache where keys or values are far from 1: sums of P v that would pass fp32 although the average does not,
+keys whose scale times the attention's is subnormal."""
 import pytest
 import torch
 
@@ -112,3 +113,27 @@ def test_large_values_in_steps(lasad, case, which):
     want, bound = pr.attend(yq, cpu(pages), table, rows, LAST, window, 0, d ** -0.5, dt, dt)
     bound = bound + query_bound(yq, eq, cpu(pages), table, rows, window, 0, d ** -0.5, dt)
     assert ((o - want).abs() <= bound + LOST).all()
+
+
+@pytest.mark.parametrize("dt", [BF, F])
+@pytest.mark.parametrize("lengths", [[200], [3], [1]])
+def test_small_keys(lasad, dt, lengths):
+    """Keys of 2^-126, held with the least scale, against queries of 2^120: scores of some tenths, from a product of scales below 2^-126."""
+    d, Hq, Hk, p, scale = 64, 4, 2, 300, 0.125
+    T, m = sum(lengths), p + sum(lengths)
+    rows = packed(lengths, [p])
+    table = table_of(rows, 10, 8)
+    pages = pr.new_pool(lasad, 10, Hk, d)
+    k = (ref.draw((m, Hk, d), torch.float64, 5) * 2.0 ** -125).to(F).cuda()
+    v = ref.draw((m, Hk, d), F, 6).cuda()
+    starts = torch.tensor([0, m], dtype=torch.int32).cuda()
+    lasad.lasad_append_pages(None, k, v, pages, table.cuda(), 0, 32, 32, norm_eps=-1.0, rope=0, row_starts=starts)
+    assert (pages.k_scales[table[0, 0].item()] == 2.0 ** -126).all()
+    q = (ref.draw((T, Hq, d), torch.float64, 7) * 2.0 ** 120).to(dt).cuda()
+    t, pos, starts = on_gpu(table, rows, lengths == [1])
+    o = lasad.lasad_forward_pages(q, pages, t, pos, 2 ** 30, 0, row_starts=starts, scale=scale).cpu().double()
+    want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, 2 ** 30, 0, scale, dt, dt)
+    # the product of the scales, 2^-128.5, is rounded by up to 2^-150: 2^-21 of a score; scores below 1
+    kk, vv = pr.values(cpu(pages))
+    slack = torch.expm1(torch.tensor(2 * 2.0 ** -21)) * vv[torch.isfinite(vv)].abs().max()
+    assert ((o - want).abs() <= bound + slack).all()
