@@ -648,8 +648,8 @@ int lasad_append_pages(const void *q, const void *k, const void *v, void *q_out,
  *   workspace lasad_forward_pages_workspace_bytes(...) bytes (one_each: row_starts is NULL), 16-byte aligned: few queries with many keys are
  *             then dealt out over several workgroups.  NULL: they are not (same results up to rounding); a smaller one is
  *             LASAD_ERR_WORKSPACE.  The query answers 0 for sizes that the call refuses.
- * A query that sees nothing has o = 0.  Codes enter the products exactly; with bf16 queries P is rounded to bf16 as a matrix-core operand, everything
- * else is fp32.  Sums are held so that values of any finite size give a finite o; beside pages whose scale is 2^72 or more, keys with less than
+ * A query that sees nothing has o = 0.  Codes enter the products exactly; with bf16 queries P is rounded to bf16 as a matrix-core operand (to 16 bits
+ * where o is fp32), everything else is fp32.  Sums are held so that values of any finite size give a finite o; beside pages whose scale is 2^72 or more, keys with less than
  * 2^-84 of a query's largest weight may count as none.  window, sinks, scale, shared key heads: as in lasad_forward_window.  Results are deterministic.
  */
 size_t lasad_forward_pages_workspace_bytes(int B, int n_q_heads, int n_k_heads, int d, int n_tokens, int one_each, int table_pages,

@@ -8,7 +8,7 @@
 // page a lane (lasad_pages.h).  Nothing passes through LDS but the join of wavefronts that share columns.  Codes become bf16 exactly; a page's
 // scale of k is applied to the scores in fp32, that of v as a power of two with the conversion and the rest in P's exponent.  fp32 queries and P
 // are three bf16 parts each; of bf16 queries P is one, rounded to 2^-9, which is what o's own rounding costs: more parts would
-// double the second product.  Its sums are those of the rounded P.
+// double the second product.  Where o is fp32, and that reason is none, P is two (2^-17).  Its sums are those of the rounded P.
 //
 // 4 x 24 heads over 8, 4096 tokens, window 1024, d = 64: 137 us a pass in a stream, 91 GFLOP, 668 TFLOP/s where a product of 8192^3 reaches 1199.
 // The matrix cores are busy for 0.29 of the time, the vector units for 0.55 (exponentials, conversions of codes and of P, 150 instructions a page
@@ -23,9 +23,10 @@ namespace lasad {
 namespace {
 
 // Workgroup: WAVES wavefronts, CW of them beside each other over CW * NT * 16 columns of a row's key head, WAVES / CW over the pages.
-// (At d = 32 the wide shape's 128 registers are four wavefronts a SIMD's; without the bound it takes two more.)
+// (Wavefronts a SIMD: at d = 32 the wide shape's 128 registers are four's, without the bound it takes two more.  With P in two parts and two
+// tiles at d = 64 three spill 31 registers: 4 x 24 heads over 8, 4096 tokens, 173 us; two without spills 195, one tile 208.)
 template <typename T, typename O, int D, int NQ, int NP, int NT, int CW, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (sizeof(T) == 4 ? 1 : 2) : D == 32 ? 4 : 3)
+__global__ void __launch_bounds__(WAVES * 64, D == 128 ? (sizeof(T) == 4 ? 1 : 2) : D == 32 && NP * NT < 4 ? 4 : 3)
 attend_pages_kernel(AttendArgs a)
 {
     constexpr int KW = WAVES / CW, COLS = CW * NT * 16, NC = D / 16, NF = D / 32;
@@ -187,15 +188,15 @@ void launch_join(const AttendArgs &a, hipStream_t s)
     join_pages_kernel<O, D><<<dim3((unsigned)((int64_t)a.rows.tokens * a.Hq)), dim3(256), 0, s>>>(a);
 }
 
-template <typename T, typename O, int D, int NP>
+template <typename T, typename O, int D, int NQ, int NP>
 hipError_t launch(const AttendArgs &a, hipStream_t s)
 {
     const Shape shape = choose(a);
     const dim3 grid((unsigned)groups_of(a, shape), (unsigned)a.splits);
     constexpr int WIDE = sizeof(T) == 2 && D <= 64 ? 2 : 1;
-    if (shape.cw == 1) attend_pages_kernel<T, O, D, NP, NP, 1, 1, 4><<<grid, dim3(256), 0, s>>>(a);
-    else if (shape.nt == 1) attend_pages_kernel<T, O, D, NP, NP, 1, 4, 4><<<grid, dim3(256), 0, s>>>(a);
-    else attend_pages_kernel<T, O, D, NP, NP, WIDE, 4, 4><<<grid, dim3(256), 0, s>>>(a);
+    if (shape.cw == 1) attend_pages_kernel<T, O, D, NQ, NP, 1, 1, 4><<<grid, dim3(256), 0, s>>>(a);
+    else if (shape.nt == 1) attend_pages_kernel<T, O, D, NQ, NP, 1, 4, 4><<<grid, dim3(256), 0, s>>>(a);
+    else attend_pages_kernel<T, O, D, NQ, NP, WIDE, 4, 4><<<grid, dim3(256), 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         launch_join<O, D>(a, s);
@@ -235,9 +236,9 @@ hipError_t launch_join_pages(const AttendArgs &a, hipStream_t s)
 
 hipError_t launch_attend_pages(const AttendArgs &a, hipStream_t s)
 {
-#define LASAD_AT(T, O, NP) (a.d == 32 ? launch<T, O, 32, NP>(a, s) : a.d == 64 ? launch<T, O, 64, NP>(a, s) : launch<T, O, 128, NP>(a, s))
-    if (a.io_dtype == LASAD_F32) return LASAD_AT(float, float, 3);
-    return a.out_dtype == LASAD_BF16 ? LASAD_AT(uint16_t, uint16_t, 1) : LASAD_AT(uint16_t, float, 1);
+#define LASAD_AT(T, O, NQ, NP) (a.d == 32 ? launch<T, O, 32, NQ, NP>(a, s) : a.d == 64 ? launch<T, O, 64, NQ, NP>(a, s) : launch<T, O, 128, NQ, NP>(a, s))
+    if (a.io_dtype == LASAD_F32) return LASAD_AT(float, float, 3, 3);
+    return a.out_dtype == LASAD_BF16 ? LASAD_AT(uint16_t, uint16_t, 1, 1) : LASAD_AT(uint16_t, float, 1, 2);
 #undef LASAD_AT
 }
 
