@@ -78,17 +78,10 @@ attend_pages_kernel(AttendArgs a)
             if (x.p[n] < 0) continue;
             const int c = c0 + 16 * n + col, token = c / G, h = hk * G + c - token * G;
             const float inv = x.l[n] == 0.f ? 0.f : 1.f / x.l[n];
-            if (a.splits > 1) {
-                float *p = a.parts + (((int64_t)(row.first + token) * a.Hq + h) * a.splits + split) * (D + 4);
+            O *op = (O *)a.o + (int64_t)(row.first + token) * a.lo.stride_n + h * a.lo.stride_h + 4 * quad;
 #pragma unroll
-                for (int b = 0; b < NC; ++b) *(float4 *)(p + 16 * b + 4 * quad) = make_float4(x.acc[n][b][0], x.acc[n][b][1], x.acc[n][b][2], x.acc[n][b][3]);
-                if (quad == 0) { p[D] = x.m[n]; p[D + 1] = x.l[n]; }
-            } else {
-                O *op = (O *)a.o + (int64_t)(row.first + token) * a.lo.stride_n + h * a.lo.stride_h + 4 * quad;
-#pragma unroll
-                for (int b = 0; b < NC; ++b)
-                    store4(op + 16 * b, x.acc[n][b][0] * inv, x.acc[n][b][1] * inv, x.acc[n][b][2] * inv, x.acc[n][b][3] * inv);
-            }
+            for (int b = 0; b < NC; ++b)
+                store4(op + 16 * b, x.acc[n][b][0] * inv, x.acc[n][b][1] * inv, x.acc[n][b][2] * inv, x.acc[n][b][3] * inv);
         }
     } else {
         static_assert(CW == 1 && NT == 1, "wavefronts over the pages have one tile of columns");
@@ -166,6 +159,10 @@ join_pages_kernel(AttendArgs a)
 // 53.6 and 65.3.
 constexpr int64_t kFull = 384;
 
+// Up to 32 columns a row on average: a workgroup's wavefronts share 16 of them over the pages, and splits share them over workgroups.
+// With more, each wavefront has columns of its own, and writes their results itself.
+bool few_columns(int64_t B, int64_t tokens, int G) { return tokens * G <= 32 * B; }
+
 // How a launch divides its columns.
 struct Shape {
     int nt, cw;
@@ -174,8 +171,7 @@ struct Shape {
 Shape choose(const AttendArgs &a)
 {
     const int G = a.Hq / a.pages.heads;
-    const int64_t columns = (int64_t)a.rows.tokens * G;
-    if (columns <= 32 * (int64_t)a.rows.B) return {1, 1};
+    if (few_columns(a.rows.B, a.rows.tokens, G)) return {1, 1};
     const Shape wide = {2, 4};
     const bool full = row_slots(a.rows, G, wide.columns(), 1) * a.pages.heads >= kFull;
     return {a.io_dtype == LASAD_BF16 && a.d <= 64 && full ? 2 : 1, 4};
@@ -212,9 +208,9 @@ int64_t attend_pages_groups(const AttendArgs &a) { return groups_of(a, choose(a)
 // Splits of a call whose rows see up to `seen` keys.
 int attend_pages_splits(int64_t B, int64_t tokens, int Hq, int Hk, bool one_each, int64_t seen)
 {
-    const int64_t columns = tokens * (Hq / Hk);
-    if (columns > 32 * B) return 1;
-    const int64_t groups = (one_each ? B * ((Hq / Hk + 15) / 16) : columns / 16 + B) * Hk;
+    const int G = Hq / Hk;
+    if (!few_columns(B, tokens, G)) return 1;
+    const int64_t groups = (one_each ? B * ((G + 15) / 16) : tokens * G / 16 + B) * Hk;
     int64_t n = 512 / groups;
     if (seen < 1536 || n < 4) return 1;
     if (n > seen / 512) n = seen / 512;
