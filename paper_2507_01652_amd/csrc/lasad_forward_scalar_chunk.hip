@@ -610,6 +610,7 @@ forward_scalar_chunk_kernel(ForwardArgs a, MultiPass m)
                     accS[t] = mfma16(k, fl, accS[t]);
                 }
             }
+            wait_for_products();
             if (MANY && --left == 0 && !last) {
                 finish();
                 begin();

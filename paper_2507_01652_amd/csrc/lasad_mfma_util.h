@@ -76,6 +76,14 @@ __device__ inline f32x4v mfma16(const Frag &a, const Frag &b, f32x4v acc)     //
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, acc, 0, 0, 0);
 }
 
+// Behind a block's last product of 16 x 16 x 32: the wait states that what reads its result must keep.  The compiler puts them in itself, but
+// leaves some out where a branch lies between (seen where a loop jumps back to moves of the sums at its head, which were stale then).
+__device__ inline void wait_for_products()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 7");
+}
+
 // Constants of the hi/lo split: the packed bf16 pairs (-1, 0) and (0, -1).  They are kept
 // opaque to the compiler (in VGPRs) because, folded into an inline constant of
 // v_dot2c_f32_bf16, -1.0 is encoded in the fp16 format and the product comes out wrong.

@@ -137,14 +137,6 @@ struct Columns {
     float m[NT], l[NT];
     f32x4v acc[NT][NC];
 
-    // The compiler counts too few wait states from a block's last product to moves of its result in the next one (seen at a loop's head with d = 32,
-    // where the second half of the sums was stale): these are enough.
-    static __device__ inline void wait_for_products()
-    {
-        __builtin_amdgcn_sched_barrier(0);
-        asm volatile("s_nop 7");
-    }
-
     // Scores of a page, 16 positions x 16 columns a product.
     __device__ inline void scores(const PagePart<D> &t, int copy, f32x4v (&s)[NT][NB]) const
     {
