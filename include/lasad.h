@@ -612,7 +612,8 @@ int lasad_decode_step_window(const void *q, const void *k, const void *v, void *
  * Rows.  A call has new tokens of B rows, one row's behind the other's: row b has tokens row_starts[b] .. row_starts[b + 1] - 1
  * (row_starts int32 [B + 1], device, not falling; tokens outside belong to no row, and what belongs to them is left as it was), at positions
  * pos_rows[b], pos_rows[b] + 1, ..  (pos_rows int32 [B], device; NULL: pos for all).  row_starts NULL: one token a row, n_tokens = B.  A row
- * with a position that is negative, off the grid or behind the table is inactive: nothing is written for it.
+ * with a position that is negative, off the grid or behind the table is inactive: nothing is written for it.  (lasad_forward_pages knows no
+ * grid: a row that is off it is inactive there only if its position is negative or behind the table.)
  */
 typedef struct {
     uint8_t *k_pages, *v_pages;

@@ -1259,7 +1259,8 @@ def lasad_forward_pages(q: torch.Tensor, pages: Pages, table: torch.Tensor, pos,
                         out: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
                         workspace: torch.Tensor | None = None, use_workspace: bool = True, stream=None) -> torch.Tensor:
     """lasad_forward_window of packed queries [T, Hq, d] (normed and rotated, their keys appended) over the rows' pages; rows, positions and
-    table as in lasad_append_pages.  Queries of inactive rows and of none are left as they were in `out`."""
+    table as in lasad_append_pages.  Queries of inactive rows (a position that is negative or behind the table; no grid is known here) and of
+    none are left as they were in `out`."""
     if out is None and out_dtype is None and workspace is None and use_workspace and stream is None:
         done = _fast("forward_pages", q, pages, table, pos, window, sinks, row_starts, _scale(scale, q))
         if done is not None:

@@ -9,12 +9,12 @@
 // A wavefront has 2048 numbers of one head of one page (queries, keys or values), in registers, so that A is known before the first code is formed:
 // of queries and keys 2048 / d tokens, a lane 8 channels of four of them in a row; of values 32 channels, a lane two of the 16 tokens whose
 // codes are 16 bytes in a row of a channel.  d / 32 wavefronts share a head and tell each other their maxima.  Twice as many numbers a lane
-// (no sharing at d = 64) took registers for two or three wavefronts a SIMD instead of four: 66 us where this takes 60.  Values in the same
-// wavefront as their keys, in the keys' order and with codes of 4 bytes: 98.  What the next head needs is on its way while one is worked on, and
+// (no sharing at d = 64) took registers for two or three wavefronts a SIMD instead of four: 66 us for the 252 MB below, where this took 60 then.  Values in
+// the same wavefront as their keys, in the keys' order and with codes of 4 bytes, before that: 98.  What the next head needs is on its way while one is worked on, and
 // the first one's before the table of angles is formed.
 //
-// Bound by memory: every number is read once, codes are written once.  4 x 4096 tokens of 72 heads in bf16, d = 64 (252 MB): 54 us, 4.6 TB/s where a
-// copy of 1 GiB reaches 5.0.  32 rows of 22 to 200 tokens of 36 heads (27 MB): 15, two rounds of latencies (row, page, numbers) and of
+// Bound by memory: every number is read once, codes are written once.  4 x 4096 tokens of 72 heads in bf16, d = 64 (252 MB): 54 us by itself, 4.6 TB/s where
+// a copy of 1 GiB reaches 5.0; 58 a pass in a stream.  32 rows of 22 to 200 tokens of 36 heads (27 MB): 15, two rounds of latencies (row, page, numbers) and of
 // workgroups on partly filled pages; one token of 36 heads 5.6, a launch and those latencies.
 #include <type_traits>
 
@@ -266,7 +266,7 @@ append_pages_kernel(AppendArgs a, int groups)
 }
 
 // Workgroups of a page's heads: as many as its heads can have, fewer where the pages alone fill the chip twice over, as each forms the table of
-// angles for itself (want 512 of them: 252 MB as above 60 us, 1024 64, 256 90; 27 MB 15.5, 17.1, 18.2).
+// angles for itself (want 512 of them: 252 MB as above 57.9 us, 1024 63.0, 256 87; 27 MB 14.9, 16.7, 17.6).
 int64_t slots_of(const AppendArgs &a) { return row_slots(a.rows, 1, kPage, 2); }
 
 int head_groups(const AppendArgs &a)

@@ -10,8 +10,8 @@
 // are three bf16 parts each; of bf16 queries P is one, rounded to 2^-9, which is what o's own rounding costs: more parts would
 // double the second product.  Where o is fp32, and that reason is none, P is two (2^-17).  Its sums are those of the rounded P.
 //
-// 4 x 24 heads over 8, 4096 tokens, window 1024, d = 64: 137 us a pass in a stream, 91 GFLOP, 668 TFLOP/s where a product of 8192^3 reaches 1199.
-// The matrix cores are busy for 0.29 of the time, the vector units for 0.55 (exponentials, conversions of codes and of P, 150 instructions a page
+// 4 x 24 heads over 8, 4096 tokens, window 1024, d = 64: 138 us a pass in a stream (148 alone), 91 GFLOP, 660 TFLOP/s where a product of 8192^3 reaches 1199.
+// The matrix cores are busy for 0.29 of the time, the vector units for 0.55 (exponentials, conversions of codes and of P, 164 instructions a page
 // of 64 keys and 32 columns), and three wavefronts a SIMD do not always have one of each.  On the way: sums of P by additions and both
 // scales by products 343; with the search for a maximum in every page 197; with the accumulators moved twice a page by it 167; with keys that
 // waited for the values behind them 154; 48 columns a wavefront 151 then, 64 176, 16 200.  Rows of 128 to 256 tokens (12 heads, window 128): 8.5 us, a
@@ -155,12 +155,14 @@ join_pages_kernel(AttendArgs a)
 }
 
 // Workgroups of 128 columns from which on they are taken instead of 64 (bf16, d up to 64; a page's codes are then turned into bf16 once for 32 columns,
-// not 16, by three wavefronts a SIMD instead of four).  12 heads, window 512: 288 workgroups 11.8 us, with 64 columns 9.0; 480 17.2 and 18.3; 1632
-// 53.6 and 65.3.
+// not 16, by three wavefronts a SIMD instead of four).  12 heads, window 512: 288 workgroups 11.8 us, with 64 columns 9.2; 480 17.6 and 18.8; 1632
+// 51.9 and 63.9.
 constexpr int64_t kFull = 384;
 
 // Up to 32 columns a row on average: a workgroup's wavefronts share 16 of them over the pages, and splits share them over workgroups.
-// With more, each wavefront has columns of its own, and writes their results itself.
+// With more, each wavefront has columns of its own, and writes their results itself.  (8 rows of 12 heads, us with wavefronts over the pages and
+// with columns of their own: 32 tokens on 200 keys 5.4 and 6.6, on 1000 10.5 and 15.9, on 4000 22 and 44; 48 tokens 5.5 and 6.7, 10.5 and 16.0,
+// 22 and 44; 64 tokens 6.7 and 7.9, 10.6 and 16.2, 22 and 46.  So the border could lie higher; where it should has not been measured.)
 bool few_columns(int64_t B, int64_t tokens, int G) { return tokens * G <= 32 * B; }
 
 // How a launch divides its columns.
@@ -205,7 +207,8 @@ hipError_t launch(const AttendArgs &a, hipStream_t s)
 
 int64_t attend_pages_groups(const AttendArgs &a) { return groups_of(a, choose(a)) * a.splits; }
 
-// Splits of a call whose rows see up to `seen` keys.
+// Splits of a call whose rows see up to `seen` keys, by the step's rule (lasad_pages_step.hip, where it was measured; here: two rows of 24 and fewer
+// tokens, 16 heads, 16448 keys for 512 workgroups 17.4 us, 256 18.4, 1024 18.9).
 int attend_pages_splits(int64_t B, int64_t tokens, int Hq, int Hk, bool one_each, int64_t seen)
 {
     const int G = Hq / Hk;

@@ -8,10 +8,11 @@
 // again, unless the page's scale had to grow.
 //
 // bf16 queries are two bf16 parts and so is P: what a step adds to o's error is far below o's own rounding.  Bound by memory where there is enough:
-// 128 rows of 20 heads that see 24 to 4001 keys (767 MB) 151 us, 5.1 TB/s; 64 rows of 24 heads over 8, 1040 keys (58 MB) 15.1 us, 3.9; two rows of
-// 16 heads, 16448 keys (67 MB) 14 in 16 parts and 4 for their join; one row of 12 heads 6.7, of which the launch, position and table take 2.3: the chain position, page, codes, norms, products,
-// join.  With up to eight query heads a key head a tile holds copies of them (Columns): 16 columns for 3 heads would
-// raise four times as many scores to powers.
+// 128 rows of 20 heads that see 24 to 4001 keys (767 MB) 151 us, 5.1 TB/s; 64 rows of 24 heads over 8, 1040 keys (58 MB) 15.2 us, 3.9; two rows of
+// 16 heads, 16448 keys (67 MB) 14 in 16 parts and 4 for their join; one row of 12 heads 6.7, of which the launch, position and table take 2.3: the
+// chain position, page, codes, norms, products, join.  With up to eight query heads a key head a tile holds copies of them (Columns): 16 columns for 3 heads would
+// raise four times as many scores to powers (64 rows of 8 key heads, 1040 keys, in a graph: one to four heads each 16.6 us, without copies 17.0 to 17.2, with
+// two 16.6; five to eight 16.7, without copies 17.1).
 #include "lasad_heads.h"
 #include "lasad_pages_codes.h"
 #include "lasad_pages_tile.h"
@@ -317,7 +318,13 @@ hipError_t launch(const AppendArgs &a, const AttendArgs &t, hipStream_t s)
 
 int64_t step_pages_groups(const AttendArgs &t) { return (int64_t)t.rows.B * t.pages.heads * t.splits; }
 
-// Splits of a step whose rows see up to `seen` keys: for 512 workgroups in all (two rows of 16 heads, 16448 keys: 19.6 us; for 256 20.7, 1024 21.5, each a little less since).
+// Splits of a step whose rows see up to `seen` keys.  us, d = 64, as many query heads as key heads; a join costs some 4:
+//   512 workgroups in all: two rows of 16 heads, 16448 keys 17.9; 256 19.0, 1024 19.5.
+//   from 1536 keys on: two rows of 16 heads 1100 keys 9.8, split 11.0; 1600 11.1 and 11.1 split, 2000 11.8 and 10.3, 4000 17.9 and 12.7.
+//   four at least: 8 rows of 16 heads 4000 keys 18.3, in four 17.6; 9 rows 18.6, in three 19.5; 16 rows 30.0, in two 32.9.  (At 16000 keys 68 and 55,
+//     71 and 62, 95 and 100: with so many three are worth their join, which the rule leaves out.)
+//   512 keys each: one row of 16 heads, 4000 keys 11.0; 256 10.4, 1024 13.0; 8000 keys 12.8; 13.2, 13.6; 2000 keys 10.3; 9.3, 11.7.
+//   64 at most: one row of 4 heads, 65000 keys 14.5; 32 15.9, 128 15.8; 40000 13.3; 13.6, 14.0.
 int step_pages_splits(int64_t B, int Hq, int Hk, int64_t seen)
 {
     int64_t n = 512 / (B * Hk);

@@ -49,7 +49,8 @@ __device__ inline void split_pair(float x, float y, uint32_t (&part)[N])
 __device__ inline uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }     // 0x80 where a code is NaN
 
 // A number at an address that is the same in all lanes, through the scalar cache: one more vector load between those of the pages would have
-// the next page's keys wait for the values behind it.  (No kernel reads what it has written like this.)
+// the next page's keys wait for the values behind it.  The scalar cache does not see what the same launch writes: the step, which writes the
+// scales of a row's last page, may find the old ones here, and has to put the new ones in their place (NewKey::put).
 template <typename T>
 __device__ inline T scalar_load(const T *p) { return *(const __attribute__((address_space(4))) T *)(uintptr_t)p; }
 
@@ -237,7 +238,7 @@ struct Columns {
     //
     // A page's P adds up to 2^16, that of 2^24 pages to 2^40: from values of 2^72 448 on the sums could pass fp32 although their average
     // does not.  The first page whose scale is 2^72 or more goes the long way, where the maximum is raised by 2^42 for good: P and its sums are
-    // less by as much, and what divides them too.  (4 x 24 heads over 8, 4096 tokens: 138.5 us without it, 139.9 with it.)
+    // less by as much, and what divides them too.  (4 x 24 heads over 8, 4096 tokens: 138.6 us with it and without.)
     template <bool FINISH, typename Next, typename LoadK, typename LoadV, typename Finish>
     __device__ __forceinline__ void run(PagePart<D> &t, const PageList &list, int i, int step, int page, float scale2, int window, int sinks, int lane, Next next,
                                         LoadK load_k, LoadV load_v, Finish finish)
