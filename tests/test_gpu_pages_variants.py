@@ -136,3 +136,46 @@ def test_step(lasad, dt, odt, d, G, by_k, by_v):
         want, bound = pr.attend(yq, now, table, rows, LAST, window, sinks, d ** -0.5, dt, odt)
         bound = bound + query_bound(yq, eq, now, table, rows, window, sinks, d ** -0.5, dt)
         assert ((o - want).abs() <= bound + 2.0 ** -112).all(), (split, ((o - want).abs() / bound).max().item())
+
+
+@pytest.mark.parametrize("lengths, few", [([20, 12], True), ([20, 13], False), ([31, 1], True), ([63, 1], False), ([1, 64], False)])
+@pytest.mark.parametrize("dt", [BF, F])
+def test_attention_at_the_border_of_few_columns(lasad, lengths, few, dt):
+    """32 columns a row on average, and one token more: wavefronts over the pages and splits, and neither."""
+    d, Hq, Hk, positions, window = 32, 4, 2, [2000, 1900], 2 ** 30
+    rows = packed(lengths, positions)
+    T = sum(lengths)
+    table = table_of(rows, 66, 8)
+    assert (lasad.lasad_forward_pages_workspace_bytes(2, Hq, Hk, d, T, False, table.shape[1], window, 0) > 0) == few
+    pages = pr.filled_pool(lasad, 66, Hk, d, 12, spread=1.5)
+    spoil(pages, table, rows)
+    q = ref.draw((T, Hq, d), dt, 30).cuda()
+    t, pos, starts = on_gpu(table, rows)
+    want, bound = pr.attend(q.cpu().double(), cpu(pages), table, rows, LAST, window, 0, d ** -0.5, dt, dt)
+    for use in (True, False):
+        o = lasad.lasad_forward_pages(q, pages, t, pos, window, row_starts=starts, use_workspace=use).cpu().double()
+        # (fp64 has exponentials that fp32 has not: 2^11 of them below 2^-126 of the largest, values below 2^4)
+        assert ((o - want).abs() <= bound + 2.0 ** -111).all(), (use, ((o - want).abs() / bound).max().item())
+
+
+@pytest.mark.parametrize("B, Hk, split", [(64, 2, True), (43, 3, False), (128, 1, True), (129, 1, False)])
+def test_step_at_the_border_of_splits(lasad, B, Hk, split):
+    """128 rows times key heads, the most that are split, and one more; a few long rows among short ones."""
+    d, G, grid, window, dt = 32, 2, (50, 50), 2 ** 30, BF
+    positions = [2100 if b in (0, B - 1) else (37 * b) % 150 for b in range(B)]
+    rows = [(b, 1, p) for b, p in enumerate(positions)]
+    need = sum(p // 64 + 1 for p in positions)
+    table = table_of(rows, need, 8)
+    assert (lasad.lasad_decode_step_pages_workspace_bytes(B, G * Hk, Hk, d, table.shape[1], window, 0) > 0) == split
+    pages = pr.filled_pool(lasad, need, Hk, d, 12)
+    before = cpu(pages)
+    q, k, v = (t.contiguous() for t in project(B, G * Hk, Hk, d, dt, 50))
+    t, pos, _ = on_gpu(table, rows)
+    yk, ek = expected(k, None, rows, B, grid[1], 2, False, EPS, dt)
+    yq, eq = expected(q, None, rows, B, grid[1], 2, False, EPS, dt)
+    o = lasad.lasad_decode_step_pages(q, k, v, pages, t, pos, *grid, window).cpu().double()
+    now = cpu(pages)
+    pr.check_append(before, now, table, rows, 2500, yk, ek, v.cpu().double())
+    want, bound = pr.attend(yq, now, table, rows, LAST, window, 0, d ** -0.5, dt, dt)
+    bound = bound + query_bound(yq, eq, now, table, rows, window, 0, d ** -0.5, dt)
+    assert ((o - want).abs() <= bound + 2.0 ** -112).all(), ((o - want).abs() / bound).max().item()
